@@ -13,11 +13,13 @@
  * entries (topk_threshold, normally one more pass over M; dual_eval_sparsify_topk
  * finds it inside the fused pass: one pass for both), and calls that work
  * on the sparse pattern only (pattern_*, hessian_*, pcg_solve, pcg_solve2, splr_direction)
- * or on vectors (dual_metrics, choose_candidate).
+ * or on vectors (dual_metrics, choose_candidate).  The row calls (row_logprob, row_distill, row_route) take a
+ * model's scores in fp32, bf16 or fp16 in place of M.
  *
  * Conventions common to all calls
  *   - All array arguments are DEVICE pointers (HBM of the current HIP device)
- *     unless the parameter comment says "host".  Everything is fp64; indices
+ *     unless the parameter comment says "host".  Everything is fp64 (but for the row
+ *     calls, which say what they take); indices
  *     are int32 (columns) and int64 (row offsets).
  *   - M is row-major with leading dimension ldM >= m (in elements).  When M is
  *     16-byte aligned and ldM is even the kernels use 128-bit loads; otherwise
@@ -536,6 +538,132 @@ int regot_splr_direction(int64_t n, int64_t m,
                          double *d,
                          double *info,                          /* [2] out */
                          void *workspace, size_t workspace_bytes, regot_stream_t stream);
+
+/*
+ * ---- Rows of scores in the types of a model: the row-conditional plan ----
+ *
+ * Where the dense calls work on the fp64 cost matrix M of a solve, these work on the matrix S of scores that a model
+ * gives its n rows (tokens, samples) against m columns (vocabulary, prototypes, experts): S_ij = -M_ij is what the model
+ * is trained through.  The plan entry T_ij = exp{(alpha_i + beta_j - M_ij)/eta} divided by its row sum does not
+ * depend on alpha:
+ *     x_ij = S_ij + bias_j,    p_ij = exp(x_ij / eta) / sum_j exp(x_ij / eta)
+ * with bias = beta, the column duals of a solve (regot_sinkhorn_sweeps), or none.  The calls give log p at given columns,
+ * the row's entropy and its largest entries (what a model answers, and the sparse targets of a balanced plan), the loss of
+ * a model's rows against sparse targets with its gradient, and the choice of k columns for each row (routing of tokens to
+ * experts, balanced by the same duals), with their gradients to S.
+ *   - `type` is the type of S and of a gradient dS: REGOT_F32, REGOT_BF16 or REGOT_F16.  Everything else is fp32 and
+ *     int32; maxima, sums and exponents are held in fp32 and a gradient is rounded to its type once.  S and dS are row-major with
+ *     leading dimensions ldS, ldD >= m in elements, aligned to their elements (wide loads are used from each row's first
+ *     16-byte boundary on, whatever the row's start is).
+ *   - Lists per row (targets, teacher entries, choices, alternatives) are dense arrays of n rows.  An index outside
+ *     [0, m), such as -1, is no entry.  A column listed twice counts twice.
+ *   - A score of -inf (a mask), or a bias of -inf, is a forbidden column: p = 0.  A row that has no other score (or m = 0) has no distribution: its
+ *     maximum and log-sum are -inf, log p is -inf, its entropy 0, it has no alternatives, and its gradient is 0.
+ *     A mask of the type's lowest finite value is a score like any other.  A row that holds a NaN, or a score of +inf, gives NaN for
+ *     every number of the row and -1 for every index.
+ *   - Sums are added up in a fixed order: the same call gives the same bits.  n, m >= 0.
+ */
+enum { REGOT_F32 = 0, REGOT_BF16 = 1, REGOT_F16 = 2 };
+
+/*
+ * Log probabilities of given columns, entropy and the most probable columns of each row:
+ *     logprob[i*targets + t]   ln p_ij at j = target[i*targets + t]; 0 where that is no entry
+ *     entropy[i]               -sum_j p_ij ln p_ij                              (optional, may be NULL)
+ *     stats[2i], stats[2i+1]   max_j x_ij and ln sum_j exp((x_ij - max)/eta)    (optional; what the gradient takes;
+ *                              the log-sum-exp of x/eta is stats[2i]/eta + stats[2i+1])
+ *     top_idx, top_logprob[i*k ..]  the k columns of largest x_ij, the largest first, equal ones by ascending column,
+ *                              and their ln p; -1 and -inf where the row has fewer that are not forbidden
+ * targets = 0 (target and logprob may be NULL) and k = 0 (top_* may be NULL) leave that part out.
+ * 0 <= targets <= REGOT_ROW_MAX_LIST, 0 <= k <= REGOT_ROW_MAX_TOP.  S is read once.
+ */
+#define REGOT_ROW_MAX_LIST 1024
+#define REGOT_ROW_MAX_TOP 128
+int regot_row_logprob_workspace_bytes(int64_t n, int64_t m, int k, size_t *bytes /* host, out */);
+int regot_row_logprob(int64_t n, int64_t m,
+                      const void *S, int type, int64_t ldS,
+                      const float *bias,                         /* [m], optional */
+                      double eta,
+                      const int32_t *target, int targets,        /* [n * targets] */
+                      int k,
+                      float *logprob,                            /* [n * targets] out */
+                      float *entropy, float *stats,              /* [n], [2n] out, optional */
+                      int32_t *top_idx, float *top_logprob,      /* [n * k] out */
+                      void *workspace, size_t workspace_bytes, regot_stream_t stream);
+
+/*
+ * The gradient of sum_it g_logprob_it logprob_it + sum_i g_entropy_i entropy_i to S:
+ *     dS_ij = (1/eta) [ sum_t g_logprob_it (1[j = target_it] - p_ij) - g_entropy_i p_ij (ln p_ij + entropy_i) ]
+ * stats and entropy are regot_row_logprob's for the same S, bias and eta.  g_logprob NULL (then target too, targets = 0)
+ * or g_entropy NULL (then entropy too) leaves that part out.  No gradient is formed for bias.  No workspace.
+ */
+int regot_row_logprob_grad(int64_t n, int64_t m,
+                           const void *S, int type, int64_t ldS,
+                           const float *bias, double eta,
+                           const int32_t *target, int targets,
+                           const float *stats, const float *entropy,
+                           const float *g_logprob,               /* [n * targets] */
+                           const float *g_entropy,               /* [n] */
+                           void *dS, int64_t ldD,                /* [n][ldD] out */
+                           regot_stream_t stream);
+
+/*
+ * Distillation: the divergence of each row's distribution from a sparse target, and its gradient in the same call.
+ *     q_il    = softmax of t_score[i*k + l] / eta over the entries l of row i's list (t_idx[i*k + l] = its column)
+ *     loss[i] = sum_l q_il (ln q_il - ln p_ij),  j = t_idx[i*k + l]
+ *     dS_ij   = (row_weight_i / eta) (p_ij - sum of q_il over l with t_idx = j)
+ * t_score may be scores or log probabilities (top_idx and top_logprob of regot_row_logprob are a target): a constant added
+ * to a row's list changes nothing.  row_weight [n] is d(total loss)/d loss_i, NULL for 1.  dS NULL: the loss alone.
+ * A row without entries, or whose entries all have the score -inf, is padding: loss 0, gradient 0, whatever S holds there.
+ * A forbidden column that the target gives weight makes the loss +inf.
+ * 1 <= k <= REGOT_ROW_MAX_LIST.
+ */
+int regot_row_distill_workspace_bytes(int64_t n, int64_t m, int k, size_t *bytes /* host, out */);
+int regot_row_distill(int64_t n, int64_t m,
+                      const void *S, int type, int64_t ldS, double eta,
+                      const int32_t *t_idx, const float *t_score, int k,  /* [n * k] */
+                      const float *row_weight,                   /* [n], optional */
+                      float *loss,                               /* [n] out */
+                      void *dS, int64_t ldD,                     /* [n][ldD] out, optional */
+                      void *workspace, size_t workspace_bytes, regot_stream_t stream);
+
+/*
+ * Routing: k of m columns (experts) for each row (token), and their weights.
+ *     s_ij    = softmax of row i at j (score = REGOT_SOFTMAX), or 1 / (1 + exp(-S_ij)) (REGOT_SIGMOID)
+ *     key_ij  = S_ij where bias is NULL (the order of s), s_ij + bias_j (bias_on = REGOT_BIAS_SCORE) or S_ij + bias_j
+ *               (REGOT_BIAS_LOGIT: the order of the plan at column duals bias, eta = 1)
+ *     groups  > 1: the columns are `groups` runs of m / groups; a group's value is its largest key (group_by =
+ *             REGOT_GROUP_MAX) or the sum of its two largest (REGOT_GROUP_TOP2), of s_ij in place of key_ij where bias is NULL; the groups_kept groups
+ *             of largest value stay, the columns of the others are not chosen
+ *     idx[i*k ..]     the k columns of largest key, the largest first; equal keys, and equal groups, by ascending index
+ *     weight[i*k ..]  scale * s_ij, divided by the sum of the chosen s where renormalise = 1 (0 where that sum is 0): the bias only chooses
+ * Keys are compared as fp32 numbers.  A column whose score or key is -inf is not chosen and is left out of its group's value; idx is -1 and weight 0 where
+ * fewer than k can be.  A row with a NaN key, or that has no softmax, has idx -1 and weight NaN.
+ * 0 <= m <= REGOT_ROW_MAX_EXPERTS, 1 <= k <= REGOT_ROW_MAX_CHOICES, 1 <= groups_kept <= groups <= 64, groups divides m.
+ */
+#define REGOT_ROW_MAX_EXPERTS 1024
+#define REGOT_ROW_MAX_CHOICES 32
+enum { REGOT_SOFTMAX = 0, REGOT_SIGMOID = 1 };
+enum { REGOT_BIAS_SCORE = 0, REGOT_BIAS_LOGIT = 1 };
+enum { REGOT_GROUP_MAX = 0, REGOT_GROUP_TOP2 = 1 };
+int regot_row_route(int64_t n, int64_t m,
+                    const void *S, int type, int64_t ldS,
+                    const float *bias, int bias_on,              /* [m], optional */
+                    int score, int groups, int groups_kept, int group_by,
+                    int k, int renormalise, double scale,
+                    int32_t *idx, float *weight,                 /* [n * k] out */
+                    regot_stream_t stream);
+
+/*
+ * The gradient of sum g_weight * weight to S at the choices idx (which are not differentiated, and may come from elsewhere): with
+ * c the chosen columns, ds_c = scale g_c, or scale (g_c - sum_c g_c s_c / Z) / Z with Z = sum_c s_c where renormalise = 1 (0 where Z = 0),
+ *     dS_ij = s_ij (ds_ij - sum_c ds_c s_c)   (softmax),     ds_ij s_ij (1 - s_ij)   (sigmoid),   ds = 0 outside c.
+ */
+int regot_row_route_grad(int64_t n, int64_t m,
+                         const void *S, int type, int64_t ldS, int score,
+                         const int32_t *idx, int k, int renormalise, double scale,
+                         const float *g_weight,                  /* [n * k] */
+                         void *dS, int64_t ldD,                  /* [n][ldD] out */
+                         regot_stream_t stream);
 
 /*
  * Measurement aid, not part of the method: one pass over M with the tiling and the loads of the dense

@@ -42,6 +42,13 @@ SYMBOLS = (
     "regot_pcg_solve_reduced",
     "regot_pcg_solve2_reduced",
     "regot_splr_direction",
+    "regot_row_logprob_workspace_bytes",
+    "regot_row_logprob",
+    "regot_row_logprob_grad",
+    "regot_row_distill_workspace_bytes",
+    "regot_row_distill",
+    "regot_row_route",
+    "regot_row_route_grad",
     "regot_profile_stage1",
     "regot_sweep_patience",
     "regot_stream_read_probe",
@@ -101,6 +108,14 @@ def load():
                                      ctypes.c_int, p, p, sz, p]
     lib.regot_pcg_solve2_reduced.argtypes = lib.regot_pcg_solve2.argtypes
     lib.regot_splr_direction.argtypes = [i64, i64, p, p, p, p, p, p, p, p, sz, p]
+    c_int = ctypes.c_int
+    lib.regot_row_logprob_workspace_bytes.argtypes = [i64, i64, c_int, ctypes.POINTER(sz)]
+    lib.regot_row_logprob.argtypes = [i64, i64, p, c_int, i64, p, dbl, p, c_int, c_int, p, p, p, p, p, p, sz, p]
+    lib.regot_row_logprob_grad.argtypes = [i64, i64, p, c_int, i64, p, dbl, p, c_int, p, p, p, p, p, i64, p]
+    lib.regot_row_distill_workspace_bytes.argtypes = [i64, i64, c_int, ctypes.POINTER(sz)]
+    lib.regot_row_distill.argtypes = [i64, i64, p, c_int, i64, dbl, p, p, c_int, p, p, p, i64, p, sz, p]
+    lib.regot_row_route.argtypes = [i64, i64, p, c_int, i64, p, c_int, c_int, c_int, c_int, c_int, c_int, c_int, dbl, p, p, p]
+    lib.regot_row_route_grad.argtypes = [i64, i64, p, c_int, i64, c_int, p, c_int, c_int, dbl, p, p, i64, p]
     lib.regot_profile_stage1.argtypes = [p, p]
     lib.regot_sweep_patience.argtypes = [ctypes.c_int]
     lib.regot_stream_read_probe.argtypes = [i64, i64, p, i64, p, p, sz, p]
@@ -469,6 +484,122 @@ def regot_splr_direction(n, m, p, q, s_prev, y_prev, v, d, info, *, workspace, s
         _p(_vector(s_prev, N, "s_prev", optional=True)), _p(_vector(y_prev, N, "y_prev", optional=True)),
         _p(_vector(v, N, "v", optional=True)), _p(_vector(d, N, "d")), _p(_vector(info, 2, "info")),
         *_ws(workspace), _stream(stream)), "regot_splr_direction")
+
+
+# ---- rows of scores (fp32, bf16 or fp16) -----------------------------------------------------------------------------
+
+SCORE_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+SCORE_KINDS = {"softmax": 0, "sigmoid": 1}
+BIAS_ON = {None: 0, "score": 0, "logit": 1}
+GROUP_BY = {"max": 0, "top2": 1}
+
+
+def _scores(S: torch.Tensor, name="S"):
+    """(n, m, type, ldS, pointer) of a matrix of scores.  Its rows may lie apart (a view of some of a wider matrix's columns),
+    but its columns may not, and rows may not share memory."""
+    if not isinstance(S, torch.Tensor) or not S.is_cuda or S.dim() != 2 or S.dtype not in SCORE_TYPES:
+        raise TypeError(f"{name} must be a 2-D float32, bfloat16 or float16 CUDA tensor")
+    n, m = S.shape
+    ld, unit = S.stride()
+    if n <= 1 or m == 0:
+        ld = max(m, 1)
+    if (m > 1 and unit != 1) or ld < m:
+        raise TypeError(f"{name} must be row-major (unit stride along columns, a row stride of at least m = {m})")
+    return n, m, SCORE_TYPES[S.dtype], ld, S.data_ptr()
+
+
+def _list(v: Optional[torch.Tensor], n: int, width: int, name: str, dtype=torch.float32, optional=False):
+    """The address of n rows of `width` numbers without gaps, 1-D or 2-D; 0 for None."""
+    if v is None:
+        if optional:
+            return 0
+        raise TypeError(f"{name} is required")
+    if not isinstance(v, torch.Tensor) or v.dtype != dtype or not v.is_cuda or v.numel() != n * width or not v.is_contiguous():
+        raise TypeError(f"{name} must be a contiguous {dtype} CUDA tensor of {n} x {width} elements")
+    return v.data_ptr()
+
+
+def _width(v: Optional[torch.Tensor], n: int, name: str) -> int:
+    """Entries per row of an n-row list given as (n, width) or, for one a row, (n,)."""
+    if v is None:
+        return 0
+    if v.dim() not in (1, 2) or v.shape[0] != n:
+        raise TypeError(f"{name} must have {n} rows")
+    return 1 if v.dim() == 1 else v.shape[1]
+
+
+def _same_scores(dS: torch.Tensor, S: torch.Tensor, name="dS"):
+    """(leading dimension, address) of an output of S's shape and type."""
+    if not isinstance(dS, torch.Tensor) or dS.dtype != S.dtype or dS.shape != S.shape:
+        raise TypeError(f"{name} must have the shape and type of S")
+    return _scores(dS, name)[3:]
+
+
+def regot_row_logprob_workspace_bytes(n: int, m: int, k: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().regot_row_logprob_workspace_bytes(int(n), int(m), int(k), ctypes.byref(out)), "regot_row_logprob_workspace_bytes")
+    return int(out.value)
+
+
+def regot_row_distill_workspace_bytes(n: int, m: int, k: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().regot_row_distill_workspace_bytes(int(n), int(m), int(k), ctypes.byref(out)), "regot_row_distill_workspace_bytes")
+    return int(out.value)
+
+
+def regot_row_logprob(S, target, eta, logprob, entropy, stats, top_idx, top_logprob, *, bias=None, workspace, stream=None) -> None:
+    """target, logprob: (n, targets) or None; entropy (n), stats (n, 2): or None; top_idx, top_logprob: (n, k) or None."""
+    n, m, kind, ld, at = _scores(S)
+    targets, k = _width(target, n, "target"), _width(top_idx, n, "top_idx")
+    _check(load().regot_row_logprob(
+        n, m, at, kind, ld, _list(bias, 1, m, "bias", optional=True), float(eta),
+        _list(target, n, targets, "target", torch.int32, optional=True), targets, k,
+        _list(logprob, n, targets, "logprob", optional=targets == 0), _list(entropy, n, 1, "entropy", optional=True),
+        _list(stats, n, 2, "stats", optional=True), _list(top_idx, n, k, "top_idx", torch.int32, optional=True),
+        _list(top_logprob, n, k, "top_logprob", optional=k == 0), *_ws(workspace), _stream(stream)), "regot_row_logprob")
+
+
+def regot_row_logprob_grad(S, target, eta, stats, entropy, g_logprob, g_entropy, dS, *, bias=None, stream=None) -> None:
+    """g_logprob (n, targets) with target, or both None; g_entropy (n) with entropy, or both None."""
+    n, m, kind, ld, at = _scores(S)
+    targets = _width(target, n, "target")
+    ldD, to = _same_scores(dS, S)
+    _check(load().regot_row_logprob_grad(
+        n, m, at, kind, ld, _list(bias, 1, m, "bias", optional=True), float(eta),
+        _list(target, n, targets, "target", torch.int32, optional=True), targets, _list(stats, n, 2, "stats"),
+        _list(entropy, n, 1, "entropy", optional=g_entropy is None), _list(g_logprob, n, targets, "g_logprob", optional=targets == 0),
+        _list(g_entropy, n, 1, "g_entropy", optional=True), to, ldD, _stream(stream)), "regot_row_logprob_grad")
+
+
+def regot_row_distill(S, t_idx, t_score, eta, loss, dS=None, *, row_weight=None, workspace, stream=None) -> None:
+    """t_idx (int32), t_score: (n, k); dS None: the loss alone."""
+    n, m, kind, ld, at = _scores(S)
+    k = _width(t_idx, n, "t_idx")
+    ldD, to = (m, 0) if dS is None else _same_scores(dS, S)
+    _check(load().regot_row_distill(
+        n, m, at, kind, ld, float(eta), _list(t_idx, n, k, "t_idx", torch.int32), _list(t_score, n, k, "t_score"), k,
+        _list(row_weight, n, 1, "row_weight", optional=True), _list(loss, n, 1, "loss"), to, ldD, *_ws(workspace),
+        _stream(stream)), "regot_row_distill")
+
+
+def regot_row_route(S, idx, weight, *, bias=None, bias_on="score", score="softmax", groups=1, groups_kept=1, group_by="max",
+                    renormalise=True, scale=1.0, stream=None) -> None:
+    """idx (int32), weight: (n, k)."""
+    n, m, kind, ld, at = _scores(S)
+    k = _width(idx, n, "idx")
+    _check(load().regot_row_route(
+        n, m, at, kind, ld, _list(bias, 1, m, "bias", optional=True), BIAS_ON[bias_on], SCORE_KINDS[score], int(groups),
+        int(groups_kept), GROUP_BY[group_by], k, int(bool(renormalise)), float(scale), _list(idx, n, k, "idx", torch.int32),
+        _list(weight, n, k, "weight"), _stream(stream)), "regot_row_route")
+
+
+def regot_row_route_grad(S, idx, g_weight, dS, *, score="softmax", renormalise=True, scale=1.0, stream=None) -> None:
+    n, m, kind, ld, at = _scores(S)
+    k = _width(idx, n, "idx")
+    ldD, to = _same_scores(dS, S)
+    _check(load().regot_row_route_grad(
+        n, m, at, kind, ld, SCORE_KINDS[score], _list(idx, n, k, "idx", torch.int32), k, int(bool(renormalise)), float(scale),
+        _list(g_weight, n, k, "g_weight"), to, ldD, _stream(stream)), "regot_row_route_grad")
 
 
 def regot_profile_stage1(start_event, stop_event) -> None:

@@ -5,7 +5,8 @@ import sys
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
-SRCS = [os.path.join(HERE, "csrc", "regot.hip"), os.path.join(HERE, "csrc", "regot_pattern.hip")]
+SRCS = [os.path.join(HERE, "csrc", "regot.hip"), os.path.join(HERE, "csrc", "regot_pattern.hip"),
+        os.path.join(HERE, "csrc", "regot_rows.hip")]
 LIB = os.path.join(HERE, "libregot.so")
 
 HIPCC_FLAGS = [

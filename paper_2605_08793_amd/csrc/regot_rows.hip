@@ -1,0 +1,567 @@
+// Row operators: log probabilities, entropy and alternatives; distillation; routing; and their gradients.
+//
+// Every kernel here gives a workgroup (log probabilities, distillation) or a wave (routing) one row.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "regot.h"
+#include "regot_rows.hpp"
+
+namespace {
+
+using namespace regot;
+
+constexpr int64_t kMaxDim = 2147483647LL;
+constexpr size_t kAlign = 256;
+
+bool misaligned(const void *p, size_t a) { return ((uintptr_t)p % a) != 0; }
+int hip_status() { return hipGetLastError() == hipSuccess ? REGOT_OK : REGOT_ERR_HIP; }
+
+struct RowArgs {
+    int n, m;
+    const void *S;
+    int64_t ldS;
+    const float *bias;
+    float inv_eta, log2_scale;  // 1 / eta, log2(e) / eta
+    const int32_t *target;
+    int targets, k;
+    float *logprob, *entropy, *stats;
+    int32_t *top_idx;
+    float *top_logprob;
+    // gradient
+    const float *stats_in, *entropy_in, *g_logprob, *g_entropy;
+    void *dS;
+    int64_t ldD;
+    // distillation
+    const float *t_score, *row_weight;
+    float *loss;
+};
+
+template <int TYPE>
+struct Row {
+    const typename Score<TYPE>::Raw *S;
+    const float *bias;
+    __device__ __forceinline__ Row(const RowArgs &A, int64_t row)
+        : S(static_cast<const typename Score<TYPE>::Raw *>(A.S) + row * A.ldS), bias(A.bias) {}
+    __device__ __forceinline__ float operator()(int j) const
+    {
+        const float x = Score<TYPE>::get(S[j]);
+        return bias ? x + bias[j] : x;
+    }
+};
+
+// max, sum of exp and sum of exp times exponent of a row, from two passes over it; NaN in `sum` where the row has a NaN or +inf
+template <int TYPE>
+__device__ void row_stats(const RowArgs &A, const Row<TYPE> &x, float *lds, float &top, float &sum, float &weighted)
+{
+    float mx = -kInf;
+    bool nan = false;
+    for (int j = threadIdx.x; j < A.m; j += kThreads) {
+        const float v = x(j);
+        nan |= v != v;
+        mx = fmaxf(mx, v);
+    }
+    mx = block_all<OpMaxF, kWaves>(mx, lds);
+    nan = __syncthreads_or(nan);
+    float s = 0.f, e1 = 0.f;
+    for (int j = threadIdx.x; j < A.m && mx > -kInf; j += kThreads) {
+        const float t = (x(j) - mx) * A.log2_scale, e = exp2_fast(t);
+        s += e;
+        e1 += e > 0.f ? e * t : 0.f;
+    }
+    top = mx;
+    sum = block_all<OpSumF, kWaves>(s, lds);
+    weighted = block_all<OpSumF, kWaves>(e1, lds) * kLn2;
+    if (nan || sum != sum) top = sum = weighted = kNan;
+}
+
+template <int TYPE>
+__global__ __launch_bounds__(kThreads) void row_logprob_kernel(RowArgs A)
+{
+    __shared__ float lds[kWaves];
+    __shared__ float best_x[kWaves];
+    __shared__ int best_j[kWaves];
+    const int64_t row = blockIdx.x;
+    const Row<TYPE> x(A, row);
+    float mx, s, e1;
+    row_stats<TYPE>(A, x, lds, mx, s, e1);
+    const bool none = mx == -kInf, bad = s != s;
+    const float log_sum = none ? -kInf : logf(s);
+    if (threadIdx.x == 0) {
+        if (A.stats) {
+            A.stats[2 * row] = mx;
+            A.stats[2 * row + 1] = log_sum;
+        }
+        if (A.entropy) A.entropy[row] = none ? 0.f : log_sum - e1 / s;
+    }
+    for (int t = threadIdx.x; t < A.targets; t += kThreads) {
+        const int j = A.target[row * A.targets + t];
+        A.logprob[row * A.targets + t] = (uint32_t)j >= (uint32_t)A.m ? 0.f : none ? -kInf : (x(j) - mx) * A.inv_eta - log_sum;
+    }
+    float last_x = kInf;
+    int last_j = -1;
+    for (int i = 0; i < A.k; ++i) {
+        float bx = -kInf;
+        int bj = A.m;
+        for (int j = threadIdx.x; j < A.m && !bad; j += kThreads) {
+            const float v = x(j);
+            if (before(last_x, last_j, v, j) && before(v, j, bx, bj)) bx = v, bj = j;
+        }
+        for (int d = 1; d < kLanes; d *= 2) {
+            const float ox = __shfl_xor(bx, d);
+            const int oj = __shfl_xor(bj, d);
+            if (before(ox, oj, bx, bj)) bx = ox, bj = oj;
+        }
+        __syncthreads();
+        if ((threadIdx.x & (kLanes - 1)) == 0) best_x[threadIdx.x / kLanes] = bx, best_j[threadIdx.x / kLanes] = bj;
+        __syncthreads();
+        for (int w = 0; w < kWaves; ++w)
+            if (before(best_x[w], best_j[w], bx, bj)) bx = best_x[w], bj = best_j[w];
+        if (threadIdx.x == 0) {
+            const bool is = bx > -kInf && !bad;
+            A.top_idx[row * A.k + i] = is ? bj : -1;
+            A.top_logprob[row * A.k + i] = bad ? kNan : is ? (bx - mx) * A.inv_eta - log_sum : -kInf;
+        }
+        last_x = bx;
+        last_j = bj;
+    }
+}
+
+template <int TYPE>
+__global__ __launch_bounds__(kThreads) void row_logprob_grad_kernel(RowArgs A)
+{
+    using T = Score<TYPE>;
+    __shared__ float lds[kWaves];
+    const int64_t row = blockIdx.x;
+    const Row<TYPE> x(A, row);
+    const float mx = A.stats_in[2 * row], log_sum = A.stats_in[2 * row + 1];
+    const bool none = mx == -kInf;
+    const float h = A.g_entropy ? A.g_entropy[row] : 0.f, H = A.g_entropy ? A.entropy_in[row] : 0.f;
+    float g = 0.f;
+    for (int t = threadIdx.x; t < A.targets; t += kThreads)
+        if ((uint32_t)A.target[row * A.targets + t] < (uint32_t)A.m) g += A.g_logprob[row * A.targets + t];
+    g = block_all<OpSumF, kWaves>(g, lds);
+    const auto value = [&](int j) {
+        const float logp = (x(j) - mx) * A.inv_eta - log_sum, p = exp2_fast(logp * 1.44269504088896340736f);
+        return -p * g - (p > 0.f ? h * p * (logp + H) : p * 0.f);
+    };
+    typename T::Raw *out = static_cast<typename T::Raw *>(A.dS) + row * A.ldD;
+    for (int j = threadIdx.x; j < A.m; j += kThreads) out[j] = T::put(none ? 0.f : value(j) * A.inv_eta);
+    __threadfence_block();
+    __syncthreads();
+    for (int t = threadIdx.x; t < A.targets && !none; t += kThreads) {
+        const int j = A.target[row * A.targets + t];
+        if ((uint32_t)j >= (uint32_t)A.m) continue;
+        float mine = 0.f;
+        for (int u = 0; u < A.targets; ++u)
+            if (A.target[row * A.targets + u] == j) mine += A.g_logprob[row * A.targets + u];
+        out[j] = T::put((mine + value(j)) * A.inv_eta);
+    }
+}
+
+template <int TYPE>
+__global__ __launch_bounds__(kThreads) void row_distill_kernel(RowArgs A)
+{
+    using T = Score<TYPE>;
+    __shared__ float lds[kWaves];
+    const int64_t row = blockIdx.x;
+    const Row<TYPE> x(A, row);
+    const int32_t *list = A.target + row * A.k;
+    const float *score = A.t_score + row * A.k;
+    typename T::Raw *out = A.dS ? static_cast<typename T::Raw *>(A.dS) + row * A.ldD : nullptr;
+    float t_max = -kInf;
+    bool nan = false;
+    for (int l = threadIdx.x; l < A.k; l += kThreads)
+        if ((uint32_t)list[l] < (uint32_t)A.m) t_max = fmaxf(t_max, score[l]), nan |= score[l] != score[l];
+    t_max = block_all<OpMaxF, kWaves>(t_max, lds);
+    nan = __syncthreads_or(nan);
+    if (t_max == -kInf && !nan) {  // padding
+        if (threadIdx.x == 0) A.loss[row] = 0.f;
+        for (int j = threadIdx.x; j < A.m && out; j += kThreads) out[j] = T::put(0.f);
+        return;
+    }
+    if (nan) t_max = kNan;
+    float q_sum = 0.f;
+    for (int l = threadIdx.x; l < A.k; l += kThreads)
+        if ((uint32_t)list[l] < (uint32_t)A.m) q_sum += exp2_fast((score[l] - t_max) * A.log2_scale);
+    q_sum = block_all<OpSumF, kWaves>(q_sum, lds);
+    float mx, s, e1;
+    row_stats<TYPE>(A, x, lds, mx, s, e1);
+    const bool none = mx == -kInf;
+    const float log_sum = none ? -kInf : logf(s), log_q = logf(q_sum);
+    float loss = 0.f;
+    for (int l = threadIdx.x; l < A.k; l += kThreads) {
+        const int j = list[l];
+        if ((uint32_t)j >= (uint32_t)A.m) continue;
+        const float t = (score[l] - t_max) * A.inv_eta, q = exp2_fast((score[l] - t_max) * A.log2_scale) / q_sum;
+        // (q times the distance before it is divided by eta: a mask of the type's lowest value stays finite)
+        loss += q == 0.f ? 0.f : none ? kInf : q * (t - log_q + log_sum) + q * A.inv_eta * (mx - x(j));
+    }
+    loss = block_all<OpSumF, kWaves>(loss, lds);
+    if (threadIdx.x == 0) A.loss[row] = loss;
+    if (!out) return;
+    const float w = q_sum != q_sum ? kNan : (A.row_weight ? A.row_weight[row] : 1.f) * A.inv_eta;
+    const float inv = 1.f / s;
+    const auto p = [&](int j) { return exp2_fast((x(j) - mx) * A.log2_scale) * inv; };
+    for (int j = threadIdx.x; j < A.m; j += kThreads) out[j] = T::put(none ? 0.f : w * p(j));
+    __threadfence_block();
+    __syncthreads();
+    for (int l = threadIdx.x; l < A.k && !none; l += kThreads) {
+        const int j = list[l];
+        if ((uint32_t)j >= (uint32_t)A.m) continue;
+        float q = 0.f;
+        for (int u = 0; u < A.k; ++u)
+            if (list[u] == j) q += exp2_fast((score[u] - t_max) * A.log2_scale) / q_sum;
+        out[j] = T::put(w * (p(j) - q));
+    }
+}
+
+struct RouteArgs {
+    int n, m;
+    const void *S;
+    int64_t ldS;
+    const float *bias;
+    int bias_on, score, groups, groups_kept, group_by, k, renormalise;
+    float scale;
+    int32_t *idx;
+    float *weight;
+    const int32_t *idx_in;
+    const float *g_weight;
+    void *dS;
+    int64_t ldD;
+};
+
+constexpr int kMaxGroups = 64;
+
+__device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + expf(-x)); }
+
+// scores of a row's columns into s: softmax, or sigmoid; by one wave
+template <int TYPE>
+__device__ void row_scores(const RouteArgs &A, const typename Score<TYPE>::Raw *S, int lane, float *s)
+{
+    float mx = -kInf;
+    bool nan = false;
+    for (int j = lane; j < A.m; j += kLanes) {
+        const float x = Score<TYPE>::get(S[j]);
+        s[j] = x;
+        nan |= x != x;
+        mx = fmaxf(mx, x);
+    }
+    if (A.score == REGOT_SIGMOID) {
+        for (int j = lane; j < A.m; j += kLanes) s[j] = sigmoid(s[j]);
+        return;
+    }
+    mx = __any(nan) ? kNan : wave_all<OpMaxF>(mx);
+    float sum = 0.f;
+    for (int j = lane; j < A.m; j += kLanes) sum += s[j] = expf(s[j] - mx);
+    sum = wave_all<OpSumF>(sum);
+    for (int j = lane; j < A.m; j += kLanes) s[j] = mx == -kInf ? 0.f : s[j] / sum;
+}
+
+template <int TYPE>
+__global__ __launch_bounds__(kLanes) void row_route_kernel(RouteArgs A)
+{
+    __shared__ float s[REGOT_ROW_MAX_EXPERTS], key[REGOT_ROW_MAX_EXPERTS], value[kMaxGroups];
+    const int64_t row = blockIdx.x;
+    const int lane = threadIdx.x;
+    const typename Score<TYPE>::Raw *S = static_cast<const typename Score<TYPE>::Raw *>(A.S) + row * A.ldS;
+    row_scores<TYPE>(A, S, lane, s);
+    bool bad = false;
+    for (int j = lane; j < A.m; j += kLanes) {
+        const float x = Score<TYPE>::get(S[j]);
+        float c = A.bias ? (A.bias_on == REGOT_BIAS_SCORE ? s[j] : x) + A.bias[j] : x;
+        if (x == -kInf) c = -kInf;
+        bad |= c != c || s[j] != s[j];
+        key[j] = c;
+    }
+    bad = __any(bad);
+    __syncthreads();
+    const int size = A.groups > 0 ? A.m / A.groups : 0;
+    if (A.groups > 1) {
+        if (lane < A.groups) {
+            float a = -kInf, b = -kInf;
+            for (int j = lane * size; j < (lane + 1) * size; ++j) {
+                if (key[j] == -kInf) continue;
+                const float c = A.bias ? key[j] : s[j];
+                b = fmaxf(b, fminf(a, c));
+                a = fmaxf(a, c);
+            }
+            value[lane] = A.group_by == REGOT_GROUP_TOP2 && b > -kInf ? a + b : a;
+        }
+        __syncthreads();
+        if (lane < A.groups) {
+            int rank = 0;
+            for (int g = 0; g < A.groups; ++g) rank += before(value[g], g, value[lane], lane);
+            if (rank >= A.groups_kept)
+                for (int j = lane * size; j < (lane + 1) * size; ++j) key[j] = -kInf;
+        }
+        __syncthreads();
+    }
+    float sum = 0.f, mine = 0.f;
+    int chosen = -1;
+    for (int i = 0; i < A.k; ++i) {
+        float bx = -kInf;
+        int bj = A.m;
+        for (int j = lane; j < A.m; j += kLanes)
+            if (before(key[j], j, bx, bj)) bx = key[j], bj = j;
+        for (int d = 1; d < kLanes; d *= 2) {
+            const float ox = __shfl_xor(bx, d);
+            const int oj = __shfl_xor(bj, d);
+            if (before(ox, oj, bx, bj)) bx = ox, bj = oj;
+        }
+        const bool is = !bad && bx > -kInf;
+        const float c = is ? s[bj] : 0.f;
+        sum += c;
+        if (lane == i) mine = c, chosen = is ? bj : -1;
+        __syncthreads();
+        if (is && lane == 0) key[bj] = -kInf;
+        __syncthreads();
+    }
+    if (lane < A.k) {
+        const float w = !A.renormalise ? mine : sum > 0.f ? mine / sum : 0.f;
+        A.idx[row * A.k + lane] = chosen;
+        A.weight[row * A.k + lane] = bad ? kNan : w * A.scale;
+    }
+}
+
+template <int TYPE>
+__global__ __launch_bounds__(kLanes) void row_route_grad_kernel(RouteArgs A)
+{
+    using T = Score<TYPE>;
+    __shared__ float s[REGOT_ROW_MAX_EXPERTS], ds[REGOT_ROW_MAX_EXPERTS];
+    const int64_t row = blockIdx.x;
+    const int lane = threadIdx.x;
+    const typename T::Raw *S = static_cast<const typename T::Raw *>(A.S) + row * A.ldS;
+    row_scores<TYPE>(A, S, lane, s);
+    for (int j = lane; j < A.m; j += kLanes) ds[j] = 0.f;
+    __syncthreads();
+    const int c = lane < A.k ? A.idx_in[row * A.k + lane] : -1;
+    const bool is = (uint32_t)c < (uint32_t)A.m;
+    const float g = is ? A.g_weight[row * A.k + lane] * A.scale : 0.f, sc = is ? s[c] : 0.f;
+    float d = g;
+    if (A.renormalise) {
+        const float Z = wave_all<OpSumF>(sc), gs = wave_all<OpSumF>(is ? g * sc : 0.f);
+        d = is && Z > 0.f ? (g - gs / Z) / Z : 0.f;
+    }
+    for (int i = 0; i < A.k; ++i) {  // (one after the other: a column may be listed twice)
+        if (lane == i && is) ds[c] += d;
+        __syncthreads();
+    }
+    const float all = A.score == REGOT_SOFTMAX ? wave_all<OpSumF>(is ? d * sc : 0.f) : 0.f;
+    const bool any = __any(is);
+    typename T::Raw *out = static_cast<typename T::Raw *>(A.dS) + row * A.ldD;
+    for (int j = lane; j < A.m; j += kLanes) {
+        const float v = A.score == REGOT_SOFTMAX ? s[j] * (ds[j] - all) : ds[j] * s[j] * (1.f - s[j]);
+        out[j] = T::put(any ? v : 0.f);
+    }
+}
+
+int element_bytes(int type) { return type == REGOT_F32 ? 4 : 2; }
+
+int check_rows(int64_t n, int64_t m, const void *S, int type, int64_t ldS, double eta)
+{
+    if (n < 0 || m < 0 || n > kMaxDim || m > kMaxDim) return REGOT_ERR_DIM;
+    if (type != REGOT_F32 && type != REGOT_BF16 && type != REGOT_F16) return REGOT_ERR_ARG;
+    // (1 / eta has to be a 32-bit number other than 0)
+    if (!(eta > 0.0) || !isfinite(eta) || !isfinite((float)(1.4426950408889634 / eta)) || (float)(1.0 / eta) < 1e-37f) return REGOT_ERR_ETA;
+    if (n > 0 && m > 0 && !S) return REGOT_ERR_NULL;
+    if (ldS < m) return REGOT_ERR_LD;
+    if (misaligned(S, element_bytes(type))) return REGOT_ERR_ALIGN;
+    return REGOT_OK;
+}
+
+RowArgs row_args(int64_t n, int64_t m, const void *S, int64_t ldS, const float *bias, double eta)
+{
+    RowArgs A{};
+    A.n = (int)n;
+    A.m = (int)m;
+    A.S = S;
+    A.ldS = ldS;
+    A.bias = bias;
+    A.inv_eta = (float)(1.0 / eta);
+    A.log2_scale = (float)(1.4426950408889634 / eta);
+    return A;
+}
+
+#define REGOT_BY_TYPE(kernel, type, grid, threads, stream, args)                                              \
+    do {                                                                                                      \
+        if ((type) == REGOT_F32) hipLaunchKernelGGL((kernel<REGOT_F32>), grid, threads, 0, stream, args);     \
+        else if ((type) == REGOT_BF16) hipLaunchKernelGGL((kernel<REGOT_BF16>), grid, threads, 0, stream, args); \
+        else hipLaunchKernelGGL((kernel<REGOT_F16>), grid, threads, 0, stream, args);                         \
+    } while (0)
+
+}  // namespace
+
+extern "C" {
+
+int regot_row_logprob_workspace_bytes(int64_t n, int64_t m, int k, size_t *bytes)
+{
+    if (!bytes) return REGOT_ERR_NULL;
+    if (n < 0 || m < 0 || n > kMaxDim || m > kMaxDim) return REGOT_ERR_DIM;
+    if (k < 0 || k > REGOT_ROW_MAX_TOP) return REGOT_ERR_ARG;
+    *bytes = kAlign;
+    return REGOT_OK;
+}
+
+int regot_row_logprob(int64_t n, int64_t m, const void *S, int type, int64_t ldS, const float *bias, double eta,
+                      const int32_t *target, int targets, int k, float *logprob, float *entropy, float *stats,
+                      int32_t *top_idx, float *top_logprob, void *workspace, size_t workspace_bytes, regot_stream_t stream)
+{
+    int st = check_rows(n, m, S, type, ldS, eta);
+    if (st != REGOT_OK) return st;
+    if (targets < 0 || targets > REGOT_ROW_MAX_LIST || k < 0 || k > REGOT_ROW_MAX_TOP) return REGOT_ERR_ARG;
+    if (n > 0 && ((targets > 0 && (!target || !logprob)) || (k > 0 && (!top_idx || !top_logprob)))) return REGOT_ERR_NULL;
+    if (misaligned(bias, 4) || misaligned(target, 4) || misaligned(logprob, 4) || misaligned(entropy, 4) || misaligned(stats, 4) ||
+        misaligned(top_idx, 4) || misaligned(top_logprob, 4))
+        return REGOT_ERR_ALIGN;
+    size_t need = 0;
+    regot_row_logprob_workspace_bytes(n, m, k, &need);
+    if (!workspace) return REGOT_ERR_NULL;
+    if (misaligned(workspace, kAlign)) return REGOT_ERR_ALIGN;
+    if (workspace_bytes < need) return REGOT_ERR_WORKSPACE;
+    if (n == 0) return REGOT_OK;
+    RowArgs A = row_args(n, m, S, ldS, bias, eta);
+    A.target = target;
+    A.targets = targets;
+    A.k = k;
+    A.logprob = logprob;
+    A.entropy = entropy;
+    A.stats = stats;
+    A.top_idx = top_idx;
+    A.top_logprob = top_logprob;
+    REGOT_BY_TYPE(row_logprob_kernel, type, dim3((unsigned)n), dim3(kThreads), static_cast<hipStream_t>(stream), A);
+    return hip_status();
+}
+
+int regot_row_logprob_grad(int64_t n, int64_t m, const void *S, int type, int64_t ldS, const float *bias, double eta,
+                           const int32_t *target, int targets, const float *stats, const float *entropy,
+                           const float *g_logprob, const float *g_entropy, void *dS, int64_t ldD, regot_stream_t stream)
+{
+    int st = check_rows(n, m, S, type, ldS, eta);
+    if (st != REGOT_OK) return st;
+    if (targets < 0 || targets > REGOT_ROW_MAX_LIST) return REGOT_ERR_ARG;
+    if (n > 0 && (!stats || (targets > 0 && (!target || !g_logprob)) || (g_entropy && !entropy) || (m > 0 && !dS))) return REGOT_ERR_NULL;
+    if (ldD < m) return REGOT_ERR_LD;
+    if (misaligned(bias, 4) || misaligned(target, 4) || misaligned(stats, 4) || misaligned(entropy, 4) || misaligned(g_logprob, 4) ||
+        misaligned(g_entropy, 4) || misaligned(dS, element_bytes(type)))
+        return REGOT_ERR_ALIGN;
+    if (n == 0 || m == 0) return REGOT_OK;
+    RowArgs A = row_args(n, m, S, ldS, bias, eta);
+    A.target = target;
+    A.targets = targets;
+    A.stats_in = stats;
+    A.entropy_in = entropy;
+    A.g_logprob = g_logprob;
+    A.g_entropy = g_entropy;
+    A.dS = dS;
+    A.ldD = ldD;
+    REGOT_BY_TYPE(row_logprob_grad_kernel, type, dim3((unsigned)n), dim3(kThreads), static_cast<hipStream_t>(stream), A);
+    return hip_status();
+}
+
+int regot_row_distill_workspace_bytes(int64_t n, int64_t m, int k, size_t *bytes)
+{
+    if (!bytes) return REGOT_ERR_NULL;
+    if (n < 0 || m < 0 || n > kMaxDim || m > kMaxDim) return REGOT_ERR_DIM;
+    if (k < 1 || k > REGOT_ROW_MAX_LIST) return REGOT_ERR_ARG;
+    *bytes = kAlign;
+    return REGOT_OK;
+}
+
+int regot_row_distill(int64_t n, int64_t m, const void *S, int type, int64_t ldS, double eta, const int32_t *t_idx,
+                      const float *t_score, int k, const float *row_weight, float *loss, void *dS, int64_t ldD,
+                      void *workspace, size_t workspace_bytes, regot_stream_t stream)
+{
+    int st = check_rows(n, m, S, type, ldS, eta);
+    if (st != REGOT_OK) return st;
+    if (k < 1 || k > REGOT_ROW_MAX_LIST) return REGOT_ERR_ARG;
+    if (n > 0 && (!t_idx || !t_score || !loss)) return REGOT_ERR_NULL;
+    if (dS && ldD < m) return REGOT_ERR_LD;
+    if (misaligned(t_idx, 4) || misaligned(t_score, 4) || misaligned(row_weight, 4) || misaligned(loss, 4) ||
+        misaligned(dS, element_bytes(type)))
+        return REGOT_ERR_ALIGN;
+    size_t need = 0;
+    regot_row_distill_workspace_bytes(n, m, k, &need);
+    if (!workspace) return REGOT_ERR_NULL;
+    if (misaligned(workspace, kAlign)) return REGOT_ERR_ALIGN;
+    if (workspace_bytes < need) return REGOT_ERR_WORKSPACE;
+    if (n == 0) return REGOT_OK;
+    RowArgs A = row_args(n, m, S, ldS, nullptr, eta);
+    A.target = t_idx;
+    A.t_score = t_score;
+    A.k = k;
+    A.row_weight = row_weight;
+    A.loss = loss;
+    A.dS = dS;
+    A.ldD = ldD;
+    REGOT_BY_TYPE(row_distill_kernel, type, dim3((unsigned)n), dim3(kThreads), static_cast<hipStream_t>(stream), A);
+    return hip_status();
+}
+
+int regot_row_route(int64_t n, int64_t m, const void *S, int type, int64_t ldS, const float *bias, int bias_on, int score,
+                    int groups, int groups_kept, int group_by, int k, int renormalise, double scale, int32_t *idx,
+                    float *weight, regot_stream_t stream)
+{
+    int st = check_rows(n, m, S, type, ldS, 1.0);
+    if (st != REGOT_OK) return st;
+    if (m > REGOT_ROW_MAX_EXPERTS) return REGOT_ERR_DIM;
+    if (k < 1 || k > REGOT_ROW_MAX_CHOICES || (score != REGOT_SOFTMAX && score != REGOT_SIGMOID) ||
+        (bias && bias_on != REGOT_BIAS_SCORE && bias_on != REGOT_BIAS_LOGIT) || groups < 1 || groups > kMaxGroups ||
+        groups_kept < 1 || groups_kept > groups || m % groups != 0 || (group_by != REGOT_GROUP_MAX && group_by != REGOT_GROUP_TOP2) ||
+        (renormalise != 0 && renormalise != 1) || !isfinite((float)scale))
+        return REGOT_ERR_ARG;
+    if (n > 0 && (!idx || !weight)) return REGOT_ERR_NULL;
+    if (misaligned(bias, 4) || misaligned(idx, 4) || misaligned(weight, 4)) return REGOT_ERR_ALIGN;
+    if (n == 0) return REGOT_OK;
+    RouteArgs A{};
+    A.n = (int)n;
+    A.m = (int)m;
+    A.S = S;
+    A.ldS = ldS;
+    A.bias = bias;
+    A.bias_on = bias_on;
+    A.score = score;
+    A.groups = groups;
+    A.groups_kept = groups_kept;
+    A.group_by = group_by;
+    A.k = k;
+    A.renormalise = renormalise;
+    A.scale = (float)scale;
+    A.idx = idx;
+    A.weight = weight;
+    REGOT_BY_TYPE(row_route_kernel, type, dim3((unsigned)n), dim3(kLanes), static_cast<hipStream_t>(stream), A);
+    return hip_status();
+}
+
+int regot_row_route_grad(int64_t n, int64_t m, const void *S, int type, int64_t ldS, int score, const int32_t *idx, int k,
+                         int renormalise, double scale, const float *g_weight, void *dS, int64_t ldD, regot_stream_t stream)
+{
+    int st = check_rows(n, m, S, type, ldS, 1.0);
+    if (st != REGOT_OK) return st;
+    if (m > REGOT_ROW_MAX_EXPERTS) return REGOT_ERR_DIM;
+    if (k < 1 || k > REGOT_ROW_MAX_CHOICES || (score != REGOT_SOFTMAX && score != REGOT_SIGMOID) ||
+        (renormalise != 0 && renormalise != 1) || !isfinite((float)scale))
+        return REGOT_ERR_ARG;
+    if (n > 0 && (!idx || !g_weight || (m > 0 && !dS))) return REGOT_ERR_NULL;
+    if (ldD < m) return REGOT_ERR_LD;
+    if (misaligned(idx, 4) || misaligned(g_weight, 4) || misaligned(dS, element_bytes(type))) return REGOT_ERR_ALIGN;
+    if (n == 0 || m == 0) return REGOT_OK;
+    RouteArgs A{};
+    A.n = (int)n;
+    A.m = (int)m;
+    A.S = S;
+    A.ldS = ldS;
+    A.score = score;
+    A.k = k;
+    A.renormalise = renormalise;
+    A.scale = (float)scale;
+    A.idx_in = idx;
+    A.g_weight = g_weight;
+    A.dS = dS;
+    A.ldD = ldD;
+    REGOT_BY_TYPE(row_route_grad_kernel, type, dim3((unsigned)n), dim3(kLanes), static_cast<hipStream_t>(stream), A);
+    return hip_status();
+}
+
+}  // extern "C"

@@ -1,0 +1,160 @@
+"""The distillation loss and its gradient against plain 64-bit ones; bounds in rows_reference."""
+import numpy as np
+import pytest
+import torch
+
+import rows_reference as ref
+from paper_2605_08793_amd import binding as B
+from paper_2605_08793_amd.rows import RowDistill
+from rows_reference import TYPE_IDS, TYPES, close
+from test_gpu_rows_logprob import KINDS, laid_out, masked, scores
+
+pytestmark = pytest.mark.gpu
+
+
+def teacher(n, m, k, seed):
+    """Distinct columns in no order; some entries missing, row 1 without any."""
+    rng = np.random.default_rng(seed)
+    idx = np.stack([rng.permutation(m)[:k] if m >= k else np.concatenate([rng.permutation(m), np.full(k - m, -1)]) for _ in range(n)])
+    idx[rng.random((n, k)) < 0.1] = -1
+    if n > 1:
+        idx[1] = -1
+    score = rng.standard_normal((n, k)) * 2.0
+    return torch.from_numpy(idx.astype(np.int32)).cuda(), torch.from_numpy(score.astype(np.float32)).cuda()
+
+
+def run(S, t_idx, t_score, eta, w, extra=0, offset=0):
+    n, m = S.shape
+    ws = torch.empty(max(B.regot_row_distill_workspace_bytes(n, m, t_idx.shape[1]), 256), dtype=torch.uint8, device="cuda")
+    loss = torch.full((n,), 12345.0, device="cuda")
+    flat = torch.full((offset + n * (m + extra) + 64,), 7.0, dtype=S.dtype, device="cuda")
+    dS = flat[offset:offset + n * (m + extra)].view(n, m + extra)[:, :m]
+    B.regot_row_distill(S, t_idx, t_score, eta, loss, dS, row_weight=w, workspace=ws)
+    torch.cuda.synchronize()
+    out = dS.cpu()
+    dS.fill_(7.0)
+    assert bool((flat == 7.0).all()), "written outside the rows"
+    alone = torch.full((n,), 12345.0, device="cuda")
+    B.regot_row_distill(S, t_idx, t_score, eta, alone, None, row_weight=w, workspace=ws)
+    torch.cuda.synchronize()
+    return loss, out, alone
+
+
+def compare(S_host, got, t_idx, t_score, eta, w, dtype, what):
+    loss, tol_loss, d, tol = ref.distill(S_host, t_idx, t_score, eta, w)
+    close(got[0], loss, tol_loss, what + " loss")
+    close(got[1], d, ref.rounded(d, tol, dtype), what + " gradient")
+    close(got[2], loss, tol_loss, what + " loss alone")
+
+
+@pytest.mark.parametrize("n,m,k", [(1, 1, 1), (3, 2, 4), (5, 63, 9), (65, 128, 16), (40, 1000, 50), (600, 301, 5), (9, 4097, 100),
+                                   (200, 3001, 32), (4, 33333, 64), (3, 70001, 300), (2, 131072, 64), (1, 200003, 1024)])
+@pytest.mark.parametrize("dtype", TYPES, ids=TYPE_IDS)
+def test_sizes(n, m, k, dtype):
+    S = scores(n, m, dtype, n + m)
+    t_idx, t_score = teacher(n, m, k, m)
+    w = (torch.rand(n, generator=torch.Generator().manual_seed(1)) + 0.1).cuda()
+    for eta, weight in ((0.7, w), (2.0, None)):
+        compare(S, run(S.cuda(), t_idx, t_score, eta, weight), t_idx, t_score, eta, weight, dtype, f"{n}x{m} k={k}")
+
+
+@pytest.mark.parametrize("offset,extra", [(1, 0), (3, 1), (8, 8), (5, 13)])
+@pytest.mark.parametrize("dtype", TYPES, ids=TYPE_IDS)
+def test_rows_that_start_anywhere(offset, extra, dtype):
+    for n, m in ((4, 5003), (33, 301), (3, 40001)):
+        S = scores(n, m, dtype, offset + m)
+        flat, view = laid_out(S, m + extra, offset)
+        t_idx, t_score = teacher(n, m, 20, m)
+        compare(S, run(view, t_idx, t_score, 1.0, None, extra=(offset * 3) % 5, offset=extra), t_idx, t_score, 1.0, None, dtype,
+                f"{n}x{m} at {offset}+{extra}")
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dtype", TYPES, ids=TYPE_IDS)
+@pytest.mark.parametrize("n,m", [(6, 777), (5, 20011), (5, 66000)])
+def test_masks_and_values(kind, dtype, n, m):
+    S = masked(kind, dtype, n, m)
+    t_idx, t_score = teacher(n, m, 24, 3)
+    compare(S, run(S.cuda(), t_idx, t_score, 0.5, None), t_idx, t_score, 0.5, None, dtype, f"{kind} {n}x{m}")
+
+
+def test_teachers_that_give_nothing_or_too_much():
+    n, m, k = 6, 3000, 8
+    S = scores(n, m, torch.float32, 9)
+    t_idx, t_score = teacher(n, m, k, 4)
+    t_idx[0] = torch.arange(k, dtype=torch.int32)
+    t_score[0, 3:] = -np.inf     # entries without weight
+    t_score[2] = -np.inf         # a list without weight is padding
+    S[3, :] = np.nan             # padding is not looked at, whatever the scores are
+    t_idx[3] = -1
+    t_idx[4, 0], t_score[4, 0] = 5, np.nan
+    t_idx[5, 0], t_score[5, 0] = 5, np.inf
+    compare(S, run(S.cuda(), t_idx, t_score, 1.0, None), t_idx, t_score, 1.0, None, torch.float32, "teachers")
+
+
+def test_a_column_listed_twice_counts_twice():
+    n, m = 3, 2000
+    S = scores(n, m, torch.float32, 10)
+    t_idx = torch.tensor([[5, 5, 9], [1999, 0, 1999], [7, 7, 7]], dtype=torch.int32).cuda()
+    t_score = torch.randn(3, 3, generator=torch.Generator().manual_seed(0)).cuda()
+    compare(S, run(S.cuda(), t_idx, t_score, 1.0, None), t_idx, t_score, 1.0, None, torch.float32, "twice")
+
+
+def test_equal_distributions_have_no_loss():
+    """A teacher that lists every column with the student's own scores: the loss is rounding, the gradient too."""
+    S = scores(4, 500, torch.float32, 2)
+    t_idx = torch.arange(500, dtype=torch.int32).repeat(4, 1).cuda()
+    compare(S, run(S.cuda(), t_idx, S.cuda().contiguous(), 1.0, None), t_idx, S, 1.0, None, torch.float32, "equal")
+
+
+def test_offsets_beyond_32_bits():
+    n, m, ld = 3, 1031, 2_200_000_000
+    flat = torch.empty((n - 1) * ld + m, dtype=torch.bfloat16, device="cuda")
+    out = torch.empty((n - 1) * ld + m, dtype=torch.bfloat16, device="cuda")
+    view, dS = flat.as_strided((n, m), (ld, 1)), out.as_strided((n, m), (ld, 1))
+    S = scores(n, m, torch.bfloat16, 8)
+    view.copy_(S)
+    t_idx, t_score = teacher(n, m, 20, 1)
+    ws = torch.empty(max(B.regot_row_distill_workspace_bytes(n, m, 20), 256), dtype=torch.uint8, device="cuda")
+    loss = torch.empty(n, device="cuda")
+    B.regot_row_distill(view, t_idx, t_score, 1.0, loss, dS, workspace=ws)
+    compare(S, (loss, dS, loss), t_idx, t_score, 1.0, None, torch.bfloat16, "far rows")
+
+
+def test_gradient_against_differences():
+    n, m, eta = 4, 900, 1.3
+    S = scores(n, m, torch.float32, 13)
+    t_idx, t_score = teacher(n, m, 12, 5)
+    w = torch.rand(n, generator=torch.Generator().manual_seed(3)).cuda() + 0.5
+    out = run(S.cuda(), t_idx, t_score, eta, w)[1].double()
+
+    def value(x):
+        lp = torch.log_softmax(x / eta, 1)
+        total = 0.0
+        for i in range(n):
+            at = [l for l in range(12) if t_idx[i, l] >= 0]
+            if at:
+                q = torch.softmax(t_score[i, at].cpu().double() / eta, 0)
+                total += float(w[i]) * float((q * (q.log() - lp[i, t_idx[i, at].cpu().long()])).sum())
+        return total
+
+    _, _, _, tol = ref.distill(S, t_idx, t_score, eta, w)
+    rng = torch.Generator().manual_seed(5)
+    for _ in range(5):
+        v = torch.randn(n, m, generator=rng, dtype=torch.float64)
+        step = 1e-4  # (error step^2 / 6 times a third derivative, and 1e-16 / step of rounding)
+        slope = (value(S.double() + step * v) - value(S.double() - step * v)) / (2 * step)
+        bound = float((ref.rounded(out, tol, torch.float32) * v.abs()).sum()) + 1e-5
+        assert abs(float((out * v).sum()) - slope) <= bound
+
+
+def test_same_bits_every_time():
+    for n, m in ((2, 131072), (70, 20000), (3000, 300)):
+        S = scores(n, m, torch.bfloat16, 2).cuda()
+        t_idx, t_score = teacher(n, m, 20, 1)
+        op = RowDistill(n, m, 20)
+        op.distill(S, t_idx, t_score)
+        loss, grad = op.loss.clone(), op.grad.clone()
+        for _ in range(3):
+            op.distill(S, t_idx, t_score)
+            assert torch.equal(loss, op.loss) and torch.equal(grad, op.grad)
