@@ -5,8 +5,10 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "regot.h"
-#include "regot_rows.hpp"
+#include "regot_rows_logprob.hpp"
 
 namespace {
 
@@ -17,26 +19,6 @@ constexpr size_t kAlign = 256;
 
 bool misaligned(const void *p, size_t a) { return ((uintptr_t)p % a) != 0; }
 int hip_status() { return hipGetLastError() == hipSuccess ? REGOT_OK : REGOT_ERR_HIP; }
-
-struct RowArgs {
-    int n, m;
-    const void *S;
-    int64_t ldS;
-    const float *bias;
-    float inv_eta, log2_scale;  // 1 / eta, log2(e) / eta
-    const int32_t *target;
-    int targets, k;
-    float *logprob, *entropy, *stats;
-    int32_t *top_idx;
-    float *top_logprob;
-    // gradient
-    const float *stats_in, *entropy_in, *g_logprob, *g_entropy;
-    void *dS;
-    int64_t ldD;
-    // distillation
-    const float *t_score, *row_weight;
-    float *loss;
-};
 
 template <int TYPE>
 struct Row {
@@ -74,58 +56,6 @@ __device__ void row_stats(const RowArgs &A, const Row<TYPE> &x, float *lds, floa
     sum = block_all<OpSumF, kWaves>(s, lds);
     weighted = block_all<OpSumF, kWaves>(e1, lds) * kLn2;
     if (nan || sum != sum) top = sum = weighted = kNan;
-}
-
-template <int TYPE>
-__global__ __launch_bounds__(kThreads) void row_logprob_kernel(RowArgs A)
-{
-    __shared__ float lds[kWaves];
-    __shared__ float best_x[kWaves];
-    __shared__ int best_j[kWaves];
-    const int64_t row = blockIdx.x;
-    const Row<TYPE> x(A, row);
-    float mx, s, e1;
-    row_stats<TYPE>(A, x, lds, mx, s, e1);
-    const bool none = mx == -kInf, bad = s != s;
-    const float log_sum = none ? -kInf : logf(s);
-    if (threadIdx.x == 0) {
-        if (A.stats) {
-            A.stats[2 * row] = mx;
-            A.stats[2 * row + 1] = log_sum;
-        }
-        if (A.entropy) A.entropy[row] = none ? 0.f : log_sum - e1 / s;
-    }
-    for (int t = threadIdx.x; t < A.targets; t += kThreads) {
-        const int j = A.target[row * A.targets + t];
-        A.logprob[row * A.targets + t] = (uint32_t)j >= (uint32_t)A.m ? 0.f : none ? -kInf : (x(j) - mx) * A.inv_eta - log_sum;
-    }
-    float last_x = kInf;
-    int last_j = -1;
-    for (int i = 0; i < A.k; ++i) {
-        float bx = -kInf;
-        int bj = A.m;
-        for (int j = threadIdx.x; j < A.m && !bad; j += kThreads) {
-            const float v = x(j);
-            if (before(last_x, last_j, v, j) && before(v, j, bx, bj)) bx = v, bj = j;
-        }
-        for (int d = 1; d < kLanes; d *= 2) {
-            const float ox = __shfl_xor(bx, d);
-            const int oj = __shfl_xor(bj, d);
-            if (before(ox, oj, bx, bj)) bx = ox, bj = oj;
-        }
-        __syncthreads();
-        if ((threadIdx.x & (kLanes - 1)) == 0) best_x[threadIdx.x / kLanes] = bx, best_j[threadIdx.x / kLanes] = bj;
-        __syncthreads();
-        for (int w = 0; w < kWaves; ++w)
-            if (before(best_x[w], best_j[w], bx, bj)) bx = best_x[w], bj = best_j[w];
-        if (threadIdx.x == 0) {
-            const bool is = bx > -kInf && !bad;
-            A.top_idx[row * A.k + i] = is ? bj : -1;
-            A.top_logprob[row * A.k + i] = bad ? kNan : is ? (bx - mx) * A.inv_eta - log_sum : -kInf;
-        }
-        last_x = bx;
-        last_j = bj;
-    }
 }
 
 template <int TYPE>
@@ -374,8 +304,8 @@ int check_rows(int64_t n, int64_t m, const void *S, int type, int64_t ldS, doubl
 RowArgs row_args(int64_t n, int64_t m, const void *S, int64_t ldS, const float *bias, double eta)
 {
     RowArgs A{};
-    A.n = (int)n;
-    A.m = (int)m;
+    A.n = n;
+    A.m = (uint32_t)m;
     A.S = S;
     A.ldS = ldS;
     A.bias = bias;
@@ -391,6 +321,86 @@ RowArgs row_args(int64_t n, int64_t m, const void *S, int64_t ldS, const float *
         else hipLaunchKernelGGL((kernel<REGOT_F16>), grid, threads, 0, stream, args);                         \
     } while (0)
 
+constexpr int64_t kMaxGrid = 1 << 22;  // (rows beyond are the same workgroups')
+
+// How the rows of a call are shared out: a few long rows are several workgroups' each, whose findings a second launch joins.  (One
+// workgroup takes 5.5 us and 0.45 for each slice of 4096 columns, the two launches 10.5 us and the reading.  us, one workgroup a row / parts, bf16, 20
+// alternatives: 1 x 131072 19.7 / 10.6, 8 x 131072 20.3 / 11.2, 64 x 50000 11.8 / 10.8, 128 x 32768 10.5 / 11.7, 256 x 131072 25.9 / 26.8.)
+constexpr int kFewRows = 192, kLongRow = 13, kPlaces = 512, kLeastParts = 8;
+
+struct RowPlan {
+    int block = 1, blocks = 1, parts = 1, part_blocks = 1;
+    size_t max = 0, total = 0;                     // workspace
+};
+
+int64_t power_of_two(int64_t least)
+{
+    int64_t p = 1;
+    while (p < least) p *= 2;
+    return p;
+}
+
+RowPlan plan_rows(int64_t n, int64_t m, int k)
+{
+    RowPlan P;
+    const int64_t slices = std::max<int64_t>((m + kSlice - 1) / kSlice, 1);
+    int64_t parts = 1;
+    if (n <= kFewRows && slices >= kLongRow) parts = std::min<int64_t>({slices, kPartBlocks, std::max<int64_t>(kPlaces / n, kLeastParts)});
+    if (parts > 1) {
+        const int64_t of_part = (slices + parts - 1) / parts;  // slices of a part
+        const int64_t most = std::max<int64_t>(kPartBlocks / parts, 1);   // blocks of a part
+        P.block = (int)power_of_two((of_part + most - 1) / most);
+        P.part_blocks = (int)((of_part + P.block - 1) / P.block);
+        P.blocks = (int)((slices + P.block - 1) / P.block);
+        P.parts = (P.blocks + P.part_blocks - 1) / P.part_blocks;
+    }
+    if (P.parts > 1) {
+        P.max = ((size_t)n * P.parts * 3 * sizeof(float) + kAlign - 1) / kAlign * kAlign;
+        P.total = P.max + (k > 0 ? (size_t)n * P.blocks * kThreads * sizeof(float) : 0);
+    } else {
+        P.block = (int)power_of_two((slices + kWholeBlocks - 1) / kWholeBlocks);
+        P.blocks = P.part_blocks = (int)((slices + P.block - 1) / P.block);
+    }
+    P.total = std::max((P.total + kAlign - 1) / kAlign * kAlign, kAlign);
+    return P;
+}
+
+template <int TYPE, bool BIAS, bool TOP>
+void launch_logprob(const RowArgs &A, const RowPlan &P, hipStream_t s)
+{
+    constexpr int kVecs = BIAS || TYPE == REGOT_F32 ? 4 : 8;  // 16-byte loads in flight: two slices, one of fp32 (1500 x 10007 fp32, 32 alternatives: 8 loads 23.8 us, 4 18.6) or with a bias
+    constexpr uint32_t kLoad = kLanes * Score<TYPE>::kVec;  // columns of a wave's load
+    const dim3 threads(kThreads);
+    const auto grid = [](int64_t blocks) { return dim3((unsigned)std::min(blocks, kMaxGrid)); };
+    const dim3 by_wave = grid((A.n + kWaves - 1) / kWaves);
+    if (A.m <= kLoad) {
+        hipLaunchKernelGGL((row_logprob_narrow_kernel<TYPE, BIAS, TOP, 1>), by_wave, threads, 0, s, A);
+    } else if (A.m <= 2 * kLoad) {
+        hipLaunchKernelGGL((row_logprob_narrow_kernel<TYPE, BIAS, TOP, 2>), by_wave, threads, 0, s, A);
+    } else if (A.m <= 8 * kLoad && P.parts == 1) {
+        hipLaunchKernelGGL((row_logprob_narrow_kernel<TYPE, BIAS, TOP, 8>), by_wave, threads, 0, s, A);
+    } else if (P.parts > 1) {
+        hipLaunchKernelGGL((row_logprob_kernel<TYPE, BIAS, TOP, kVecs, true>), grid(A.n * P.parts), threads, 0, s, A);
+        hipLaunchKernelGGL((row_logprob_join_kernel<TYPE, BIAS, TOP>), grid(A.n), threads, 0, s, A);
+    } else {
+        hipLaunchKernelGGL((row_logprob_kernel<TYPE, BIAS, TOP, kVecs, false>), grid(A.n), threads, 0, s, A);
+    }
+}
+
+template <int TYPE>
+void launch_logprob(const RowArgs &A, const RowPlan &P, hipStream_t s)
+{
+    if (A.bias) A.k > 0 ? launch_logprob<TYPE, true, true>(A, P, s) : launch_logprob<TYPE, true, false>(A, P, s);
+    else A.k > 0 ? launch_logprob<TYPE, false, true>(A, P, s) : launch_logprob<TYPE, false, false>(A, P, s);
+}
+
+void launch_logprob(const RowArgs &A, int type, const RowPlan &P, hipStream_t s)
+{
+    if (type == REGOT_F32) launch_logprob<REGOT_F32>(A, P, s);
+    else if (type == REGOT_BF16) launch_logprob<REGOT_BF16>(A, P, s);
+    else launch_logprob<REGOT_F16>(A, P, s);
+}
+
 }  // namespace
 
 extern "C" {
@@ -400,7 +410,7 @@ int regot_row_logprob_workspace_bytes(int64_t n, int64_t m, int k, size_t *bytes
     if (!bytes) return REGOT_ERR_NULL;
     if (n < 0 || m < 0 || n > kMaxDim || m > kMaxDim) return REGOT_ERR_DIM;
     if (k < 0 || k > REGOT_ROW_MAX_TOP) return REGOT_ERR_ARG;
-    *bytes = kAlign;
+    *bytes = plan_rows(n, m, k).total;
     return REGOT_OK;
 }
 
@@ -415,11 +425,10 @@ int regot_row_logprob(int64_t n, int64_t m, const void *S, int type, int64_t ldS
     if (misaligned(bias, 4) || misaligned(target, 4) || misaligned(logprob, 4) || misaligned(entropy, 4) || misaligned(stats, 4) ||
         misaligned(top_idx, 4) || misaligned(top_logprob, 4))
         return REGOT_ERR_ALIGN;
-    size_t need = 0;
-    regot_row_logprob_workspace_bytes(n, m, k, &need);
+    const RowPlan P = plan_rows(n, m, k);
     if (!workspace) return REGOT_ERR_NULL;
     if (misaligned(workspace, kAlign)) return REGOT_ERR_ALIGN;
-    if (workspace_bytes < need) return REGOT_ERR_WORKSPACE;
+    if (workspace_bytes < P.total) return REGOT_ERR_WORKSPACE;
     if (n == 0) return REGOT_OK;
     RowArgs A = row_args(n, m, S, ldS, bias, eta);
     A.target = target;
@@ -430,7 +439,15 @@ int regot_row_logprob(int64_t n, int64_t m, const void *S, int type, int64_t ldS
     A.stats = stats;
     A.top_idx = top_idx;
     A.top_logprob = top_logprob;
-    REGOT_BY_TYPE(row_logprob_kernel, type, dim3((unsigned)n), dim3(kThreads), static_cast<hipStream_t>(stream), A);
+    A.block = P.block;
+    A.block_log2 = cbits(P.block);
+    A.blocks = P.blocks;
+    A.scan_log2 = cbits(power_of_two(P.blocks));
+    A.parts = P.parts;
+    A.part_blocks = P.part_blocks;
+    A.part_sums = static_cast<float *>(workspace);
+    A.part_max = reinterpret_cast<float *>(static_cast<char *>(workspace) + P.max);
+    launch_logprob(A, type, P, static_cast<hipStream_t>(stream));
     return hip_status();
 }
 

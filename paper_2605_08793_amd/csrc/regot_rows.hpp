@@ -12,6 +12,19 @@ namespace regot {
 constexpr float kInf = __builtin_inff();
 constexpr float kNan = __builtin_nanf("");
 constexpr float kLn2 = 0.693147180559945309417f;
+constexpr float kLog2e = 1.44269504088896340736f;
+
+__host__ __device__ constexpr int cbits(int64_t v) { return v > 1 ? 1 + cbits(v / 2) : 0; }  // log2 of a power of two
+
+// orders a wave's accesses to LDS that its lanes share
+__device__ __forceinline__ void wave_lds()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef u32x4 Any __attribute__((aligned(2)));  // 16 bytes at any multiple of 2
 
 // A score as a 32-bit number, and back (rounded to nearest even, once).
 template <int TYPE>
@@ -19,38 +32,126 @@ struct Score;
 template <>
 struct Score<REGOT_F32> {
     using Raw = float;
+    static constexpr int kVec = 4;
+    static constexpr uint32_t kMinusInf = 0xff800000u;
     static __device__ __forceinline__ float get(Raw v) { return v; }
     static __device__ __forceinline__ Raw put(float v) { return v; }
+    static __device__ __forceinline__ void unpack(u32x4 v, float *x)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(v[i]);
+    }
 };
 template <>
 struct Score<REGOT_BF16> {
     using Raw = __bf16;
+    static constexpr int kVec = 8;
+    static constexpr uint32_t kMinusInf = 0xff80ff80u;
     static __device__ __forceinline__ float get(Raw v) { return (float)v; }
     static __device__ __forceinline__ Raw put(float v) { return (__bf16)v; }
+    static __device__ __forceinline__ void unpack(u32x4 v, float *x)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = __uint_as_float(v[i] << 16);
+            x[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+        }
+    }
 };
 template <>
 struct Score<REGOT_F16> {
     using Raw = _Float16;
+    static constexpr int kVec = 8;
+    static constexpr uint32_t kMinusInf = 0xfc00fc00u;
     static __device__ __forceinline__ float get(Raw v) { return (float)v; }
     static __device__ __forceinline__ Raw put(float v) { return (_Float16)v; }
+    static __device__ __forceinline__ void unpack(u32x4 v, float *x)
+    {
+        _Float16 h[8];
+        __builtin_memcpy(h, &v, 16);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = (float)h[i];
+    }
+};
+
+// The 16 bytes of a row's columns that a lane takes at column j.  Where they would reach beyond the row they are moved back
+// to end with it, so that every load is whole and unconditional; the columns before j, which another lane has, are then
+// forbidden ones here.  (Rows start at any multiple of their element: the load is one instruction whatever the address.)
+template <int TYPE>
+struct Span {
+    using T = Score<TYPE>;
+    uint32_t first, own;  // the columns first .. first + kVec - 1, of which those from `own` on count
+    __device__ __forceinline__ Span(uint32_t j, uint32_t m) : first(m >= T::kVec ? min(j, m - T::kVec) : 0), own(j) {}
+    // ONCE: nothing reads the row again soon
+    template <bool ONCE>
+    __device__ __forceinline__ u32x4 load(const typename T::Raw *S, uint32_t m) const
+    {
+        u32x4 v;
+        if (m >= T::kVec) {
+            if constexpr (ONCE) v = __builtin_nontemporal_load(reinterpret_cast<const Any *>(S + first));
+            else v = *reinterpret_cast<const Any *>(S + first);
+            return v;
+        }
+        v = u32x4{T::kMinusInf, T::kMinusInf, T::kMinusInf, T::kMinusInf};  // a row shorter than one load
+        typename T::Raw part[T::kVec];
+        __builtin_memcpy(part, &v, 16);
+#pragma unroll
+        for (int e = 0; e < T::kVec; ++e)
+            if ((uint32_t)e < m) part[e] = S[e];
+        __builtin_memcpy(&v, part, 16);
+        return v;
+    }
+    // x[e] to -inf where column first + e does not count
+    __device__ __forceinline__ void mask(float *x) const
+    {
+        if (first != own) {
+#pragma unroll
+            for (int e = 0; e < T::kVec; ++e) x[e] = first + e >= own ? x[e] : -kInf;
+        }
+    }
+    __device__ __forceinline__ void add_bias(float *x, const float *bias, uint32_t m) const
+    {
+        float b[T::kVec];
+        if (m >= T::kVec) {
+            __builtin_memcpy(b, bias + first, sizeof(b));
+        } else {
+#pragma unroll
+            for (int e = 0; e < T::kVec; ++e) b[e] = (uint32_t)e < m ? bias[e] : 0.f;
+        }
+#pragma unroll
+        for (int e = 0; e < T::kVec; ++e) x[e] += b[e];
+    }
 };
 
 // 2^t by the hardware's exponential (within 1 unit in the last place; results below the smallest normal number are 0)
 __device__ __forceinline__ float exp2_fast(float t) { return __builtin_amdgcn_exp2f(t); }
 
+// the larger one, NaN if either is
+__device__ __forceinline__ float max_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
 struct OpSumF {
     static __device__ __forceinline__ float apply(float a, float b) { return a + b; }
 };
 struct OpMaxF {
-    static __device__ __forceinline__ float apply(float a, float b) { return fmaxf(a, b); }
+    static __device__ __forceinline__ float apply(float a, float b) { return max_nan(a, b); }
 };
 
+template <int CTRL>
+__device__ __forceinline__ float dpp_f32(float v)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+
+// over the wave, in a fixed order; the result in every lane
 template <typename Op>
 __device__ __forceinline__ float wave_all(float v)
 {
-#pragma unroll
-    for (int d = 1; d < kLanes; d *= 2) v = Op::apply(v, __shfl_xor(v, d));
-    return v;
+    v = Op::apply(v, dpp_f32<kDppXor1>(v));
+    v = Op::apply(v, dpp_f32<kDppXor2>(v));
+    v = Op::apply(v, dpp_f32<kDppHalfMirror>(v));
+    v = Op::apply(v, dpp_f32<kDppMirror>(v));
+    const auto lane = [&](int l) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), l)); };
+    return Op::apply(Op::apply(lane(0), lane(16)), Op::apply(lane(32), lane(48)));
 }
 
 // over the workgroup, in a fixed order; the result in every thread.  lds: one float for each wave.
@@ -68,6 +169,105 @@ __device__ __forceinline__ float block_all(float v, float *lds)
 }
 
 // (x, column) comes before (y, other) among a row's alternatives
-__device__ __forceinline__ bool before(float x, int column, float y, int other) { return x > y || (x == y && column < other); }
+__device__ __forceinline__ bool before(float x, uint32_t column, float y, uint32_t other) { return x > y || (x == y && column < other); }
+
+// 32 bits that are ordered as the numbers are, and back
+__device__ __forceinline__ uint32_t ordered(float x)
+{
+    const uint32_t u = __float_as_uint(x);
+    return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float from_ordered(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o); }
+
+// max, sum of e^z and sum of e^z z (in units of ln 2) of what a lane has seen of its row, z = (x - max) / eta: one pass, the
+// sums brought to a new maximum where one comes.  A NaN makes the maximum NaN, a score of +inf the sum.
+struct Softmax {
+    float max = -kInf, base = 0.f;  // base: what is subtracted, 0 while there is no maximum
+    float sum = 0.f, weighted = 0.f;
+
+    // brings the sums to the maximum `to`, which is no less than max
+    __device__ __forceinline__ void raise(float to, float c)
+    {
+        const bool empty = max == -kInf;
+        const float d = (max - to) * c, f = exp2_fast(d);
+        weighted = empty ? 0.f : f * fmaf(sum, d, weighted);
+        sum = empty ? 0.f : sum * f;
+        max = to;
+        base = to == -kInf ? 0.f : to;
+    }
+
+    // `count` scores whose largest is `top`; c = log2(e) / eta
+    template <int COUNT>
+    __device__ __forceinline__ void add(const float (&x)[COUNT], float top, float c)
+    {
+        const float to = max_nan(max, top);
+        if (!(to == max)) raise(to, c);
+        float s[2] = {0.f, 0.f}, w[2] = {0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) {
+            const float t = (x[i] - base) * c, e = exp2_fast(t);
+            s[i & 1] += e;
+            w[i & 1] = fmaf(e, t, w[i & 1]);
+        }
+        float ws = w[0] + w[1];
+        if (ws != ws) {  // 0 times -inf of a forbidden column, which adds nothing (a NaN among the scores is in the sum)
+            ws = 0.f;
+#pragma unroll
+            for (int i = 0; i < COUNT; ++i) {
+                const float t = (x[i] - base) * c, e = exp2_fast(t);
+                ws += e > 0.f ? e * t : 0.f;
+            }
+        }
+        sum += s[0] + s[1];
+        weighted += ws;
+    }
+
+    // all lanes' in every lane
+    __device__ __forceinline__ void over_wave(float c)
+    {
+        raise(wave_all<OpMaxF>(max), c);
+        sum = wave_all<OpSumF>(sum);
+        weighted = wave_all<OpSumF>(weighted);
+    }
+    // all waves' in every thread.  lds: 3 WAVES floats, not in use by what comes before.  (A barrier inside.)
+    template <int WAVES>
+    __device__ __forceinline__ void over_block(float c, float *lds)
+    {
+        over_wave(c);
+        if constexpr (WAVES > 1) {
+            if ((threadIdx.x & (kLanes - 1)) == 0) {
+                float *mine = lds + 3 * (threadIdx.x / kLanes);
+                mine[0] = max, mine[1] = sum, mine[2] = weighted;
+            }
+            __syncthreads();
+            Softmax all;
+            float top = lds[0];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) top = max_nan(top, lds[3 * w]);
+            all.max = top;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
+                Softmax one;
+                one.max = lds[3 * w], one.sum = lds[3 * w + 1], one.weighted = lds[3 * w + 2];
+                one.raise(top, c);
+                all.sum += one.sum, all.weighted += one.weighted;
+            }
+            *this = all;
+        }
+    }
+    __device__ __forceinline__ bool none() const { return max == -kInf; }
+    __device__ __forceinline__ bool bad() const { return max != max || sum != sum; }
+    __device__ __forceinline__ float log_sum() const { return none() ? -kInf : logf(sum); }
+    __device__ __forceinline__ float entropy() const { return none() ? 0.f : logf(sum) - weighted * kLn2 / sum; }
+};
+
+template <int COUNT>
+__device__ __forceinline__ float largest(const float (&x)[COUNT])
+{
+    float m = x[0];
+#pragma unroll
+    for (int i = 1; i < COUNT; ++i) m = max_nan(m, x[i]);
+    return m;
+}
 
 }  // namespace regot

@@ -1,0 +1,479 @@
+// Log probabilities of given columns, entropy and alternatives of rows of scores, from one read of the scores.
+#pragma once
+
+#include "regot_rows.hpp"
+
+namespace regot {
+
+struct RowArgs {
+    int64_t n;
+    uint32_t m;
+    const void *S;
+    int64_t ldS;
+    const float *bias;
+    float inv_eta, log2_scale;  // 1 / eta, log2(e) / eta
+    const int32_t *target;
+    int targets, k;
+    float *logprob, *entropy, *stats;
+    int32_t *top_idx;
+    float *top_logprob;
+    // a row is cut into slices of kSlice columns, `block` of them a block; a workgroup takes part_blocks blocks of a row.
+    // What the parts of rows found is in the workspace.
+    int block, block_log2, blocks, scan_log2, parts, part_blocks;  // (block: a power of two; 1 << scan_log2 is not below blocks)
+    float *part_sums;       // [n][parts][3]
+    float *part_max;        // [n][blocks][kThreads]
+    // gradient
+    const float *stats_in, *entropy_in, *g_logprob, *g_entropy;
+    void *dS;
+    int64_t ldD;
+    // distillation
+    const float *t_score, *row_weight;
+    float *loss;
+};
+
+constexpr int kGroup = 16;                    // scores a lane works on at a time
+constexpr uint32_t kSlice = kThreads * kGroup;  // columns of a row that a workgroup works on at a time
+constexpr int kWholeBlocks = 16;              // blocks of a row that one workgroup reads
+constexpr int kPartBlocks = 64;               // of one that several do, at most
+constexpr int kList = 512;                    // blocks, and columns, that may hold the best k; beyond, they are found one by one
+
+// A column and its score as one number: larger for what comes first among a row's alternatives.  0 is none.
+__device__ __forceinline__ uint64_t alternative(float x, uint32_t column) { return (uint64_t)ordered(x + 0.f) << 32 | (uint32_t)~column; }
+__device__ __forceinline__ float score_of(uint64_t a) { return from_ordered((uint32_t)(a >> 32)); }
+__device__ __forceinline__ uint32_t column_of(uint64_t a) { return ~(uint32_t)a; }
+constexpr uint64_t kForbidden = (uint64_t)0x007fffffu << 32 | 0xffffffffu;  // (-inf, column 0)
+
+// The k-th largest of COUNT scores a lane over the wave, its low 16 bits cut off: k of them are not below it; -inf if there
+// are fewer than k above that.
+template <int COUNT>
+__device__ __forceinline__ float kth_largest_bound(const float (&x)[COUNT], int k)
+{
+    uint32_t p[COUNT], t = 0;
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) p[i] = ordered(x[i]) >> 16;
+#pragma unroll
+    for (int bit = 15; bit >= 0; --bit) {
+        const uint32_t c = t | 1u << bit;
+        int have = 0;
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) have += __builtin_popcountll(__ballot(p[i] >= c));
+        if (have >= k) t = c;
+    }
+    return t > 0x007fu ? from_ordered(t << 16) : -kInf;
+}
+
+// The same for few: the k-th largest of one score a lane (k <= 64), by counting for each lane those above its own.  About 800
+// cycles, where the 16 rounds above, one after the other, are about 3700 for four scores a lane.
+constexpr int kFew = 32;
+__device__ __forceinline__ float kth_largest_few(float x, int k)
+{
+    int above = 0;
+#pragma unroll
+    for (int l = 0; l < kLanes; ++l) above += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), l)) > x;
+    return -wave_all<OpMaxF>(above < k ? -x : -kInf);
+}
+
+// Ranks `count` different alternatives by comparing each with all: place(rank, alternative) for those among the first k.
+// The list has kRankPad entries of room behind them.
+constexpr int kRankPad = 8;
+template <typename F>
+__device__ __forceinline__ void rank_all(const uint64_t *list, int count, int thread, int threads, int k, F place)
+{
+    for (int i = thread; i < count; i += threads) {
+        const uint64_t mine = list[i];
+        int rank = 0;
+        for (int o = 0; o < count; o += kRankPad) {
+            uint64_t v[kRankPad];
+#pragma unroll
+            for (int q = 0; q < kRankPad; ++q) v[q] = list[o + q];
+#pragma unroll
+            for (int q = 0; q < kRankPad; ++q) rank += v[q] > mine && o + q < count;
+        }
+        if (rank < k) place(rank, mine);
+    }
+}
+
+// What is written of a row once its sums are known.
+struct RowOut {
+    const RowArgs &A;
+    int64_t row;
+    bool none, bad;
+    float max, log_sum;
+    __device__ __forceinline__ RowOut(const RowArgs &A_, int64_t row_, const Softmax &soft, bool first) : A(A_), row(row_), none(soft.none()), bad(soft.bad())
+    {
+        max = bad ? kNan : soft.max;
+        log_sum = bad ? kNan : soft.log_sum();
+        if (first) {
+            if (A.stats) {
+                A.stats[2 * row] = max;
+                A.stats[2 * row + 1] = log_sum;
+            }
+            if (A.entropy) A.entropy[row] = bad ? kNan : soft.entropy();
+        }
+    }
+    __device__ __forceinline__ float logprob(float x) const { return none ? -kInf : (x - max) * A.inv_eta - log_sum; }
+    __device__ __forceinline__ void top(int rank, uint64_t a) const
+    {
+        A.top_idx[row * A.k + rank] = (int32_t)column_of(a);
+        A.top_logprob[row * A.k + rank] = logprob(score_of(a));
+    }
+    __device__ __forceinline__ void no_top(int rank) const
+    {
+        A.top_idx[row * A.k + rank] = -1;
+        A.top_logprob[row * A.k + rank] = bad ? kNan : -kInf;
+    }
+};
+
+// The scores of one row.
+template <int TYPE, bool BIAS>
+struct RowScores {
+    using T = Score<TYPE>;
+    static constexpr int kGroupVecs = kGroup / T::kVec;
+    const typename T::Raw *S;
+    const float *bias;
+    uint32_t m;
+    __device__ __forceinline__ RowScores(const RowArgs &A, int64_t row) : S(static_cast<const typename T::Raw *>(A.S) + row * A.ldS), bias(A.bias), m(A.m) {}
+    __device__ __forceinline__ float operator()(uint32_t j) const
+    {
+        const float v = T::get(S[j]);
+        return BIAS ? v + bias[j] : v;
+    }
+    // 16 bytes from column j on
+    __device__ __forceinline__ void unpack(u32x4 raw, uint32_t j, float *x) const
+    {
+        const Span<TYPE> span(j, m);
+        T::unpack(raw, x);
+        if constexpr (BIAS) span.add_bias(x, bias, m);
+        span.mask(x);
+    }
+    __device__ __forceinline__ void read(uint32_t j, float *x) const { unpack(Span<TYPE>(j, m).template load<false>(S, m), j, x); }
+};
+
+// The given columns' log probabilities.  The first one of each thread is asked for before the row is read.
+template <int TYPE, bool BIAS>
+struct Given {
+    int column = -1;
+    float x = 0.f;
+    __device__ __forceinline__ void ask(const RowArgs &A, int64_t row, const RowScores<TYPE, BIAS> &scores, int t)
+    {
+        if (t >= A.targets) return;
+        column = A.target[row * A.targets + t];
+        if ((uint32_t)column < A.m) x = scores((uint32_t)column);
+    }
+    __device__ __forceinline__ void tell(const RowArgs &A, const RowOut &out, const RowScores<TYPE, BIAS> &scores, int thread, int threads)
+    {
+        for (int t = thread; t < A.targets; t += threads) {
+            if (t != thread) ask(A, out.row, scores, t);
+            A.logprob[out.row * A.targets + t] = (uint32_t)column < A.m ? out.logprob(x) : 0.f;
+        }
+    }
+};
+
+// The best of a thread's columns (the 16 bytes number thread, thread + threads, ... of the row) that comes behind `last`; 0: none.
+template <int TYPE, bool BIAS>
+__device__ __forceinline__ uint64_t best_before(const RowScores<TYPE, BIAS> &scores, uint64_t last, int thread, int threads)
+{
+    using T = Score<TYPE>;
+    uint64_t best = 0;
+    for (uint32_t j = thread * T::kVec; j < scores.m; j += threads * T::kVec) {
+        float x[T::kVec];
+        scores.read(j, x);
+        const uint32_t first = Span<TYPE>(j, scores.m).first;
+#pragma unroll
+        for (int e = 0; e < T::kVec; ++e) {
+            const uint64_t a = alternative(x[e], first + e);
+            if (a < last && a > best && a > kForbidden) best = a;
+        }
+    }
+    return best;
+}
+
+struct TopShared {
+    float lane_max[kThreads];
+    uint32_t hot[kThreads], block[kList];
+    __align__(16) uint64_t list[kList + kRankPad];
+    uint64_t best[kWaves];
+    int hots, blocks, count;
+};
+
+// The k best columns of a row, by a workgroup that knows the maximum of each thread's columns in each block of the row
+// (block_max[b], thread t having the 16 bytes number t, t + kThreads, ... of the row): k columns are at or above the
+// k-th largest of the threads' maxima, and little more than k are, in little more than k of the (block, thread) pairs.
+// Those are read again.  Where more than fit the lists may be among the best (many equal scores), the
+// best are found one by one, each thread offering the best of its columns that is behind the last one found.
+template <int TYPE, bool BIAS>
+__device__ __forceinline__ void best_columns(const RowArgs &A, const RowOut &out, const RowScores<TYPE, BIAS> &scores, float my_max,
+                                             const float (*block_max)[kThreads], TopShared &L)
+{
+    using T = Score<TYPE>;
+    const int lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes;
+    constexpr uint32_t kStep = kThreads * T::kVec;
+    const int vecs_log2 = A.block_log2 + cbits(kSlice / kStep);  // 16-byte loads of a pair
+    L.lane_max[threadIdx.x] = my_max;
+    if (threadIdx.x == 0) L.hots = L.blocks = L.count = 0;
+    __syncthreads();
+    int count = 0;
+    if (!out.bad && !out.none) {
+        float all[kWaves];
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) all[w] = L.lane_max[w * kLanes + lane];
+        const float bound = A.k <= kFew ? kth_largest_few(largest(all), A.k) : kth_largest_bound(all, A.k);
+        if (my_max >= bound && my_max > -kInf) L.hot[atomicAdd(&L.hots, 1)] = threadIdx.x;
+        __syncthreads();
+        const int hots = L.hots;
+        for (int i = threadIdx.x; i < hots << A.scan_log2; i += kThreads) {
+            const uint32_t thread = L.hot[i >> A.scan_log2];
+            const int b = i & ((1 << A.scan_log2) - 1);
+            if (b >= A.blocks) continue;
+            const float top = block_max[b][thread];
+            if (top >= bound && top > -kInf) {
+                const int at = atomicAdd(&L.blocks, 1);
+                if (at < kList) L.block[at] = (uint32_t)b * kThreads + thread;
+            }
+        }
+        __syncthreads();
+        const int pairs = L.blocks;
+        if (pairs <= kList) {
+            for (int i = threadIdx.x; i < pairs << vecs_log2; i += kThreads) {
+                const uint32_t pair = L.block[i >> vecs_log2];
+                const uint32_t j = (((pair / kThreads) << vecs_log2) + (i & ((1 << vecs_log2) - 1))) * kStep + (pair % kThreads) * T::kVec;
+                if (j >= A.m) continue;
+                float x[T::kVec];
+                scores.read(j, x);
+                const uint32_t first = Span<TYPE>(j, A.m).first;
+#pragma unroll
+                for (int e = 0; e < T::kVec; ++e)
+                    if (x[e] >= bound && x[e] > -kInf) {
+                        const int at = atomicAdd(&L.count, 1);
+                        if (at < kList) L.list[at] = alternative(x[e], first + e);
+                    }
+            }
+        }
+        __syncthreads();
+        count = L.count;
+        if (pairs > kList || count > kList) {
+            uint64_t mine = best_before(scores, ~0ull, threadIdx.x, kThreads);
+            for (count = 0; count < A.k; ++count) {
+                uint64_t best = mine;
+#pragma unroll
+                for (int d = 1; d < kLanes; d *= 2) {
+                    const uint64_t other = __shfl_xor((unsigned long long)best, d);
+                    best = other > best ? other : best;
+                }
+                __syncthreads();
+                if (lane == 0) L.best[wave] = best;
+                __syncthreads();
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w) best = L.best[w] > best ? L.best[w] : best;
+                if (best == 0) break;
+                if (threadIdx.x == 0) out.top(count, best);
+                if (best == mine) mine = best_before(scores, best, threadIdx.x, kThreads);
+            }
+        } else {
+            rank_all(L.list, count, threadIdx.x, kThreads, A.k, [&](int rank, uint64_t a) { out.top(rank, a); });
+        }
+    }
+    for (int i = count + threadIdx.x; i < A.k; i += kThreads) out.no_top(i);
+}
+
+// A row, or a part of one, by a workgroup.  VECS: 16-byte loads a lane has in flight.
+template <int TYPE, bool BIAS, bool TOP, int VECS, bool PARTS>
+__global__ __launch_bounds__(kThreads) void row_logprob_kernel(RowArgs A)
+{
+    using T = Score<TYPE>;
+    using Scores = RowScores<TYPE, BIAS>;
+    constexpr uint32_t kStep = kThreads * T::kVec;
+    constexpr int kVecsOfGroup = Scores::kGroupVecs, kGroups = VECS / kVecsOfGroup;
+    __shared__ float block_max[kWholeBlocks][kThreads];  // (TOP and whole rows)
+    __shared__ float team_sums[3 * kWaves];
+    __shared__ TopShared shared;
+    const uint32_t at = threadIdx.x * T::kVec;
+
+    const int64_t tasks = PARTS ? A.n * A.parts : A.n;
+    for (int64_t task = blockIdx.x; task < tasks; task += gridDim.x) {
+        const int64_t row = PARTS ? task / A.parts : task;
+        const int part = PARTS ? (int)(task - row * A.parts) : 0;
+        const Scores scores(A, row);
+        const uint32_t part_columns = PARTS ? (uint32_t)A.part_blocks * A.block * kSlice : 0;
+        const uint32_t begin = part * part_columns, end = PARTS ? min(A.m, begin + part_columns) : A.m;
+        Given<TYPE, BIAS> given;
+        if constexpr (!PARTS) given.ask(A, row, scores, threadIdx.x);
+
+        Softmax soft;
+        float top_of_block = -kInf;
+        int block = part * A.part_blocks, left = A.block;  // slices of the block still to come
+        const auto block_done = [&]() {
+            if constexpr (PARTS) A.part_max[(row * A.blocks + block) * kThreads + threadIdx.x] = top_of_block;
+            else block_max[block][threadIdx.x] = top_of_block;
+            top_of_block = -kInf;
+            ++block;
+            left = A.block;
+        };
+        for (uint32_t j0 = begin; j0 < end; j0 += VECS * kStep) {
+            u32x4 raw[VECS];
+#pragma unroll
+            for (int u = 0; u < VECS; ++u)
+                if (j0 + u / kVecsOfGroup * kSlice < end) raw[u] = Span<TYPE>(j0 + u * kStep + at, A.m).template load<true>(scores.S, A.m);
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) {
+                if (j0 + g * kSlice < end) {
+                    float x[kGroup];
+#pragma unroll
+                    for (int v = 0; v < kVecsOfGroup; ++v) scores.unpack(raw[g * kVecsOfGroup + v], j0 + (g * kVecsOfGroup + v) * kStep + at, x + v * T::kVec);
+                    const float top = largest(x);
+                    soft.add(x, top, A.log2_scale);
+                    if constexpr (TOP) {
+                        top_of_block = max_nan(top_of_block, top);
+                        if (--left == 0) block_done();
+                    }
+                }
+            }
+        }
+        if constexpr (TOP)
+            if (left < A.block) block_done();
+        const float my_max = soft.max;
+        soft.over_block<kWaves>(A.log2_scale, team_sums);
+        if constexpr (PARTS) {
+            if (threadIdx.x == 0) {
+                float *const sums = A.part_sums + 3 * task;
+                sums[0] = soft.max, sums[1] = soft.sum, sums[2] = soft.weighted;
+            }
+        } else {
+            const RowOut out(A, row, soft, threadIdx.x == 0);
+            given.tell(A, out, scores, threadIdx.x, kThreads);
+            if constexpr (TOP) best_columns(A, out, scores, my_max, block_max, shared);
+        }
+        __syncthreads();  // the sums and the lists are read
+    }
+}
+
+// A row's parts joined: a workgroup a row.
+template <int TYPE, bool BIAS, bool TOP>
+__global__ __launch_bounds__(kThreads) void row_logprob_join_kernel(RowArgs A)
+{
+    __shared__ float team_sums[3 * kWaves];
+    __shared__ TopShared shared;
+    __shared__ float block_max[kPartBlocks][kThreads];
+    for (int64_t row = blockIdx.x; row < A.n; row += gridDim.x) {
+        const RowScores<TYPE, BIAS> scores(A, row);
+        Given<TYPE, BIAS> given;
+        given.ask(A, row, scores, threadIdx.x);
+        float my_max = -kInf;
+        if constexpr (TOP) {
+            const float *const maxima = A.part_max + row * A.blocks * kThreads + threadIdx.x;
+            constexpr int kAsked = 32;  // (all of them, but for long rows)
+            for (int b0 = 0; b0 < A.blocks; b0 += kAsked) {
+                float top[kAsked];
+#pragma unroll
+                for (int i = 0; i < kAsked; ++i) top[i] = b0 + i < A.blocks ? maxima[(b0 + i) * kThreads] : -kInf;
+#pragma unroll
+                for (int i = 0; i < kAsked; ++i) block_max[b0 + i][threadIdx.x] = top[i], my_max = max_nan(my_max, top[i]);
+            }
+        }
+        Softmax soft;
+        for (int p = threadIdx.x; p < A.parts; p += kThreads) {  // (at most kThreads parts)
+            const float *const sums = A.part_sums + 3 * (row * A.parts + p);
+            soft.max = sums[0], soft.sum = sums[1], soft.weighted = sums[2];
+        }
+        soft.over_block<kWaves>(A.log2_scale, team_sums);
+        const RowOut out(A, row, soft, threadIdx.x == 0);
+        given.tell(A, out, scores, threadIdx.x, kThreads);
+        if constexpr (TOP) best_columns(A, out, scores, my_max, block_max, shared);
+        __syncthreads();
+    }
+}
+
+// Narrow rows: a wave a row, which is held in registers as it was read: VECS 16-byte loads a lane.
+template <int TYPE, bool BIAS, bool TOP, int VECS>
+__global__ __launch_bounds__(kThreads) void row_logprob_narrow_kernel(RowArgs A)
+{
+    using T = Score<TYPE>;
+    using Scores = RowScores<TYPE, BIAS>;
+    constexpr uint32_t kStep = kLanes * T::kVec;
+    constexpr int kHeld = 256;
+    __shared__ uint16_t pair[kWaves][VECS * kLanes];
+    __shared__ __align__(16) uint64_t list[kWaves][kHeld + kRankPad];
+    const int lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes;
+    const uint32_t at = lane * T::kVec;
+    for (int64_t row = (int64_t)blockIdx.x * kWaves + wave; row < A.n; row += (int64_t)gridDim.x * kWaves) {
+        const Scores scores(A, row);
+        Given<TYPE, BIAS> given;
+        given.ask(A, row, scores, lane);
+        u32x4 raw[VECS];
+#pragma unroll
+        for (int u = 0; u < VECS; ++u) raw[u] = Span<TYPE>(u * kStep + at, A.m).template load<true>(scores.S, A.m);
+        Softmax soft;
+        float top[VECS];  // the largest of each load
+#pragma unroll
+        for (int u = 0; u < VECS; ++u) {
+            top[u] = -kInf;
+            if (u * kStep < A.m) {
+                float x[T::kVec];
+                scores.unpack(raw[u], u * kStep + at, x);
+                top[u] = largest(x);
+                soft.add(x, top[u], A.log2_scale);
+            }
+        }
+        soft.over_wave(A.log2_scale);
+        const RowOut out(A, row, soft, lane == 0);
+        given.tell(A, out, scores, lane, kLanes);
+        if constexpr (TOP) {
+            // as in best_columns, with two maxima a lane for the bound, and (load, lane) for (block, thread)
+            int count = 0;
+            if (!out.bad && !out.none) {
+                float half[VECS == 1 ? 1 : 2];
+                half[0] = top[0];
+#pragma unroll
+                for (int u = 1; u < VECS; ++u) half[u & 1] = u == 1 ? top[1] : max_nan(half[u & 1], top[u]);
+                const float bound = kth_largest_bound(half, A.k);
+                int pairs = 0;
+                wave_lds();
+#pragma unroll
+                for (int u = 0; u < VECS; ++u) {
+                    const bool is = top[u] >= bound && top[u] > -kInf;
+                    const uint64_t mask = __ballot(is);
+                    if (is) pair[wave][pairs + lanes_below(mask)] = u * kLanes + lane;
+                    pairs += __builtin_popcountll(mask);
+                }
+                wave_lds();
+                for (int i0 = 0; i0 < pairs; i0 += kLanes) {
+                    float x[T::kVec];
+                    uint32_t first = 0;
+                    if (i0 + lane < pairs) {
+                        const uint32_t j = pair[wave][i0 + lane] * T::kVec;
+                        scores.read(j, x);
+                        first = Span<TYPE>(j, A.m).first;
+                    }
+#pragma unroll
+                    for (int e = 0; e < T::kVec; ++e) {
+                        const bool is = i0 + lane < pairs && x[e] >= bound && x[e] > -kInf;
+                        const uint64_t mask = __ballot(is);
+                        const int to = count + lanes_below(mask);
+                        if (is && to < kHeld) list[wave][to] = alternative(x[e], first + e);
+                        count += __builtin_popcountll(mask);
+                    }
+                }
+                wave_lds();
+                if (count <= kHeld) {
+                    rank_all(list[wave], count, lane, kLanes, A.k, [&](int rank, uint64_t a) { out.top(rank, a); });
+                } else {
+                    uint64_t last = ~0ull;
+                    for (count = 0; count < A.k; ++count) {
+                        uint64_t best = best_before(scores, last, lane, kLanes);
+#pragma unroll
+                        for (int d = 1; d < kLanes; d *= 2) {
+                            const uint64_t other = __shfl_xor((unsigned long long)best, d);
+                            best = other > best ? other : best;
+                        }
+                        if (best == 0) break;
+                        if (lane == 0) out.top(count, best);
+                        last = best;
+                    }
+                }
+            }
+            for (int i = count + lane; i < A.k; i += kLanes) out.no_top(i);
+        }
+    }
+}
+
+}  // namespace regot
