@@ -8,6 +8,7 @@
 #include <algorithm>
 
 #include "regot.h"
+#include "regot_rows_grad.hpp"
 #include "regot_rows_logprob.hpp"
 
 namespace {
@@ -19,133 +20,6 @@ constexpr size_t kAlign = 256;
 
 bool misaligned(const void *p, size_t a) { return ((uintptr_t)p % a) != 0; }
 int hip_status() { return hipGetLastError() == hipSuccess ? REGOT_OK : REGOT_ERR_HIP; }
-
-template <int TYPE>
-struct Row {
-    const typename Score<TYPE>::Raw *S;
-    const float *bias;
-    __device__ __forceinline__ Row(const RowArgs &A, int64_t row)
-        : S(static_cast<const typename Score<TYPE>::Raw *>(A.S) + row * A.ldS), bias(A.bias) {}
-    __device__ __forceinline__ float operator()(int j) const
-    {
-        const float x = Score<TYPE>::get(S[j]);
-        return bias ? x + bias[j] : x;
-    }
-};
-
-// max, sum of exp and sum of exp times exponent of a row, from two passes over it; NaN in `sum` where the row has a NaN or +inf
-template <int TYPE>
-__device__ void row_stats(const RowArgs &A, const Row<TYPE> &x, float *lds, float &top, float &sum, float &weighted)
-{
-    float mx = -kInf;
-    bool nan = false;
-    for (int j = threadIdx.x; j < A.m; j += kThreads) {
-        const float v = x(j);
-        nan |= v != v;
-        mx = fmaxf(mx, v);
-    }
-    mx = block_all<OpMaxF, kWaves>(mx, lds);
-    nan = __syncthreads_or(nan);
-    float s = 0.f, e1 = 0.f;
-    for (int j = threadIdx.x; j < A.m && mx > -kInf; j += kThreads) {
-        const float t = (x(j) - mx) * A.log2_scale, e = exp2_fast(t);
-        s += e;
-        e1 += e > 0.f ? e * t : 0.f;
-    }
-    top = mx;
-    sum = block_all<OpSumF, kWaves>(s, lds);
-    weighted = block_all<OpSumF, kWaves>(e1, lds) * kLn2;
-    if (nan || sum != sum) top = sum = weighted = kNan;
-}
-
-template <int TYPE>
-__global__ __launch_bounds__(kThreads) void row_logprob_grad_kernel(RowArgs A)
-{
-    using T = Score<TYPE>;
-    __shared__ float lds[kWaves];
-    const int64_t row = blockIdx.x;
-    const Row<TYPE> x(A, row);
-    const float mx = A.stats_in[2 * row], log_sum = A.stats_in[2 * row + 1];
-    const bool none = mx == -kInf;
-    const float h = A.g_entropy ? A.g_entropy[row] : 0.f, H = A.g_entropy ? A.entropy_in[row] : 0.f;
-    float g = 0.f;
-    for (int t = threadIdx.x; t < A.targets; t += kThreads)
-        if ((uint32_t)A.target[row * A.targets + t] < (uint32_t)A.m) g += A.g_logprob[row * A.targets + t];
-    g = block_all<OpSumF, kWaves>(g, lds);
-    const auto value = [&](int j) {
-        const float logp = (x(j) - mx) * A.inv_eta - log_sum, p = exp2_fast(logp * 1.44269504088896340736f);
-        return -p * g - (p > 0.f ? h * p * (logp + H) : p * 0.f);
-    };
-    typename T::Raw *out = static_cast<typename T::Raw *>(A.dS) + row * A.ldD;
-    for (int j = threadIdx.x; j < A.m; j += kThreads) out[j] = T::put(none ? 0.f : value(j) * A.inv_eta);
-    __threadfence_block();
-    __syncthreads();
-    for (int t = threadIdx.x; t < A.targets && !none; t += kThreads) {
-        const int j = A.target[row * A.targets + t];
-        if ((uint32_t)j >= (uint32_t)A.m) continue;
-        float mine = 0.f;
-        for (int u = 0; u < A.targets; ++u)
-            if (A.target[row * A.targets + u] == j) mine += A.g_logprob[row * A.targets + u];
-        out[j] = T::put((mine + value(j)) * A.inv_eta);
-    }
-}
-
-template <int TYPE>
-__global__ __launch_bounds__(kThreads) void row_distill_kernel(RowArgs A)
-{
-    using T = Score<TYPE>;
-    __shared__ float lds[kWaves];
-    const int64_t row = blockIdx.x;
-    const Row<TYPE> x(A, row);
-    const int32_t *list = A.target + row * A.k;
-    const float *score = A.t_score + row * A.k;
-    typename T::Raw *out = A.dS ? static_cast<typename T::Raw *>(A.dS) + row * A.ldD : nullptr;
-    float t_max = -kInf;
-    bool nan = false;
-    for (int l = threadIdx.x; l < A.k; l += kThreads)
-        if ((uint32_t)list[l] < (uint32_t)A.m) t_max = fmaxf(t_max, score[l]), nan |= score[l] != score[l];
-    t_max = block_all<OpMaxF, kWaves>(t_max, lds);
-    nan = __syncthreads_or(nan);
-    if (t_max == -kInf && !nan) {  // padding
-        if (threadIdx.x == 0) A.loss[row] = 0.f;
-        for (int j = threadIdx.x; j < A.m && out; j += kThreads) out[j] = T::put(0.f);
-        return;
-    }
-    if (nan) t_max = kNan;
-    float q_sum = 0.f;
-    for (int l = threadIdx.x; l < A.k; l += kThreads)
-        if ((uint32_t)list[l] < (uint32_t)A.m) q_sum += exp2_fast((score[l] - t_max) * A.log2_scale);
-    q_sum = block_all<OpSumF, kWaves>(q_sum, lds);
-    float mx, s, e1;
-    row_stats<TYPE>(A, x, lds, mx, s, e1);
-    const bool none = mx == -kInf;
-    const float log_sum = none ? -kInf : logf(s), log_q = logf(q_sum);
-    float loss = 0.f;
-    for (int l = threadIdx.x; l < A.k; l += kThreads) {
-        const int j = list[l];
-        if ((uint32_t)j >= (uint32_t)A.m) continue;
-        const float t = (score[l] - t_max) * A.inv_eta, q = exp2_fast((score[l] - t_max) * A.log2_scale) / q_sum;
-        // (q times the distance before it is divided by eta: a mask of the type's lowest value stays finite)
-        loss += q == 0.f ? 0.f : none ? kInf : q * (t - log_q + log_sum) + q * A.inv_eta * (mx - x(j));
-    }
-    loss = block_all<OpSumF, kWaves>(loss, lds);
-    if (threadIdx.x == 0) A.loss[row] = loss;
-    if (!out) return;
-    const float w = q_sum != q_sum ? kNan : (A.row_weight ? A.row_weight[row] : 1.f) * A.inv_eta;
-    const float inv = 1.f / s;
-    const auto p = [&](int j) { return exp2_fast((x(j) - mx) * A.log2_scale) * inv; };
-    for (int j = threadIdx.x; j < A.m; j += kThreads) out[j] = T::put(none ? 0.f : w * p(j));
-    __threadfence_block();
-    __syncthreads();
-    for (int l = threadIdx.x; l < A.k && !none; l += kThreads) {
-        const int j = list[l];
-        if ((uint32_t)j >= (uint32_t)A.m) continue;
-        float q = 0.f;
-        for (int u = 0; u < A.k; ++u)
-            if (list[u] == j) q += exp2_fast((score[u] - t_max) * A.log2_scale) / q_sum;
-        out[j] = T::put(w * (p(j) - q));
-    }
-}
 
 struct RouteArgs {
     int n, m;
@@ -340,12 +214,12 @@ int64_t power_of_two(int64_t least)
     return p;
 }
 
-RowPlan plan_rows(int64_t n, int64_t m, int k)
+RowPlan plan_rows(int64_t n, int64_t m, int k, int few = kFewRows)
 {
     RowPlan P;
     const int64_t slices = std::max<int64_t>((m + kSlice - 1) / kSlice, 1);
     int64_t parts = 1;
-    if (n <= kFewRows && slices >= kLongRow) parts = std::min<int64_t>({slices, kPartBlocks, std::max<int64_t>(kPlaces / n, kLeastParts)});
+    if (n <= few && slices >= kLongRow) parts = std::min<int64_t>({slices, kPartBlocks, std::max<int64_t>(kPlaces / n, kLeastParts)});
     if (parts > 1) {
         const int64_t of_part = (slices + parts - 1) / parts;  // slices of a part
         const int64_t most = std::max<int64_t>(kPartBlocks / parts, 1);   // blocks of a part
@@ -373,7 +247,9 @@ void launch_logprob(const RowArgs &A, const RowPlan &P, hipStream_t s)
     const dim3 threads(kThreads);
     const auto grid = [](int64_t blocks) { return dim3((unsigned)std::min(blocks, kMaxGrid)); };
     const dim3 by_wave = grid((A.n + kWaves - 1) / kWaves);
-    if (A.m <= kLoad) {
+    if (A.m <= 2 * kLanes) {
+        hipLaunchKernelGGL((row_logprob_narrow_kernel<TYPE + kSingle, BIAS, TOP, 2>), by_wave, threads, 0, s, A);
+    } else if (A.m <= kLoad) {
         hipLaunchKernelGGL((row_logprob_narrow_kernel<TYPE, BIAS, TOP, 1>), by_wave, threads, 0, s, A);
     } else if (A.m <= 2 * kLoad) {
         hipLaunchKernelGGL((row_logprob_narrow_kernel<TYPE, BIAS, TOP, 2>), by_wave, threads, 0, s, A);
@@ -392,6 +268,102 @@ void launch_logprob(const RowArgs &A, const RowPlan &P, hipStream_t s)
 {
     if (A.bias) A.k > 0 ? launch_logprob<TYPE, true, true>(A, P, s) : launch_logprob<TYPE, true, false>(A, P, s);
     else A.k > 0 ? launch_logprob<TYPE, false, true>(A, P, s) : launch_logprob<TYPE, false, false>(A, P, s);
+}
+
+void take_plan(RowArgs &A, const RowPlan &P, void *workspace)
+{
+    A.block = P.block;
+    A.block_log2 = cbits(P.block);
+    A.blocks = P.blocks;
+    A.scan_log2 = cbits(power_of_two(P.blocks));
+    A.parts = P.parts;
+    A.part_blocks = P.part_blocks;
+    A.part_columns = (uint32_t)P.part_blocks * P.block * kSlice;
+    A.part_sums = static_cast<float *>(workspace);
+    A.part_max = reinterpret_cast<float *>(static_cast<char *>(workspace) + P.max);
+}
+
+// Gradients of log probabilities: parts of rows, so that there are workgroups enough.
+template <int TYPE, bool BIAS>
+void launch_logprob_grad(RowArgs &A, hipStream_t s)
+{
+    constexpr int kVecs = 4;
+    const auto grid = [](int64_t blocks) { return dim3((unsigned)std::min(blocks, kMaxGrid)); };
+    if (A.m <= 2 * kLanes) {
+        A.parts = 1;
+        A.part_columns = A.m;
+        hipLaunchKernelGGL((row_logprob_grad_kernel<TYPE + kSingle, BIAS, 1, 2>), grid((A.n + kWaves - 1) / kWaves), dim3(kThreads), 0, s, A);
+    } else if (A.m <= kVecs * kLanes * Score<TYPE>::kVec) {
+        A.parts = 1;
+        A.part_columns = A.m;
+        hipLaunchKernelGGL((row_logprob_grad_kernel<TYPE, BIAS, 1, kVecs>), grid((A.n + kWaves - 1) / kWaves), dim3(kThreads), 0, s, A);
+    } else {
+        constexpr uint32_t kColumns = kVecs * kThreads * Score<TYPE>::kVec;
+        A.part_columns = kColumns;
+        A.parts = (int)((A.m + kColumns - 1) / kColumns);
+        hipLaunchKernelGGL((row_logprob_grad_kernel<TYPE, BIAS, kWaves, kVecs>), grid(A.n * A.parts), dim3(kThreads), 0, s, A);
+    }
+}
+
+template <int TYPE>
+void launch_logprob_grad(RowArgs &A, hipStream_t s)
+{
+    A.bias ? launch_logprob_grad<TYPE, true>(A, s) : launch_logprob_grad<TYPE, false>(A, s);
+}
+
+void launch_logprob_grad(RowArgs &A, int type, hipStream_t s)
+{
+    if (type == REGOT_F32) launch_logprob_grad<REGOT_F32>(A, s);
+    else if (type == REGOT_BF16) launch_logprob_grad<REGOT_BF16>(A, s);
+    else launch_logprob_grad<REGOT_F16>(A, s);
+}
+
+// Parts as for log probabilities, up to the rows at which a team of 16 waves each is as fast: 64 x 131072 bf16 19.4 us in parts and 25.8, 128 rows
+// 28.5 and 27.4, 192 rows 36.3 and 30.6; 1 row 10.8 and 25.2.
+constexpr int kFewDistilled = 96;
+RowPlan plan_distill(int64_t n, int64_t m) { return plan_rows(n, m, 0, kFewDistilled); }
+
+constexpr int kCUs = 256;
+
+template <int TYPE>
+void launch_distill(const RowArgs &A, hipStream_t s)
+{
+    constexpr uint32_t kLoad = kLanes * Score<TYPE>::kVec;
+    const auto grid = [](int64_t blocks) { return dim3((unsigned)std::min(blocks, kMaxGrid)); };
+    // Teams of more waves hold more of a row between its two reads (the last stretch in registers, the one before in LDS) and
+    // make less of the traffic; of fewer, they keep more rows under way.  us: 16384 x 1000 bf16 1 wave 29, 4 waves 64; 4096 x 10000 4 waves
+    // 51, 8 waves 70; 999 x 33333 4 waves 44, 8 waves holding 40; 4096 x 131072 4 waves 530, 8 waves 518, holding 441, 16 waves holding 488;
+    // 256 x 131072 8 waves holding 39, 16 waves holding 32; 256 x 10000 fp32 4 waves 11.0, 8 waves 9.4.
+    const uint32_t loads = A.m / Score<TYPE>::kVec;
+#define GO(TYPE, W, V, K) hipLaunchKernelGGL((row_distill_kernel<TYPE, W, V, K, false>), grid(W == 1 ? (A.n + kWaves - 1) / kWaves : A.n), dim3(Team<W>::kBlock), 0, s, A)
+    if (A.parts > 1) {
+        hipLaunchKernelGGL((row_logprob_kernel<TYPE, false, false, 8, true>), grid(A.n * A.parts), dim3(kThreads), 0, s, A);
+        hipLaunchKernelGGL((row_distill_kernel<TYPE, kWaves, 4, 0, true>), grid(A.n * A.parts), dim3(kThreads), 0, s, A);
+    } else if (A.m <= 2 * kLanes) {
+        GO(TYPE + kSingle, 1, 2, 0);
+    } else if (A.n > 512 && loads <= 2 * kLanes) {
+        GO(TYPE, 1, 2, 0);
+    } else if (A.n > 512 && loads <= 4 * kLanes) {
+        GO(TYPE, 1, 4, 0);
+    } else if (A.n > 512 && loads <= 8 * kLanes) {
+        GO(TYPE, 1, 8, 0);
+    } else if (loads <= (A.n > 512 ? 64 : 8) * kLanes) {
+        GO(TYPE, 4, 2, 0);
+    } else if (loads <= 64 * kLanes) {
+        GO(TYPE, 8, 4, 0);
+    } else if (A.n > kCUs) {
+        GO(TYPE, 8, 8, 8);
+    } else {
+        GO(TYPE, 16, 8, 8);
+    }
+#undef GO
+}
+
+void launch_distill(const RowArgs &A, int type, hipStream_t s)
+{
+    if (type == REGOT_F32) launch_distill<REGOT_F32>(A, s);
+    else if (type == REGOT_BF16) launch_distill<REGOT_BF16>(A, s);
+    else launch_distill<REGOT_F16>(A, s);
 }
 
 void launch_logprob(const RowArgs &A, int type, const RowPlan &P, hipStream_t s)
@@ -439,14 +411,7 @@ int regot_row_logprob(int64_t n, int64_t m, const void *S, int type, int64_t ldS
     A.stats = stats;
     A.top_idx = top_idx;
     A.top_logprob = top_logprob;
-    A.block = P.block;
-    A.block_log2 = cbits(P.block);
-    A.blocks = P.blocks;
-    A.scan_log2 = cbits(power_of_two(P.blocks));
-    A.parts = P.parts;
-    A.part_blocks = P.part_blocks;
-    A.part_sums = static_cast<float *>(workspace);
-    A.part_max = reinterpret_cast<float *>(static_cast<char *>(workspace) + P.max);
+    take_plan(A, P, workspace);
     launch_logprob(A, type, P, static_cast<hipStream_t>(stream));
     return hip_status();
 }
@@ -473,7 +438,7 @@ int regot_row_logprob_grad(int64_t n, int64_t m, const void *S, int type, int64_
     A.g_entropy = g_entropy;
     A.dS = dS;
     A.ldD = ldD;
-    REGOT_BY_TYPE(row_logprob_grad_kernel, type, dim3((unsigned)n), dim3(kThreads), static_cast<hipStream_t>(stream), A);
+    launch_logprob_grad(A, type, static_cast<hipStream_t>(stream));
     return hip_status();
 }
 
@@ -482,7 +447,7 @@ int regot_row_distill_workspace_bytes(int64_t n, int64_t m, int k, size_t *bytes
     if (!bytes) return REGOT_ERR_NULL;
     if (n < 0 || m < 0 || n > kMaxDim || m > kMaxDim) return REGOT_ERR_DIM;
     if (k < 1 || k > REGOT_ROW_MAX_LIST) return REGOT_ERR_ARG;
-    *bytes = kAlign;
+    *bytes = plan_distill(n, m).total;
     return REGOT_OK;
 }
 
@@ -498,11 +463,10 @@ int regot_row_distill(int64_t n, int64_t m, const void *S, int type, int64_t ldS
     if (misaligned(t_idx, 4) || misaligned(t_score, 4) || misaligned(row_weight, 4) || misaligned(loss, 4) ||
         misaligned(dS, element_bytes(type)))
         return REGOT_ERR_ALIGN;
-    size_t need = 0;
-    regot_row_distill_workspace_bytes(n, m, k, &need);
+    const RowPlan P = plan_distill(n, m);
     if (!workspace) return REGOT_ERR_NULL;
     if (misaligned(workspace, kAlign)) return REGOT_ERR_ALIGN;
-    if (workspace_bytes < need) return REGOT_ERR_WORKSPACE;
+    if (workspace_bytes < P.total) return REGOT_ERR_WORKSPACE;
     if (n == 0) return REGOT_OK;
     RowArgs A = row_args(n, m, S, ldS, nullptr, eta);
     A.target = t_idx;
@@ -512,7 +476,8 @@ int regot_row_distill(int64_t n, int64_t m, const void *S, int type, int64_t ldS
     A.loss = loss;
     A.dS = dS;
     A.ldD = ldD;
-    REGOT_BY_TYPE(row_distill_kernel, type, dim3((unsigned)n), dim3(kThreads), static_cast<hipStream_t>(stream), A);
+    take_plan(A, P, workspace);
+    launch_distill(A, type, static_cast<hipStream_t>(stream));
     return hip_status();
 }
 

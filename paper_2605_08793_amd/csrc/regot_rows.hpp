@@ -24,16 +24,35 @@ __device__ __forceinline__ void wave_lds()
 }
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef u32x4 Any __attribute__((aligned(2)));  // 16 bytes at any multiple of 2
 
-// A score as a 32-bit number, and back (rounded to nearest even, once).
+// A score as a 32-bit number, and back (rounded to nearest even, once); kVec of them are what a lane loads at a time.
+// TYPE + kSingle: one score at a time, for rows that are shorter than a load, or give few lanes one.
+constexpr int kSingle = 16;
 template <int TYPE>
-struct Score;
+struct Score {
+    using Wide = Score<TYPE - kSingle>;
+    using Raw = typename Wide::Raw;
+    using Chunk = Raw;
+    static constexpr int kVec = 1;
+    static __device__ __forceinline__ float get(Raw v) { return Wide::get(v); }
+    static __device__ __forceinline__ Raw put(float v) { return Wide::put(v); }
+    static __device__ __forceinline__ void unpack(Chunk v, float *x) { x[0] = Wide::get(v); }
+    static __device__ __forceinline__ Chunk pack(const Raw *v) { return v[0]; }
+};
+struct WideChunk {
+    using Chunk = u32x4;
+    template <typename Raw>
+    static __device__ __forceinline__ Chunk pack(const Raw *v)
+    {
+        Chunk c;
+        __builtin_memcpy(&c, v, 16);
+        return c;
+    }
+};
 template <>
-struct Score<REGOT_F32> {
+struct Score<REGOT_F32> : WideChunk {
     using Raw = float;
     static constexpr int kVec = 4;
-    static constexpr uint32_t kMinusInf = 0xff800000u;
     static __device__ __forceinline__ float get(Raw v) { return v; }
     static __device__ __forceinline__ Raw put(float v) { return v; }
     static __device__ __forceinline__ void unpack(u32x4 v, float *x)
@@ -43,10 +62,9 @@ struct Score<REGOT_F32> {
     }
 };
 template <>
-struct Score<REGOT_BF16> {
+struct Score<REGOT_BF16> : WideChunk {
     using Raw = __bf16;
     static constexpr int kVec = 8;
-    static constexpr uint32_t kMinusInf = 0xff80ff80u;
     static __device__ __forceinline__ float get(Raw v) { return (float)v; }
     static __device__ __forceinline__ Raw put(float v) { return (__bf16)v; }
     static __device__ __forceinline__ void unpack(u32x4 v, float *x)
@@ -59,10 +77,9 @@ struct Score<REGOT_BF16> {
     }
 };
 template <>
-struct Score<REGOT_F16> {
+struct Score<REGOT_F16> : WideChunk {
     using Raw = _Float16;
     static constexpr int kVec = 8;
-    static constexpr uint32_t kMinusInf = 0xfc00fc00u;
     static __device__ __forceinline__ float get(Raw v) { return (float)v; }
     static __device__ __forceinline__ Raw put(float v) { return (_Float16)v; }
     static __device__ __forceinline__ void unpack(u32x4 v, float *x)
@@ -74,52 +91,64 @@ struct Score<REGOT_F16> {
     }
 };
 
-// The 16 bytes of a row's columns that a lane takes at column j.  Where they would reach beyond the row they are moved back
+// The same number, known from here on only: what is computed from it stays in the branch it is in, instead of taking registers
+// beside the common path (the masks of a row's end took up to 200 scalar registers more than there are).
+__device__ __forceinline__ uint32_t here(uint32_t v)
+{
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
+// What a lane takes of a row at column j, the row having at least kVec.  Where it would reach beyond the row it is moved back
 // to end with it, so that every load is whole and unconditional; the columns before j, which another lane has, are then
 // forbidden ones here.  (Rows start at any multiple of their element: the load is one instruction whatever the address.)
 template <int TYPE>
 struct Span {
     using T = Score<TYPE>;
+    using Raw = typename T::Raw;
+    using Chunk = typename T::Chunk;
+    typedef Chunk Any __attribute__((aligned(alignof(uint16_t))));
     uint32_t first, own;  // the columns first .. first + kVec - 1, of which those from `own` on count
-    __device__ __forceinline__ Span(uint32_t j, uint32_t m) : first(m >= T::kVec ? min(j, m - T::kVec) : 0), own(j) {}
+    __device__ __forceinline__ Span(uint32_t j, uint32_t m) : first(min(j, m - T::kVec)), own(j) {}
     // ONCE: nothing reads the row again soon
     template <bool ONCE>
-    __device__ __forceinline__ u32x4 load(const typename T::Raw *S, uint32_t m) const
+    __device__ __forceinline__ Chunk load(const Raw *S) const
     {
-        u32x4 v;
-        if (m >= T::kVec) {
-            if constexpr (ONCE) v = __builtin_nontemporal_load(reinterpret_cast<const Any *>(S + first));
-            else v = *reinterpret_cast<const Any *>(S + first);
-            return v;
-        }
-        v = u32x4{T::kMinusInf, T::kMinusInf, T::kMinusInf, T::kMinusInf};  // a row shorter than one load
-        typename T::Raw part[T::kVec];
-        __builtin_memcpy(part, &v, 16);
-#pragma unroll
-        for (int e = 0; e < T::kVec; ++e)
-            if ((uint32_t)e < m) part[e] = S[e];
-        __builtin_memcpy(&v, part, 16);
-        return v;
+        if constexpr (T::kVec == 1) return S[first];
+        else if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const Any *>(S + first));
+        else return *reinterpret_cast<const Any *>(S + first);
     }
     // x[e] to -inf where column first + e does not count
     __device__ __forceinline__ void mask(float *x) const
     {
-        if (first != own) {
+        if (__any(first != own)) {  // (the wave at the row's end)
+            const uint32_t from = here(first);
 #pragma unroll
-            for (int e = 0; e < T::kVec; ++e) x[e] = first + e >= own ? x[e] : -kInf;
+            for (int e = 0; e < T::kVec; ++e) x[e] = from + e >= own ? x[e] : -kInf;
         }
     }
-    __device__ __forceinline__ void add_bias(float *x, const float *bias, uint32_t m) const
+    __device__ __forceinline__ void add_bias(float *x, const float *bias) const
     {
         float b[T::kVec];
-        if (m >= T::kVec) {
-            __builtin_memcpy(b, bias + first, sizeof(b));
-        } else {
-#pragma unroll
-            for (int e = 0; e < T::kVec; ++e) b[e] = (uint32_t)e < m ? bias[e] : 0.f;
-        }
+        __builtin_memcpy(b, bias + first, sizeof(b));
 #pragma unroll
         for (int e = 0; e < T::kVec; ++e) x[e] += b[e];
+    }
+    // what a lane computed from the chunk, to the columns that count: one store where all do
+    __device__ __forceinline__ void store(Raw *out, const float *v) const
+    {
+        Raw part[T::kVec];
+#pragma unroll
+        for (int e = 0; e < T::kVec; ++e) part[e] = T::put(v[e]);
+        if (first == own) {
+            if constexpr (T::kVec == 1) out[first] = part[0];
+            else __builtin_nontemporal_store(T::pack(part), reinterpret_cast<Any *>(out + first));
+        } else {
+            const uint32_t from = here(first);
+#pragma unroll
+            for (int e = 0; e < T::kVec; ++e)
+                if (from + e >= own) out[from + e] = part[e];
+        }
     }
 };
 
@@ -196,8 +225,8 @@ struct Softmax {
         base = to == -kInf ? 0.f : to;
     }
 
-    // `count` scores whose largest is `top`; c = log2(e) / eta
-    template <int COUNT>
+    // `count` scores whose largest is `top`; c = log2(e) / eta.  ENTROPY: the weighted sum too
+    template <bool ENTROPY = true, int COUNT>
     __device__ __forceinline__ void add(const float (&x)[COUNT], float top, float c)
     {
         const float to = max_nan(max, top);
@@ -207,10 +236,10 @@ struct Softmax {
         for (int i = 0; i < COUNT; ++i) {
             const float t = (x[i] - base) * c, e = exp2_fast(t);
             s[i & 1] += e;
-            w[i & 1] = fmaf(e, t, w[i & 1]);
+            if constexpr (ENTROPY) w[i & 1] = fmaf(e, t, w[i & 1]);
         }
         float ws = w[0] + w[1];
-        if (ws != ws) {  // 0 times -inf of a forbidden column, which adds nothing (a NaN among the scores is in the sum)
+        if (ENTROPY && ws != ws) {  // 0 times -inf of a forbidden column, which adds nothing (a NaN among the scores is in the sum)
             ws = 0.f;
 #pragma unroll
             for (int i = 0; i < COUNT; ++i) {

@@ -20,6 +20,7 @@ struct RowArgs {
     // a row is cut into slices of kSlice columns, `block` of them a block; a workgroup takes part_blocks blocks of a row.
     // What the parts of rows found is in the workspace.
     int block, block_log2, blocks, scan_log2, parts, part_blocks;  // (block: a power of two; 1 << scan_log2 is not below blocks)
+    uint32_t part_columns;
     float *part_sums;       // [n][parts][3]
     float *part_max;        // [n][blocks][kThreads]
     // gradient
@@ -128,6 +129,7 @@ struct RowOut {
 template <int TYPE, bool BIAS>
 struct RowScores {
     using T = Score<TYPE>;
+    using Chunk = typename T::Chunk;
     static constexpr int kGroupVecs = kGroup / T::kVec;
     const typename T::Raw *S;
     const float *bias;
@@ -138,15 +140,16 @@ struct RowScores {
         const float v = T::get(S[j]);
         return BIAS ? v + bias[j] : v;
     }
-    // 16 bytes from column j on
-    __device__ __forceinline__ void unpack(u32x4 raw, uint32_t j, float *x) const
+    template <bool ONCE>
+    __device__ __forceinline__ Chunk ask(uint32_t j) const { return Span<TYPE>(j, m).template load<ONCE>(S); }
+    __device__ __forceinline__ void unpack(Chunk chunk, uint32_t j, float *x) const
     {
         const Span<TYPE> span(j, m);
-        T::unpack(raw, x);
-        if constexpr (BIAS) span.add_bias(x, bias, m);
+        T::unpack(chunk, x);
+        if constexpr (BIAS) span.add_bias(x, bias);
         span.mask(x);
     }
-    __device__ __forceinline__ void read(uint32_t j, float *x) const { unpack(Span<TYPE>(j, m).template load<false>(S, m), j, x); }
+    __device__ __forceinline__ void read(uint32_t j, float *x) const { unpack(ask<false>(j), j, x); }
 };
 
 // The given columns' log probabilities.  The first one of each thread is asked for before the row is read.
@@ -310,10 +313,10 @@ __global__ __launch_bounds__(kThreads) void row_logprob_kernel(RowArgs A)
             left = A.block;
         };
         for (uint32_t j0 = begin; j0 < end; j0 += VECS * kStep) {
-            u32x4 raw[VECS];
+            typename T::Chunk raw[VECS];
 #pragma unroll
             for (int u = 0; u < VECS; ++u)
-                if (j0 + u / kVecsOfGroup * kSlice < end) raw[u] = Span<TYPE>(j0 + u * kStep + at, A.m).template load<true>(scores.S, A.m);
+                if (j0 + u / kVecsOfGroup * kSlice < end) raw[u] = scores.template ask<true>(j0 + u * kStep + at);
 #pragma unroll
             for (int g = 0; g < kGroups; ++g) {
                 if (j0 + g * kSlice < end) {
@@ -399,9 +402,11 @@ __global__ __launch_bounds__(kThreads) void row_logprob_narrow_kernel(RowArgs A)
         const Scores scores(A, row);
         Given<TYPE, BIAS> given;
         given.ask(A, row, scores, lane);
-        u32x4 raw[VECS];
+        typename T::Chunk raw[VECS];
+        if (A.m > 0) {
 #pragma unroll
-        for (int u = 0; u < VECS; ++u) raw[u] = Span<TYPE>(u * kStep + at, A.m).template load<true>(scores.S, A.m);
+            for (int u = 0; u < VECS; ++u) raw[u] = scores.template ask<true>(u * kStep + at);
+        }
         Softmax soft;
         float top[VECS];  // the largest of each load
 #pragma unroll
