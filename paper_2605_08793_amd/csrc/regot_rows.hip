@@ -10,6 +10,7 @@
 #include "regot.h"
 #include "regot_rows_grad.hpp"
 #include "regot_rows_logprob.hpp"
+#include "regot_rows_route.hpp"
 
 namespace {
 
@@ -20,146 +21,6 @@ constexpr size_t kAlign = 256;
 
 bool misaligned(const void *p, size_t a) { return ((uintptr_t)p % a) != 0; }
 int hip_status() { return hipGetLastError() == hipSuccess ? REGOT_OK : REGOT_ERR_HIP; }
-
-struct RouteArgs {
-    int n, m;
-    const void *S;
-    int64_t ldS;
-    const float *bias;
-    int bias_on, score, groups, groups_kept, group_by, k, renormalise;
-    float scale;
-    int32_t *idx;
-    float *weight;
-    const int32_t *idx_in;
-    const float *g_weight;
-    void *dS;
-    int64_t ldD;
-};
-
-constexpr int kMaxGroups = 64;
-
-__device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + expf(-x)); }
-
-// scores of a row's columns into s: softmax, or sigmoid; by one wave
-template <int TYPE>
-__device__ void row_scores(const RouteArgs &A, const typename Score<TYPE>::Raw *S, int lane, float *s)
-{
-    float mx = -kInf;
-    bool nan = false;
-    for (int j = lane; j < A.m; j += kLanes) {
-        const float x = Score<TYPE>::get(S[j]);
-        s[j] = x;
-        nan |= x != x;
-        mx = fmaxf(mx, x);
-    }
-    if (A.score == REGOT_SIGMOID) {
-        for (int j = lane; j < A.m; j += kLanes) s[j] = sigmoid(s[j]);
-        return;
-    }
-    mx = __any(nan) ? kNan : wave_all<OpMaxF>(mx);
-    float sum = 0.f;
-    for (int j = lane; j < A.m; j += kLanes) sum += s[j] = expf(s[j] - mx);
-    sum = wave_all<OpSumF>(sum);
-    for (int j = lane; j < A.m; j += kLanes) s[j] = mx == -kInf ? 0.f : s[j] / sum;
-}
-
-template <int TYPE>
-__global__ __launch_bounds__(kLanes) void row_route_kernel(RouteArgs A)
-{
-    __shared__ float s[REGOT_ROW_MAX_EXPERTS], key[REGOT_ROW_MAX_EXPERTS], value[kMaxGroups];
-    const int64_t row = blockIdx.x;
-    const int lane = threadIdx.x;
-    const typename Score<TYPE>::Raw *S = static_cast<const typename Score<TYPE>::Raw *>(A.S) + row * A.ldS;
-    row_scores<TYPE>(A, S, lane, s);
-    bool bad = false;
-    for (int j = lane; j < A.m; j += kLanes) {
-        const float x = Score<TYPE>::get(S[j]);
-        float c = A.bias ? (A.bias_on == REGOT_BIAS_SCORE ? s[j] : x) + A.bias[j] : x;
-        if (x == -kInf) c = -kInf;
-        bad |= c != c || s[j] != s[j];
-        key[j] = c;
-    }
-    bad = __any(bad);
-    __syncthreads();
-    const int size = A.groups > 0 ? A.m / A.groups : 0;
-    if (A.groups > 1) {
-        if (lane < A.groups) {
-            float a = -kInf, b = -kInf;
-            for (int j = lane * size; j < (lane + 1) * size; ++j) {
-                if (key[j] == -kInf) continue;
-                const float c = A.bias ? key[j] : s[j];
-                b = fmaxf(b, fminf(a, c));
-                a = fmaxf(a, c);
-            }
-            value[lane] = A.group_by == REGOT_GROUP_TOP2 && b > -kInf ? a + b : a;
-        }
-        __syncthreads();
-        if (lane < A.groups) {
-            int rank = 0;
-            for (int g = 0; g < A.groups; ++g) rank += before(value[g], g, value[lane], lane);
-            if (rank >= A.groups_kept)
-                for (int j = lane * size; j < (lane + 1) * size; ++j) key[j] = -kInf;
-        }
-        __syncthreads();
-    }
-    float sum = 0.f, mine = 0.f;
-    int chosen = -1;
-    for (int i = 0; i < A.k; ++i) {
-        float bx = -kInf;
-        int bj = A.m;
-        for (int j = lane; j < A.m; j += kLanes)
-            if (before(key[j], j, bx, bj)) bx = key[j], bj = j;
-        for (int d = 1; d < kLanes; d *= 2) {
-            const float ox = __shfl_xor(bx, d);
-            const int oj = __shfl_xor(bj, d);
-            if (before(ox, oj, bx, bj)) bx = ox, bj = oj;
-        }
-        const bool is = !bad && bx > -kInf;
-        const float c = is ? s[bj] : 0.f;
-        sum += c;
-        if (lane == i) mine = c, chosen = is ? bj : -1;
-        __syncthreads();
-        if (is && lane == 0) key[bj] = -kInf;
-        __syncthreads();
-    }
-    if (lane < A.k) {
-        const float w = !A.renormalise ? mine : sum > 0.f ? mine / sum : 0.f;
-        A.idx[row * A.k + lane] = chosen;
-        A.weight[row * A.k + lane] = bad ? kNan : w * A.scale;
-    }
-}
-
-template <int TYPE>
-__global__ __launch_bounds__(kLanes) void row_route_grad_kernel(RouteArgs A)
-{
-    using T = Score<TYPE>;
-    __shared__ float s[REGOT_ROW_MAX_EXPERTS], ds[REGOT_ROW_MAX_EXPERTS];
-    const int64_t row = blockIdx.x;
-    const int lane = threadIdx.x;
-    const typename T::Raw *S = static_cast<const typename T::Raw *>(A.S) + row * A.ldS;
-    row_scores<TYPE>(A, S, lane, s);
-    for (int j = lane; j < A.m; j += kLanes) ds[j] = 0.f;
-    __syncthreads();
-    const int c = lane < A.k ? A.idx_in[row * A.k + lane] : -1;
-    const bool is = (uint32_t)c < (uint32_t)A.m;
-    const float g = is ? A.g_weight[row * A.k + lane] * A.scale : 0.f, sc = is ? s[c] : 0.f;
-    float d = g;
-    if (A.renormalise) {
-        const float Z = wave_all<OpSumF>(sc), gs = wave_all<OpSumF>(is ? g * sc : 0.f);
-        d = is && Z > 0.f ? (g - gs / Z) / Z : 0.f;
-    }
-    for (int i = 0; i < A.k; ++i) {  // (one after the other: a column may be listed twice)
-        if (lane == i && is) ds[c] += d;
-        __syncthreads();
-    }
-    const float all = A.score == REGOT_SOFTMAX ? wave_all<OpSumF>(is ? d * sc : 0.f) : 0.f;
-    const bool any = __any(is);
-    typename T::Raw *out = static_cast<typename T::Raw *>(A.dS) + row * A.ldD;
-    for (int j = lane; j < A.m; j += kLanes) {
-        const float v = A.score == REGOT_SOFTMAX ? s[j] * (ds[j] - all) : ds[j] * s[j] * (1.f - s[j]);
-        out[j] = T::put(any ? v : 0.f);
-    }
-}
 
 int element_bytes(int type) { return type == REGOT_F32 ? 4 : 2; }
 
@@ -187,13 +48,6 @@ RowArgs row_args(int64_t n, int64_t m, const void *S, int64_t ldS, const float *
     A.log2_scale = (float)(1.4426950408889634 / eta);
     return A;
 }
-
-#define REGOT_BY_TYPE(kernel, type, grid, threads, stream, args)                                              \
-    do {                                                                                                      \
-        if ((type) == REGOT_F32) hipLaunchKernelGGL((kernel<REGOT_F32>), grid, threads, 0, stream, args);     \
-        else if ((type) == REGOT_BF16) hipLaunchKernelGGL((kernel<REGOT_BF16>), grid, threads, 0, stream, args); \
-        else hipLaunchKernelGGL((kernel<REGOT_F16>), grid, threads, 0, stream, args);                         \
-    } while (0)
 
 constexpr int64_t kMaxGrid = 1 << 22;  // (rows beyond are the same workgroups')
 
@@ -373,6 +227,56 @@ void launch_logprob(const RowArgs &A, int type, const RowPlan &P, hipStream_t s)
     else launch_logprob<REGOT_F16>(A, P, s);
 }
 
+// Rows of a route by their length: 16 lanes with 4 or 16 scores each, or a wave with 16.  Loads of 16 bytes where the columns of
+// each lie in one group; otherwise, and for short rows, a score at a time.
+template <int TYPE, int LANES, int VALUES>
+void launch_route(const RouteArgs &A, hipStream_t s)
+{
+    const dim3 grid((unsigned)std::min((A.n + kThreads / LANES - 1) / (kThreads / LANES), kMaxGrid));
+    if (A.k <= 8) hipLaunchKernelGGL((row_route_kernel<TYPE, LANES, VALUES, 8>), grid, dim3(kThreads), 0, s, A);
+    else hipLaunchKernelGGL((row_route_kernel<TYPE, LANES, VALUES, REGOT_ROW_MAX_CHOICES>), grid, dim3(kThreads), 0, s, A);
+}
+
+template <int TYPE>
+void launch_route(RouteArgs &A, hipStream_t s)
+{
+    const bool wide = A.m >= Score<TYPE>::kVec && (A.groups == 1 || A.group_size % Score<TYPE>::kVec == 0);
+    const int lanes = A.m <= 256 ? 16 : kLanes;
+    A.group_lanes = (int)std::max<int64_t>(lanes / power_of_two(A.groups), 1);
+    if (A.m <= 64) launch_route<TYPE + kSingle, 16, 4>(A, s);
+    else if (A.m <= 256) wide ? launch_route<TYPE, 16, 16>(A, s) : launch_route<TYPE + kSingle, 16, 16>(A, s);
+    else wide ? launch_route<TYPE, kLanes, 16>(A, s) : launch_route<TYPE + kSingle, kLanes, 16>(A, s);
+}
+
+void launch_route(RouteArgs &A, int type, hipStream_t s)
+{
+    if (type == REGOT_F32) launch_route<REGOT_F32>(A, s);
+    else if (type == REGOT_BF16) launch_route<REGOT_BF16>(A, s);
+    else launch_route<REGOT_F16>(A, s);
+}
+
+template <int TYPE, int LANES, int VALUES>
+void launch_route_grad(const RouteArgs &A, hipStream_t s)
+{
+    const dim3 grid((unsigned)std::min((A.n + kThreads / LANES - 1) / (kThreads / LANES), kMaxGrid));
+    hipLaunchKernelGGL((row_route_grad_kernel<TYPE, LANES, VALUES>), grid, dim3(kThreads), 0, s, A);
+}
+
+template <int TYPE>
+void launch_route_grad(const RouteArgs &A, hipStream_t s)
+{
+    if (A.m <= 64) launch_route_grad<TYPE + kSingle, 16, 4>(A, s);
+    else if (A.m <= 256) launch_route_grad<TYPE, 16, 16>(A, s);
+    else launch_route_grad<TYPE, kLanes, 16>(A, s);
+}
+
+void launch_route_grad(const RouteArgs &A, int type, hipStream_t s)
+{
+    if (type == REGOT_F32) launch_route_grad<REGOT_F32>(A, s);
+    else if (type == REGOT_BF16) launch_route_grad<REGOT_BF16>(A, s);
+    else launch_route_grad<REGOT_F16>(A, s);
+}
+
 }  // namespace
 
 extern "C" {
@@ -490,15 +394,15 @@ int regot_row_route(int64_t n, int64_t m, const void *S, int type, int64_t ldS, 
     if (m > REGOT_ROW_MAX_EXPERTS) return REGOT_ERR_DIM;
     if (k < 1 || k > REGOT_ROW_MAX_CHOICES || (score != REGOT_SOFTMAX && score != REGOT_SIGMOID) ||
         (bias && bias_on != REGOT_BIAS_SCORE && bias_on != REGOT_BIAS_LOGIT) || groups < 1 || groups > kMaxGroups ||
-        groups_kept < 1 || groups_kept > groups || m % groups != 0 || (group_by != REGOT_GROUP_MAX && group_by != REGOT_GROUP_TOP2) ||
+        groups_kept < 1 || groups_kept > groups || (m % groups != 0) || (group_by != REGOT_GROUP_MAX && group_by != REGOT_GROUP_TOP2) ||
         (renormalise != 0 && renormalise != 1) || !isfinite((float)scale))
         return REGOT_ERR_ARG;
     if (n > 0 && (!idx || !weight)) return REGOT_ERR_NULL;
     if (misaligned(bias, 4) || misaligned(idx, 4) || misaligned(weight, 4)) return REGOT_ERR_ALIGN;
     if (n == 0) return REGOT_OK;
     RouteArgs A{};
-    A.n = (int)n;
-    A.m = (int)m;
+    A.n = n;
+    A.m = (uint32_t)m;
     A.S = S;
     A.ldS = ldS;
     A.bias = bias;
@@ -512,7 +416,9 @@ int regot_row_route(int64_t n, int64_t m, const void *S, int type, int64_t ldS, 
     A.scale = (float)scale;
     A.idx = idx;
     A.weight = weight;
-    REGOT_BY_TYPE(row_route_kernel, type, dim3((unsigned)n), dim3(kLanes), static_cast<hipStream_t>(stream), A);
+    A.group_size = (uint32_t)(m / groups);
+    A.group_magic = A.group_size > 1 ? (uint32_t)(((1ull << 32) + A.group_size - 1) / A.group_size) : 0;
+    launch_route(A, type, static_cast<hipStream_t>(stream));
     return hip_status();
 }
 
@@ -530,8 +436,8 @@ int regot_row_route_grad(int64_t n, int64_t m, const void *S, int type, int64_t 
     if (misaligned(idx, 4) || misaligned(g_weight, 4) || misaligned(dS, element_bytes(type))) return REGOT_ERR_ALIGN;
     if (n == 0 || m == 0) return REGOT_OK;
     RouteArgs A{};
-    A.n = (int)n;
-    A.m = (int)m;
+    A.n = n;
+    A.m = (uint32_t)m;
     A.S = S;
     A.ldS = ldS;
     A.score = score;
@@ -542,7 +448,7 @@ int regot_row_route_grad(int64_t n, int64_t m, const void *S, int type, int64_t 
     A.g_weight = g_weight;
     A.dS = dS;
     A.ldD = ldD;
-    REGOT_BY_TYPE(row_route_grad_kernel, type, dim3((unsigned)n), dim3(kLanes), static_cast<hipStream_t>(stream), A);
+    launch_route_grad(A, type, static_cast<hipStream_t>(stream));
     return hip_status();
 }
 

@@ -1,0 +1,373 @@
+// Routing of rows to k of their columns, and its gradient.
+//
+// A row is LANES lanes', which hold VALUES of its scores each; a wave has 64 / LANES rows, a workgroup four waves.  The k best
+// come out of a network without branches: each lane sorts what it has to a list of its KEPT best, and lists of
+// pairs of lanes are merged until every lane has the row's.  Keys and columns are one number, so that ties need nothing
+// of their own.  65536 rows of 256 fp32 scores: the reading is 67 MB; the network of 8 of 16 values is about 300 instructions for
+// four rows, which is what bounds it beside the exponentials.
+#pragma once
+
+#include "regot_rows.hpp"
+
+namespace regot {
+
+struct RouteArgs {
+    int64_t n;
+    uint32_t m;
+    const void *S;
+    int64_t ldS;
+    const float *bias;
+    int bias_on, score, groups, groups_kept, group_by, k, renormalise;
+    uint32_t group_size, group_magic;  // column / group_size = (column * group_magic) >> 32; 0 for groups of one column
+    int group_lanes;                   // lanes that look at one group (a power of two)
+    float scale;
+    int32_t *idx;
+    float *weight;
+    const int32_t *idx_in;
+    const float *g_weight;
+    void *dS;
+    int64_t ldD;
+};
+
+constexpr int kMaxGroups = 64;
+
+// A key and its column as a double: larger for what is chosen first, and above kNoChoice.
+__device__ __forceinline__ double choice(float key, uint32_t column)
+{
+    const uint64_t payload = (uint64_t)ordered(key + 0.f) << 16 | (0xffffu - column);
+    return __longlong_as_double((long long)(payload | 1ull << 62));
+}
+constexpr uint64_t kNoChoiceBits = 1ull << 62;
+__device__ __forceinline__ double no_choice() { return __longlong_as_double((long long)kNoChoiceBits); }
+__device__ __forceinline__ uint32_t chosen_column(double c) { return 0xffffu - ((uint32_t)__double_as_longlong(c) & 0xffffu); }
+
+// Both in order, the larger first.
+__device__ __forceinline__ void in_order(double &a, double &b)
+{
+    const double hi = fmax(a, b), lo = fmin(a, b);
+    a = hi;
+    b = lo;
+}
+
+// A sequence that rises once and falls once (either way around), into descending order.
+template <int COUNT>
+__device__ __forceinline__ void merge_down(double *a)
+{
+    if constexpr (COUNT > 1) {
+#pragma unroll
+        for (int i = 0; i < COUNT / 2; ++i) in_order(a[i], a[i + COUNT / 2]);
+        merge_down<COUNT / 2>(a);
+        merge_down<COUNT / 2>(a + COUNT / 2);
+    }
+}
+
+template <int COUNT>
+__device__ __forceinline__ void sort_down(double *a)
+{
+    if constexpr (COUNT > 1) {
+        sort_down<COUNT / 2>(a);
+        sort_down<COUNT / 2>(a + COUNT / 2);
+#pragma unroll
+        for (int i = 0; i < COUNT / 2; ++i) in_order(a[i], a[COUNT - 1 - i]);
+        merge_down<COUNT / 2>(a);
+        merge_down<COUNT / 2>(a + COUNT / 2);
+    }
+}
+
+// a: the best KEPT of a and b, both in descending order
+template <int KEPT, typename F>
+__device__ __forceinline__ void merge_lists(double (&a)[KEPT], F b)
+{
+    double c[KEPT];
+#pragma unroll
+    for (int i = 0; i < KEPT; ++i) c[i] = fmax(a[i], b(KEPT - 1 - i));
+#pragma unroll
+    for (int i = 0; i < KEPT; ++i) a[i] = c[i];
+    merge_down<KEPT>(a);
+}
+
+// over the LANES lanes of a row, in a fixed order, the result in all of them
+template <typename Op, int LANES>
+__device__ __forceinline__ float row_all(float v)
+{
+    if constexpr (LANES == kLanes) return wave_all<Op>(v);
+    v = Op::apply(v, dpp_f32<kDppXor1>(v));
+    v = Op::apply(v, dpp_f32<kDppXor2>(v));
+    v = Op::apply(v, dpp_f32<kDppHalfMirror>(v));
+    return Op::apply(v, dpp_f32<kDppMirror>(v));
+}
+
+// Where score j of a row is kept in LDS: rows of 16 apart by one, so that lanes that go through neighbouring groups do not meet.
+__device__ __forceinline__ uint32_t place(uint32_t j) { return j + (j >> 4); }
+constexpr int places(int columns) { return columns + columns / 16; }
+
+// A lane's columns of its row.
+template <int TYPE, int LANES, int VALUES>
+struct RouteRow {
+    using T = Score<TYPE>;
+    static constexpr int kChunks = VALUES / T::kVec;
+    static constexpr int kColumns = LANES * VALUES;
+    uint32_t m;
+    int l;
+    // the columns of chunk c; of value v
+    __device__ __forceinline__ Span<TYPE> span(int c) const { return Span<TYPE>((uint32_t)(c * LANES + l) * T::kVec, m); }
+    __device__ __forceinline__ uint32_t column(int v) const { return span(v / T::kVec).first + v % T::kVec; }
+
+    __device__ __forceinline__ void load(const typename T::Raw *S, float (&x)[VALUES]) const
+    {
+        if (m == 0) {
+#pragma unroll
+            for (int v = 0; v < VALUES; ++v) x[v] = -kInf;
+            return;
+        }
+        typename T::Chunk raw[kChunks];
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) raw[c] = span(c).template load<false>(S);
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) {
+            T::unpack(raw[c], x + c * T::kVec);
+            span(c).mask(x + c * T::kVec);
+        }
+    }
+
+    // softmax or sigmoid of x
+    static __device__ __forceinline__ void scores(int score, const float (&x)[VALUES], float (&s)[VALUES])
+    {
+        if (score == REGOT_SIGMOID) {
+#pragma unroll
+            for (int v = 0; v < VALUES; ++v) s[v] = __builtin_amdgcn_rcpf(1.f + exp2_fast(-x[v] * kLog2e));
+            return;
+        }
+        float top = x[0];
+#pragma unroll
+        for (int v = 1; v < VALUES; ++v) top = max_nan(top, x[v]);
+        top = row_all<OpMaxF, LANES>(top);
+        const float from = top == -kInf ? 0.f : top;
+        float sum = 0.f;
+#pragma unroll
+        for (int v = 0; v < VALUES; ++v) sum += s[v] = exp2_fast((x[v] - from) * kLog2e);
+        sum = row_all<OpSumF, LANES>(sum);
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+        for (int v = 0; v < VALUES; ++v) s[v] *= inv;
+    }
+};
+
+template <int TYPE, int LANES, int VALUES, int KEPT>
+__global__ __launch_bounds__(kThreads) void row_route_kernel(RouteArgs A)
+{
+    using T = Score<TYPE>;
+    using Row = RouteRow<TYPE, LANES, VALUES>;
+    constexpr int kRows = kThreads / LANES;
+    __shared__ float held[kRows][places(Row::kColumns)];
+    __shared__ float value[kRows][kMaxGroups];
+    __shared__ uint32_t shut[kRows][kMaxGroups];
+    const int lane = threadIdx.x & (kLanes - 1), at = threadIdx.x / LANES;
+    const Row R{A.m, (int)(threadIdx.x % LANES)};
+    for (int64_t row0 = (int64_t)blockIdx.x * kRows; row0 < A.n; row0 += (int64_t)gridDim.x * kRows) {
+        const bool there = row0 + at < A.n;
+        const int64_t row = there ? row0 + at : A.n - 1;
+        float x[VALUES], s[VALUES];
+        R.load(static_cast<const typename T::Raw *>(A.S) + row * A.ldS, x);
+        Row::scores(A.score, x, s);
+        float key[VALUES];
+        bool bad = false;
+#pragma unroll
+        for (int c = 0; c < Row::kChunks; ++c) {
+            float b[T::kVec] = {};
+            if (A.bias && A.m > 0) R.span(c).add_bias(b, A.bias);
+#pragma unroll
+            for (int e = 0; e < T::kVec; ++e) {
+                const int v = c * T::kVec + e;
+                key[v] = A.bias ? (A.bias_on == REGOT_BIAS_SCORE ? s[v] : x[v]) + b[e] : x[v];
+                if (x[v] == -kInf) key[v] = -kInf;
+                bad |= key[v] != key[v] || s[v] != s[v];
+            }
+        }
+        const uint64_t bad_lanes = __ballot(bad);
+        bad = LANES == kLanes ? bad_lanes != 0 : (bad_lanes >> (lane / LANES * LANES) & ((1ull << (LANES % kLanes)) - 1)) != 0;
+        float *const mine = held[at];
+        if (A.groups > 1 && A.m > 0) {
+            wave_lds();
+#pragma unroll
+            for (int v = 0; v < VALUES; ++v)
+                if (R.span(v / T::kVec).first + v % T::kVec >= R.span(v / T::kVec).own) mine[place(R.column(v))] = key[v] == -kInf ? -kInf : A.bias ? key[v] : s[v];
+            wave_lds();
+            // the value of each group, by group_lanes lanes
+            const int lanes = A.group_lanes, part = R.l & (lanes - 1);
+            const uint32_t each = (A.group_size + lanes - 1) / lanes;
+            for (int g = R.l / lanes; g < A.groups; g += LANES / lanes) {
+                const uint32_t from = g * A.group_size + part * each, to = min(from + each, (uint32_t)(g + 1) * A.group_size);
+                float first = -kInf, second = -kInf;
+                for (uint32_t j = from; j < to; ++j) {
+                    const float c = mine[place(j)];
+                    second = fmaxf(second, fminf(first, c));
+                    first = fmaxf(first, c);
+                }
+                for (int d = 1; d < lanes; d *= 2) {
+                    const float first_o = __shfl_xor(first, d), second_o = __shfl_xor(second, d);
+                    second = fmaxf(fmaxf(second, second_o), fminf(first, first_o));
+                    first = fmaxf(first, first_o);
+                }
+                if (part == 0) value[at][g] = A.group_by == REGOT_GROUP_TOP2 && second > -kInf ? first + second : first;
+            }
+            wave_lds();
+            for (int g = R.l; g < A.groups; g += LANES) {
+                const float v = value[at][g];
+                int better = 0;
+                for (int o = 0; o < A.groups; ++o) better += before(value[at][o], o, v, g);
+                shut[at][g] = better >= A.groups_kept;
+            }
+            wave_lds();
+#pragma unroll
+            for (int c = 0; c < Row::kChunks; ++c) {  // (a chunk lies in one group)
+                const uint32_t first = R.span(c).first;
+                if (shut[at][A.group_magic ? __umulhi(first, A.group_magic) : first]) {
+#pragma unroll
+                    for (int e = 0; e < T::kVec; ++e) key[c * T::kVec + e] = -kInf;
+                }
+            }
+            wave_lds();
+        }
+        // the scores, for those who come to know which are chosen
+#pragma unroll
+        for (int v = 0; v < VALUES; ++v)
+            if (R.span(v / T::kVec).first + v % T::kVec >= R.span(v / T::kVec).own) mine[place(R.column(v))] = s[v];
+
+        double best[KEPT];
+        {
+            constexpr int kList = VALUES < KEPT ? VALUES : KEPT;
+            double list[VALUES];
+#pragma unroll
+            for (int v = 0; v < VALUES; ++v) list[v] = key[v] > -kInf ? choice(key[v], R.column(v)) : no_choice();
+#pragma unroll
+            for (int i = 0; i < VALUES; i += kList) sort_down<kList>(list + i);
+#pragma unroll
+            for (int i = 0; i < KEPT; ++i) best[i] = i < kList ? list[i] : no_choice();
+#pragma unroll
+            for (int p = kList; p < VALUES; p += kList) merge_lists<KEPT>(best, [&](int i) { return list[p + i]; });
+        }
+        merge_lists<KEPT>(best, [&](int i) { return dpp_f64<kDppXor1>(best[i]); });
+        merge_lists<KEPT>(best, [&](int i) { return dpp_f64<kDppXor2>(best[i]); });
+        merge_lists<KEPT>(best, [&](int i) { return dpp_f64<kDppHalfMirror>(best[i]); });
+        merge_lists<KEPT>(best, [&](int i) { return dpp_f64<kDppMirror>(best[i]); });
+        if constexpr (LANES == kLanes) {
+            merge_lists<KEPT>(best, [&](int i) { return __shfl_xor(best[i], 16); });
+            merge_lists<KEPT>(best, [&](int i) { return __shfl_xor(best[i], 32); });
+        }
+        wave_lds();
+        constexpr int kRounds = (KEPT + LANES - 1) / LANES;
+        int column[kRounds];
+        float w[kRounds], sum = 0.f;
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) {
+            double c = no_choice();
+#pragma unroll
+            for (int i = r * LANES; i < KEPT && i < (r + 1) * LANES; ++i) c = R.l == i - r * LANES ? best[i] : c;
+            const bool is = !bad && r * LANES + R.l < A.k && (uint64_t)__double_as_longlong(c) != kNoChoiceBits;
+            column[r] = is ? (int)chosen_column(c) : -1;
+            w[r] = is ? mine[place((uint32_t)column[r])] : 0.f;
+            sum += w[r];
+        }
+        sum = row_all<OpSumF, LANES>(sum);
+        const float factor = !A.renormalise ? A.scale : sum > 0.f ? A.scale / sum : 0.f;
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) {
+            const int i = r * LANES + R.l;
+            if (!there || i >= A.k) continue;
+            A.idx[row * A.k + i] = column[r];
+            A.weight[row * A.k + i] = bad ? kNan : w[r] * factor;
+        }
+        wave_lds();
+    }
+}
+
+template <int TYPE, int LANES, int VALUES>
+__global__ __launch_bounds__(kThreads) void row_route_grad_kernel(RouteArgs A)
+{
+    using T = Score<TYPE>;
+    using Row = RouteRow<TYPE, LANES, VALUES>;
+    constexpr int kRows = kThreads / LANES, kRounds = (REGOT_ROW_MAX_CHOICES + LANES - 1) / LANES;
+    __shared__ float held[kRows][Row::kColumns];
+    __shared__ uint32_t listed[kRows][REGOT_ROW_MAX_CHOICES];
+    __shared__ float gradient[kRows][REGOT_ROW_MAX_CHOICES];
+    const int at = threadIdx.x / LANES;
+    const Row R{A.m, (int)(threadIdx.x % LANES)};
+    for (int64_t row0 = (int64_t)blockIdx.x * kRows; row0 < A.n; row0 += (int64_t)gridDim.x * kRows) {
+        const bool there = row0 + at < A.n;
+        const int64_t row = there ? row0 + at : A.n - 1;
+        float x[VALUES], s[VALUES];
+        R.load(static_cast<const typename T::Raw *>(A.S) + row * A.ldS, x);
+        uint32_t column[kRounds];
+        float g[kRounds];
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) {
+            const int i = r * LANES + R.l;
+            column[r] = i < A.k ? (uint32_t)A.idx_in[row * A.k + i] : 0xffffffffu;
+            g[r] = column[r] < A.m ? A.g_weight[row * A.k + i] * A.scale : 0.f;
+        }
+        Row::scores(A.score, x, s);
+        float *const mine = held[at];
+        wave_lds();
+#pragma unroll
+        for (int v = 0; v < VALUES; ++v)
+            if (R.span(v / T::kVec).first + v % T::kVec >= R.span(v / T::kVec).own) mine[R.column(v)] = s[v];
+        wave_lds();
+        float c[kRounds], Z = 0.f, gs = 0.f, any = 0.f;
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) {
+            c[r] = column[r] < A.m ? mine[column[r]] : 0.f;
+            Z += c[r];
+            gs += column[r] < A.m ? g[r] * c[r] : 0.f;
+            any += column[r] < A.m ? 1.f : 0.f;
+        }
+        any = row_all<OpSumF, LANES>(any);
+        if (A.renormalise) {
+            Z = row_all<OpSumF, LANES>(Z);
+            gs = row_all<OpSumF, LANES>(gs) / Z;
+        }
+        float all = 0.f;
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) {
+            if (A.renormalise) g[r] = column[r] < A.m && !(Z <= 0.f) ? (g[r] - gs) / Z : 0.f;
+            all += column[r] < A.m ? g[r] * c[r] : 0.f;
+        }
+        all = A.score == REGOT_SOFTMAX ? row_all<OpSumF, LANES>(all) : 0.f;
+        // each column's part, a column listed twice having the sum of its entries'
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) {
+            const int i = r * LANES + R.l;
+            if (i < A.k) listed[at][i] = column[r], gradient[at][i] = g[r];
+        }
+        wave_lds();
+#pragma unroll
+        for (int v = 0; v < VALUES; ++v)
+            if (R.span(v / T::kVec).first + v % T::kVec >= R.span(v / T::kVec).own) mine[R.column(v)] = 0.f;
+        wave_lds();
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) {
+            if (r * LANES >= A.k) continue;
+            float sum = 0.f;
+            for (int o = 0; o < A.k; ++o) sum += listed[at][o] == column[r] ? gradient[at][o] : 0.f;
+            if (column[r] < A.m) mine[column[r]] = sum;
+        }
+        wave_lds();
+        typename T::Raw *const out = static_cast<typename T::Raw *>(A.dS) + row * A.ldD;
+#pragma unroll
+        for (int ch = 0; ch < Row::kChunks; ++ch) {
+            const Span<TYPE> span = R.span(ch);
+            if (!there || span.own >= A.m) continue;
+            float d[T::kVec];
+#pragma unroll
+            for (int e = 0; e < T::kVec; ++e) {
+                const int v = ch * T::kVec + e;
+                const float ds = mine[span.first + e];
+                d[e] = any == 0.f ? 0.f : A.score == REGOT_SOFTMAX ? s[v] * (ds - all) : ds * s[v] * (1.f - s[v]);
+            }
+            span.store(out, d);
+        }
+        wave_lds();
+    }
+}
+
+}  // namespace regot
