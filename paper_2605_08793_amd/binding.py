@@ -495,7 +495,7 @@ GROUP_BY = {"max": 0, "top2": 1}
 
 
 def _scores(S: torch.Tensor, name="S"):
-    """(n, m, type, ldS, pointer) of a matrix of scores.  Its rows may lie apart (a view of some of a wider matrix's columns),
+    """(n, m, type, ldS, address) of a matrix of scores.  Its rows may lie apart (a view of some of a wider matrix's columns),
     but its columns may not, and rows may not share memory."""
     if not isinstance(S, torch.Tensor) or not S.is_cuda or S.dim() != 2 or S.dtype not in SCORE_TYPES:
         raise TypeError(f"{name} must be a 2-D float32, bfloat16 or float16 CUDA tensor")
@@ -535,6 +535,17 @@ def _same_scores(dS: torch.Tensor, S: torch.Tensor, name="dS"):
     return _scores(dS, name)[3:]
 
 
+def _row_stream(S: torch.Tensor, stream):
+    """The stream of a call on S: the given one, or the current one of S's device, which has to be the current device.  (The raw
+    handle: the object that torch.cuda.current_stream makes costs 2.7 us, as much as a small call's launch.)"""
+    if stream is not None:
+        return _stream(stream)
+    device = S.device.index
+    if device != torch._C._cuda_getDevice():
+        raise ValueError(f"S is on device {device}, which is not the current one")
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
 def regot_row_logprob_workspace_bytes(n: int, m: int, k: int) -> int:
     out = ctypes.c_size_t(0)
     _check(load().regot_row_logprob_workspace_bytes(int(n), int(m), int(k), ctypes.byref(out)), "regot_row_logprob_workspace_bytes")
@@ -556,7 +567,7 @@ def regot_row_logprob(S, target, eta, logprob, entropy, stats, top_idx, top_logp
         _list(target, n, targets, "target", torch.int32, optional=True), targets, k,
         _list(logprob, n, targets, "logprob", optional=targets == 0), _list(entropy, n, 1, "entropy", optional=True),
         _list(stats, n, 2, "stats", optional=True), _list(top_idx, n, k, "top_idx", torch.int32, optional=True),
-        _list(top_logprob, n, k, "top_logprob", optional=k == 0), *_ws(workspace), _stream(stream)), "regot_row_logprob")
+        _list(top_logprob, n, k, "top_logprob", optional=k == 0), *_ws(workspace), _row_stream(S, stream)), "regot_row_logprob")
 
 
 def regot_row_logprob_grad(S, target, eta, stats, entropy, g_logprob, g_entropy, dS, *, bias=None, stream=None) -> None:
@@ -568,7 +579,7 @@ def regot_row_logprob_grad(S, target, eta, stats, entropy, g_logprob, g_entropy,
         n, m, at, kind, ld, _list(bias, 1, m, "bias", optional=True), float(eta),
         _list(target, n, targets, "target", torch.int32, optional=True), targets, _list(stats, n, 2, "stats"),
         _list(entropy, n, 1, "entropy", optional=g_entropy is None), _list(g_logprob, n, targets, "g_logprob", optional=targets == 0),
-        _list(g_entropy, n, 1, "g_entropy", optional=True), to, ldD, _stream(stream)), "regot_row_logprob_grad")
+        _list(g_entropy, n, 1, "g_entropy", optional=True), to, ldD, _row_stream(S, stream)), "regot_row_logprob_grad")
 
 
 def regot_row_distill(S, t_idx, t_score, eta, loss, dS=None, *, row_weight=None, workspace, stream=None) -> None:
@@ -579,7 +590,7 @@ def regot_row_distill(S, t_idx, t_score, eta, loss, dS=None, *, row_weight=None,
     _check(load().regot_row_distill(
         n, m, at, kind, ld, float(eta), _list(t_idx, n, k, "t_idx", torch.int32), _list(t_score, n, k, "t_score"), k,
         _list(row_weight, n, 1, "row_weight", optional=True), _list(loss, n, 1, "loss"), to, ldD, *_ws(workspace),
-        _stream(stream)), "regot_row_distill")
+        _row_stream(S, stream)), "regot_row_distill")
 
 
 def regot_row_route(S, idx, weight, *, bias=None, bias_on="score", score="softmax", groups=1, groups_kept=1, group_by="max",
@@ -590,7 +601,7 @@ def regot_row_route(S, idx, weight, *, bias=None, bias_on="score", score="softma
     _check(load().regot_row_route(
         n, m, at, kind, ld, _list(bias, 1, m, "bias", optional=True), BIAS_ON[bias_on], SCORE_KINDS[score], int(groups),
         int(groups_kept), GROUP_BY[group_by], k, int(bool(renormalise)), float(scale), _list(idx, n, k, "idx", torch.int32),
-        _list(weight, n, k, "weight"), _stream(stream)), "regot_row_route")
+        _list(weight, n, k, "weight"), _row_stream(S, stream)), "regot_row_route")
 
 
 def regot_row_route_grad(S, idx, g_weight, dS, *, score="softmax", renormalise=True, scale=1.0, stream=None) -> None:
@@ -599,7 +610,7 @@ def regot_row_route_grad(S, idx, g_weight, dS, *, score="softmax", renormalise=T
     ldD, to = _same_scores(dS, S)
     _check(load().regot_row_route_grad(
         n, m, at, kind, ld, SCORE_KINDS[score], _list(idx, n, k, "idx", torch.int32), k, int(bool(renormalise)), float(scale),
-        _list(g_weight, n, k, "g_weight"), to, ldD, _stream(stream)), "regot_row_route_grad")
+        _list(g_weight, n, k, "g_weight"), to, ldD, _row_stream(S, stream)), "regot_row_route_grad")
 
 
 def regot_profile_stage1(start_event, stop_event) -> None:

@@ -182,7 +182,6 @@ constexpr int kCUs = 256;
 template <int TYPE>
 void launch_distill(const RowArgs &A, hipStream_t s)
 {
-    constexpr uint32_t kLoad = kLanes * Score<TYPE>::kVec;
     const auto grid = [](int64_t blocks) { return dim3((unsigned)std::min(blocks, kMaxGrid)); };
     // Teams of more waves hold more of a row between its two reads (the last stretch in registers, the one before in LDS) and
     // make less of the traffic; of fewer, they keep more rows under way.  us: 16384 x 1000 bf16 1 wave 29, 4 waves 64; 4096 x 10000 4 waves
@@ -227,13 +226,16 @@ void launch_logprob(const RowArgs &A, int type, const RowPlan &P, hipStream_t s)
     else launch_logprob<REGOT_F16>(A, P, s);
 }
 
-// Rows of a route by their length: 16 lanes with 4 or 16 scores each, or a wave with 16.  Loads of 16 bytes where the columns of
+// Rows of a route by their length: 16 lanes with 4, 8 or 16 scores each, or a wave with 16 (65536 x 128 bf16, 6 choices: 16 lanes with 16 scores
+// each 28 us, with 8 19 us).  Loads of 16 bytes where the columns of
 // each lie in one group; otherwise, and for short rows, a score at a time.
 template <int TYPE, int LANES, int VALUES>
 void launch_route(const RouteArgs &A, hipStream_t s)
 {
     const dim3 grid((unsigned)std::min((A.n + kThreads / LANES - 1) / (kThreads / LANES), kMaxGrid));
-    if (A.k <= 8) hipLaunchKernelGGL((row_route_kernel<TYPE, LANES, VALUES, 8>), grid, dim3(kThreads), 0, s, A);
+    if (A.k <= 4) hipLaunchKernelGGL((row_route_kernel<TYPE, LANES, VALUES, 4>), grid, dim3(kThreads), 0, s, A);
+    else if (A.k <= 8) hipLaunchKernelGGL((row_route_kernel<TYPE, LANES, VALUES, 8>), grid, dim3(kThreads), 0, s, A);
+    else if (A.k <= 16) hipLaunchKernelGGL((row_route_kernel<TYPE, LANES, VALUES, 16>), grid, dim3(kThreads), 0, s, A);
     else hipLaunchKernelGGL((row_route_kernel<TYPE, LANES, VALUES, REGOT_ROW_MAX_CHOICES>), grid, dim3(kThreads), 0, s, A);
 }
 
@@ -244,6 +246,7 @@ void launch_route(RouteArgs &A, hipStream_t s)
     const int lanes = A.m <= 256 ? 16 : kLanes;
     A.group_lanes = (int)std::max<int64_t>(lanes / power_of_two(A.groups), 1);
     if (A.m <= 64) launch_route<TYPE + kSingle, 16, 4>(A, s);
+    else if (A.m <= 128 && wide) launch_route<TYPE, 16, 8>(A, s);
     else if (A.m <= 256) wide ? launch_route<TYPE, 16, 16>(A, s) : launch_route<TYPE + kSingle, 16, 16>(A, s);
     else wide ? launch_route<TYPE, kLanes, 16>(A, s) : launch_route<TYPE + kSingle, kLanes, 16>(A, s);
 }
@@ -266,6 +269,7 @@ template <int TYPE>
 void launch_route_grad(const RouteArgs &A, hipStream_t s)
 {
     if (A.m <= 64) launch_route_grad<TYPE + kSingle, 16, 4>(A, s);
+    else if (A.m <= 128) launch_route_grad<TYPE, 16, 8>(A, s);
     else if (A.m <= 256) launch_route_grad<TYPE, 16, 16>(A, s);
     else launch_route_grad<TYPE, kLanes, 16>(A, s);
 }

@@ -426,10 +426,10 @@ __global__ __launch_bounds__(kThreads) void row_logprob_narrow_kernel(RowArgs A)
             // as in best_columns, with two maxima a lane for the bound, and (load, lane) for (block, thread)
             int count = 0;
             if (!out.bad && !out.none) {
-                float half[VECS == 1 ? 1 : 2];
-                half[0] = top[0];
+                constexpr int kHalves = VECS == 1 ? 1 : 2;
+                float half[kHalves];
 #pragma unroll
-                for (int u = 1; u < VECS; ++u) half[u & 1] = u == 1 ? top[1] : max_nan(half[u & 1], top[u]);
+                for (int u = 0; u < VECS; ++u) half[u % kHalves] = u < kHalves ? top[u] : max_nan(half[u % kHalves], top[u]);
                 const float bound = kth_largest_bound(half, A.k);
                 int pairs = 0;
                 wave_lds();

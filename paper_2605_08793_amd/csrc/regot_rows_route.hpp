@@ -130,26 +130,38 @@ struct RouteRow {
         }
     }
 
-    // softmax or sigmoid of x
-    static __device__ __forceinline__ void scores(int score, const float (&x)[VALUES], float (&s)[VALUES])
+};
+
+// What makes a row's scores of its logits: e^(x - from) / sum, or 1 / (1 + e^-x).  Which one it is is looked at once for all
+// values (a choice for each value made half of the kernel's instructions branches).
+struct RouteScore {
+    bool sigmoid;
+    float from = 0.f, inv = 1.f;
+    template <int LANES, int VALUES>
+    __device__ __forceinline__ void of_row(const float (&x)[VALUES])
     {
-        if (score == REGOT_SIGMOID) {
-#pragma unroll
-            for (int v = 0; v < VALUES; ++v) s[v] = __builtin_amdgcn_rcpf(1.f + exp2_fast(-x[v] * kLog2e));
-            return;
-        }
+        if (sigmoid) return;
         float top = x[0];
 #pragma unroll
         for (int v = 1; v < VALUES; ++v) top = max_nan(top, x[v]);
         top = row_all<OpMaxF, LANES>(top);
-        const float from = top == -kInf ? 0.f : top;
+        from = top == -kInf ? 0.f : top;
         float sum = 0.f;
 #pragma unroll
-        for (int v = 0; v < VALUES; ++v) sum += s[v] = exp2_fast((x[v] - from) * kLog2e);
+        for (int v = 0; v < VALUES; ++v) sum += exp2_fast((x[v] - from) * kLog2e);
         sum = row_all<OpSumF, LANES>(sum);
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        inv = sum == 0.f ? 0.f : 1.f / sum;
+    }
+    template <int VALUES>
+    __device__ __forceinline__ void operator()(const float (&x)[VALUES], float (&s)[VALUES]) const
+    {
+        if (sigmoid) {
 #pragma unroll
-        for (int v = 0; v < VALUES; ++v) s[v] *= inv;
+            for (int v = 0; v < VALUES; ++v) s[v] = __builtin_amdgcn_rcpf(1.f + exp2_fast(-x[v] * kLog2e));
+        } else {
+#pragma unroll
+            for (int v = 0; v < VALUES; ++v) s[v] = exp2_fast((x[v] - from) * kLog2e) * inv;
+        }
     }
 };
 
@@ -167,31 +179,50 @@ __global__ __launch_bounds__(kThreads) void row_route_kernel(RouteArgs A)
     for (int64_t row0 = (int64_t)blockIdx.x * kRows; row0 < A.n; row0 += (int64_t)gridDim.x * kRows) {
         const bool there = row0 + at < A.n;
         const int64_t row = there ? row0 + at : A.n - 1;
-        float x[VALUES], s[VALUES];
-        R.load(static_cast<const typename T::Raw *>(A.S) + row * A.ldS, x);
-        Row::scores(A.score, x, s);
-        float key[VALUES];
+        const typename T::Raw *const S = static_cast<const typename T::Raw *>(A.S) + row * A.ldS;
+        float x[VALUES], key[VALUES];
+        R.load(S, x);
+        RouteScore score{A.score == REGOT_SIGMOID};
+        score.template of_row<LANES>(x);
+        // (the score itself is part of some keys only: it is formed again for what is chosen)
+        const bool keys_of_scores = A.bias && A.bias_on == REGOT_BIAS_SCORE;
+        float s[VALUES];
+        if (keys_of_scores || (!A.bias && A.groups > 1)) score(x, s);
         bool bad = false;
+        if (keys_of_scores) {
 #pragma unroll
-        for (int c = 0; c < Row::kChunks; ++c) {
-            float b[T::kVec] = {};
-            if (A.bias && A.m > 0) R.span(c).add_bias(b, A.bias);
+            for (int v = 0; v < VALUES; ++v) key[v] = s[v];
+        } else {
 #pragma unroll
-            for (int e = 0; e < T::kVec; ++e) {
-                const int v = c * T::kVec + e;
-                key[v] = A.bias ? (A.bias_on == REGOT_BIAS_SCORE ? s[v] : x[v]) + b[e] : x[v];
-                if (x[v] == -kInf) key[v] = -kInf;
-                bad |= key[v] != key[v] || s[v] != s[v];
-            }
+            for (int v = 0; v < VALUES; ++v) key[v] = x[v];
         }
+        if (A.bias && A.m > 0) {
+#pragma unroll
+            for (int c = 0; c < Row::kChunks; ++c) R.span(c).add_bias(key + c * T::kVec, A.bias);
+        }
+#pragma unroll
+        for (int v = 0; v < VALUES; ++v) {
+            key[v] = x[v] == -kInf ? -kInf : key[v];
+            bad |= key[v] != key[v];
+        }
+        bad |= score.inv != score.inv;
         const uint64_t bad_lanes = __ballot(bad);
         bad = LANES == kLanes ? bad_lanes != 0 : (bad_lanes >> (lane / LANES * LANES) & ((1ull << (LANES % kLanes)) - 1)) != 0;
         float *const mine = held[at];
         if (A.groups > 1 && A.m > 0) {
             wave_lds();
+            if (A.bias) {
 #pragma unroll
-            for (int v = 0; v < VALUES; ++v)
-                if (R.span(v / T::kVec).first + v % T::kVec >= R.span(v / T::kVec).own) mine[place(R.column(v))] = key[v] == -kInf ? -kInf : A.bias ? key[v] : s[v];
+                for (int v = 0; v < VALUES; ++v) s[v] = key[v];
+            }
+#pragma unroll
+            for (int c = 0; c < Row::kChunks; ++c) {
+                const Span<TYPE> span = R.span(c);
+                const bool whole = span.first == span.own;
+#pragma unroll
+                for (int e = 0; e < T::kVec; ++e)
+                    if (whole || span.first + e >= span.own) mine[place(span.first + e)] = key[c * T::kVec + e] == -kInf ? -kInf : s[c * T::kVec + e];
+            }
             wave_lds();
             // the value of each group, by group_lanes lanes
             const int lanes = A.group_lanes, part = R.l & (lanes - 1);
@@ -229,11 +260,6 @@ __global__ __launch_bounds__(kThreads) void row_route_kernel(RouteArgs A)
             }
             wave_lds();
         }
-        // the scores, for those who come to know which are chosen
-#pragma unroll
-        for (int v = 0; v < VALUES; ++v)
-            if (R.span(v / T::kVec).first + v % T::kVec >= R.span(v / T::kVec).own) mine[place(R.column(v))] = s[v];
-
         double best[KEPT];
         {
             constexpr int kList = VALUES < KEPT ? VALUES : KEPT;
@@ -255,10 +281,9 @@ __global__ __launch_bounds__(kThreads) void row_route_kernel(RouteArgs A)
             merge_lists<KEPT>(best, [&](int i) { return __shfl_xor(best[i], 16); });
             merge_lists<KEPT>(best, [&](int i) { return __shfl_xor(best[i], 32); });
         }
-        wave_lds();
         constexpr int kRounds = (KEPT + LANES - 1) / LANES;
         int column[kRounds];
-        float w[kRounds], sum = 0.f;
+        float w[kRounds], at_chosen[kRounds], sum = 0.f;
 #pragma unroll
         for (int r = 0; r < kRounds; ++r) {
             double c = no_choice();
@@ -266,9 +291,11 @@ __global__ __launch_bounds__(kThreads) void row_route_kernel(RouteArgs A)
             for (int i = r * LANES; i < KEPT && i < (r + 1) * LANES; ++i) c = R.l == i - r * LANES ? best[i] : c;
             const bool is = !bad && r * LANES + R.l < A.k && (uint64_t)__double_as_longlong(c) != kNoChoiceBits;
             column[r] = is ? (int)chosen_column(c) : -1;
-            w[r] = is ? mine[place((uint32_t)column[r])] : 0.f;
-            sum += w[r];
+            at_chosen[r] = is ? T::get(S[column[r]]) : 0.f;
         }
+        score(at_chosen, w);
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) sum += w[r] = column[r] < 0 ? 0.f : w[r];
         sum = row_all<OpSumF, LANES>(sum);
         const float factor = !A.renormalise ? A.scale : sum > 0.f ? A.scale / sum : 0.f;
 #pragma unroll
@@ -278,7 +305,6 @@ __global__ __launch_bounds__(kThreads) void row_route_kernel(RouteArgs A)
             A.idx[row * A.k + i] = column[r];
             A.weight[row * A.k + i] = bad ? kNan : w[r] * factor;
         }
-        wave_lds();
     }
 }
 
@@ -296,8 +322,9 @@ __global__ __launch_bounds__(kThreads) void row_route_grad_kernel(RouteArgs A)
     for (int64_t row0 = (int64_t)blockIdx.x * kRows; row0 < A.n; row0 += (int64_t)gridDim.x * kRows) {
         const bool there = row0 + at < A.n;
         const int64_t row = there ? row0 + at : A.n - 1;
-        float x[VALUES], s[VALUES];
-        R.load(static_cast<const typename T::Raw *>(A.S) + row * A.ldS, x);
+        const typename T::Raw *const S = static_cast<const typename T::Raw *>(A.S) + row * A.ldS;
+        float x[VALUES];
+        R.load(S, x);
         uint32_t column[kRounds];
         float g[kRounds];
 #pragma unroll
@@ -306,17 +333,18 @@ __global__ __launch_bounds__(kThreads) void row_route_grad_kernel(RouteArgs A)
             column[r] = i < A.k ? (uint32_t)A.idx_in[row * A.k + i] : 0xffffffffu;
             g[r] = column[r] < A.m ? A.g_weight[row * A.k + i] * A.scale : 0.f;
         }
-        Row::scores(A.score, x, s);
-        float *const mine = held[at];
-        wave_lds();
+        float at_listed[kRounds];
 #pragma unroll
-        for (int v = 0; v < VALUES; ++v)
-            if (R.span(v / T::kVec).first + v % T::kVec >= R.span(v / T::kVec).own) mine[R.column(v)] = s[v];
-        wave_lds();
-        float c[kRounds], Z = 0.f, gs = 0.f, any = 0.f;
+        for (int r = 0; r < kRounds; ++r) at_listed[r] = column[r] < A.m ? T::get(S[column[r]]) : 0.f;
+        RouteScore score{A.score == REGOT_SIGMOID};
+        score.template of_row<LANES>(x);
+        float *const mine = held[at];
+        float c[kRounds], s[VALUES], Z = 0.f, gs = 0.f, any = 0.f;
+        score(at_listed, c);
+        score(x, s);
 #pragma unroll
         for (int r = 0; r < kRounds; ++r) {
-            c[r] = column[r] < A.m ? mine[column[r]] : 0.f;
+            c[r] = column[r] < A.m ? c[r] : 0.f;
             Z += c[r];
             gs += column[r] < A.m ? g[r] * c[r] : 0.f;
             any += column[r] < A.m ? 1.f : 0.f;
@@ -341,8 +369,7 @@ __global__ __launch_bounds__(kThreads) void row_route_grad_kernel(RouteArgs A)
         }
         wave_lds();
 #pragma unroll
-        for (int v = 0; v < VALUES; ++v)
-            if (R.span(v / T::kVec).first + v % T::kVec >= R.span(v / T::kVec).own) mine[R.column(v)] = 0.f;
+        for (int v = 0; v < VALUES; ++v) mine[v * LANES + R.l] = 0.f;
         wave_lds();
 #pragma unroll
         for (int r = 0; r < kRounds; ++r) {
@@ -353,6 +380,7 @@ __global__ __launch_bounds__(kThreads) void row_route_grad_kernel(RouteArgs A)
         }
         wave_lds();
         typename T::Raw *const out = static_cast<typename T::Raw *>(A.dS) + row * A.ldD;
+        const bool sigmoid = score.sigmoid;
 #pragma unroll
         for (int ch = 0; ch < Row::kChunks; ++ch) {
             const Span<TYPE> span = R.span(ch);
@@ -360,9 +388,12 @@ __global__ __launch_bounds__(kThreads) void row_route_grad_kernel(RouteArgs A)
             float d[T::kVec];
 #pragma unroll
             for (int e = 0; e < T::kVec; ++e) {
-                const int v = ch * T::kVec + e;
-                const float ds = mine[span.first + e];
-                d[e] = any == 0.f ? 0.f : A.score == REGOT_SOFTMAX ? s[v] * (ds - all) : ds * s[v] * (1.f - s[v]);
+                const float p = s[ch * T::kVec + e];
+                d[e] = p * (mine[span.first + e] * (sigmoid ? 1.f - p : 1.f) - all);  // (all: 0 for sigmoid)
+            }
+            if (any == 0.f) {
+#pragma unroll
+                for (int e = 0; e < T::kVec; ++e) d[e] = 0.f;
             }
             span.store(out, d);
         }
