@@ -1,0 +1,110 @@
+"""The row operators as they are used: with the solver's duals, in a captured step, and the example that runs them together."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2605_08793_amd import balanced
+from paper_2605_08793_amd.driver import DualPass
+from paper_2605_08793_amd.rows import RowDistill, RowLogprob, RowRoute
+
+pytestmark = pytest.mark.gpu
+
+
+def test_example_student_learns_balanced_targets():
+    s = balanced.train_student()
+    assert np.isfinite(s["loss"]).all()
+    assert s["loss"][-1] < 0.7 * s["loss"][0]
+    assert s["most_balanced"] < 0.5 * s["most_plain"]
+
+
+def test_example_router_is_balanced_and_sorted():
+    r = balanced.route_tokens()
+    assert r["load_balanced"] < 0.6 * r["load_plain"]
+    n, k = r["idx"].shape
+    start, tokens, idx = r["start"].cpu().numpy(), r["tokens"].cpu().numpy(), r["idx"].cpu().numpy()
+    assert start[-1] == n * k
+    for e in range(len(start) - 1):
+        np.testing.assert_array_equal(tokens[start[e]:start[e + 1]], np.flatnonzero((idx == e).any(1)))
+    assert torch.allclose(r["weight"].sum(1), torch.ones(n, device="cuda"), atol=1e-6)
+    # renormalised weights add up to 1 whatever the scores: the gradient of their sum vanishes
+    assert float(r["grad"].abs().max()) < 1e-6
+
+
+def test_rows_of_the_plan():
+    """p with the duals as bias is the plan's row over its sum: what the dense call gives at the same point."""
+    n, m, eta = 300, 700, 0.05
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    S = -torch.rand(n, m, generator=gen, device="cuda")
+    M = (-S).double()
+    a, b = (torch.full((c,), 1.0 / c, dtype=torch.float64, device="cuda") for c in (n, m))
+    dp = DualPass(n, m, capacity=n * m)
+    alpha, beta = dp.sinkhorn_sweeps(M, a, b, eta, 4)
+    beta = beta.float().double()  # (the duals as the row operator takes them)
+    dp.dual_eval_sparsify(M, a, b, alpha, beta, eta, 0.0)
+    rows = RowLogprob(n, m, k=8, targets=1, dtype=torch.float32)
+    target = torch.arange(n, dtype=torch.int32, device="cuda")[:, None] % m
+    rows.logprob(S, target, eta=eta, bias=beta.float())
+    plan = dp.val.view(n, m) / dp.row_sum[:, None]
+    want = plan.gather(1, target.long()).log()
+    # 32 bits: x / eta is off by 2^-24 |x| / eta, |x| < 1.5 here, and log p by a few times that
+    assert torch.allclose(rows.logprob_out.double(), want, atol=10 * 2.0 ** -24 * 1.5 / eta, rtol=0)
+    best = plan.gather(1, rows.top_idx.long())
+    assert torch.allclose(best, plan.topk(8, dim=1).values, rtol=20 * 2.0 ** -24 * 1.5 / eta)
+
+
+def test_captured_step_replays_like_eager():
+    n, m, k = 70, 60000, 9     # rows in parts: two launches and a workspace between them
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    S = torch.empty(n, m, dtype=torch.bfloat16, device="cuda")
+    R = torch.empty(n, 96, device="cuda")
+    target = torch.zeros(n, 1, dtype=torch.int32, device="cuda")
+    g = torch.ones(n, 1, device="cuda")
+    ask, learn, route = RowLogprob(n, m, k=k), RowDistill(n, m, k), RowRoute(n, 96, 4, score="sigmoid")
+    ask.dS = torch.empty_like(S)
+
+    def step():
+        ask.logprob(S, target)
+        learn.distill(S, ask.top_idx, ask.top_logprob, eta=2.0)
+        ask.grad(S, target, g, g[:, 0])
+        route.route(R)
+        route.grad(R, route.weight)
+
+    def results():
+        torch.cuda.synchronize()
+        return [t.clone() for t in (ask.logprob_out, ask.entropy, ask.stats, ask.top_idx, ask.top_logprob, ask.dS, learn.loss, learn.grad,
+                                    route.idx, route.weight, route.dS)]
+
+    S.normal_(generator=gen)
+    R.normal_(generator=gen)
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for replay in range(4):
+        S.normal_(generator=gen)
+        R.normal_(generator=gen)
+        target.random_(0, m, generator=gen)
+        step()
+        eager = results()
+        for t in (ask.logprob_out, ask.entropy, ask.stats, ask.top_logprob, ask.dS, learn.loss, learn.grad, route.weight, route.dS):
+            t.fill_(float("nan"))
+        torch.cuda.synchronize()
+        graph.replay()
+        for i, (x, y) in enumerate(zip(eager, results())):
+            assert torch.equal(x, y), (replay, i)
+
+
+def test_wrong_sizes_are_refused():
+    op = RowLogprob(4, 100, k=3, dtype=torch.float32)
+    target = torch.zeros(4, 1, dtype=torch.int32, device="cuda")
+    S = torch.zeros(4, 100, device="cuda")
+    for args in ((S[:3], target), (S.double(), target), (S, target.long()), (S.t(), target), (S, target[:2])):
+        with pytest.raises(TypeError):
+            op.logprob(*args)
+    with pytest.raises(TypeError):
+        op.logprob(S, target, bias=torch.zeros(99, device="cuda"))
+    with pytest.raises(TypeError):
+        RowDistill(4, 100, 3, dtype=torch.bfloat16).distill(S, torch.zeros(4, 3, dtype=torch.int32, device="cuda"), torch.zeros(4, 3, device="cuda"))
+    with pytest.raises(TypeError):
+        RowRoute(4, 100, 3).route(S, bias=torch.zeros(100, dtype=torch.float64, device="cuda"))
