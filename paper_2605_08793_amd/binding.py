@@ -540,7 +540,7 @@ def _row_stream(S: torch.Tensor, stream):
     handle: the object that torch.cuda.current_stream makes costs 2.7 us, as much as a small call's launch.)"""
     if stream is not None:
         return _stream(stream)
-    device = S.device.index
+    device = S.get_device()
     if device != torch._C._cuda_getDevice():
         raise ValueError(f"S is on device {device}, which is not the current one")
     return torch._C._cuda_getCurrentRawStream(device)
