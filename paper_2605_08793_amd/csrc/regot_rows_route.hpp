@@ -31,20 +31,36 @@ struct RouteArgs {
 
 constexpr int kMaxGroups = 64;
 
-// A key and its column as a double: larger for what is chosen first, and above kNoChoice.
+// A key and its column as a double, larger for what is chosen first: 48 bits, the key's 32 in the order of numbers above the
+// column's complement, below a fixed exponent.  -inf comes below all other keys, and no_choice() below that.
 __device__ __forceinline__ double choice(float key, uint32_t column)
 {
-    const uint64_t payload = (uint64_t)ordered(key + 0.f) << 16 | (0xffffu - column);
-    return __longlong_as_double((long long)(payload | 1ull << 62));
+    const uint32_t o = ordered(key + 0.f);
+    return __hiloint2double((int)__builtin_amdgcn_alignbit(0x4000u, o, 16), (int)(o << 16 | (0xffffu - column)));
 }
-constexpr uint64_t kNoChoiceBits = 1ull << 62;
-__device__ __forceinline__ double no_choice() { return __longlong_as_double((long long)kNoChoiceBits); }
-__device__ __forceinline__ uint32_t chosen_column(double c) { return 0xffffu - ((uint32_t)__double_as_longlong(c) & 0xffffu); }
+__device__ __forceinline__ double no_choice() { return __hiloint2double(0x40000000, 0); }
+__device__ __forceinline__ bool is_choice(double c) { return (uint32_t)__double2hiint(c) > 0x4000007fu; }  // (-inf: 0x4000007f)
+__device__ __forceinline__ uint32_t chosen_column(double c) { return 0xffffu - ((uint32_t)__double2loint(c) & 0xffffu); }
+
+// The larger and the smaller of two such numbers.  (Written out because fmax first makes each operand a proper number, which
+// they are: a fourth more instructions in the network.)
+__device__ __forceinline__ double larger(double a, double b)
+{
+    double r;
+    asm("v_max_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+__device__ __forceinline__ double smaller(double a, double b)
+{
+    double r;
+    asm("v_min_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
 
 // Both in order, the larger first.
 __device__ __forceinline__ void in_order(double &a, double &b)
 {
-    const double hi = fmax(a, b), lo = fmin(a, b);
+    const double hi = larger(a, b), lo = smaller(a, b);
     a = hi;
     b = lo;
 }
@@ -80,7 +96,7 @@ __device__ __forceinline__ void merge_lists(double (&a)[KEPT], F b)
 {
     double c[KEPT];
 #pragma unroll
-    for (int i = 0; i < KEPT; ++i) c[i] = fmax(a[i], b(KEPT - 1 - i));
+    for (int i = 0; i < KEPT; ++i) c[i] = larger(a[i], b(KEPT - 1 - i));
 #pragma unroll
     for (int i = 0; i < KEPT; ++i) a[i] = c[i];
     merge_down<KEPT>(a);
@@ -97,9 +113,12 @@ __device__ __forceinline__ float row_all(float v)
     return Op::apply(v, dpp_f32<kDppMirror>(v));
 }
 
-// Where score j of a row is kept in LDS: rows of 16 apart by one, so that lanes that go through neighbouring groups do not meet.
-__device__ __forceinline__ uint32_t place(uint32_t j) { return j + (j >> 4); }
-constexpr int places(int columns) { return columns + columns / 16; }
+// Where column j of a row is kept in LDS: rows of 16 apart by four more, so that lanes that go through neighbouring groups do not
+// meet, and 16 bytes stay together.
+__device__ __forceinline__ uint32_t place(uint32_t j) { return j + (j >> 4) * 4; }
+constexpr int places(int columns) { return columns + columns / 4; }
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // A lane's columns of its row.
 template <int TYPE, int LANES, int VALUES>
@@ -124,9 +143,10 @@ struct RouteRow {
 #pragma unroll
         for (int c = 0; c < kChunks; ++c) raw[c] = span(c).template load<false>(S);
 #pragma unroll
-        for (int c = 0; c < kChunks; ++c) {
-            T::unpack(raw[c], x + c * T::kVec);
-            span(c).mask(x + c * T::kVec);
+        for (int c = 0; c < kChunks; ++c) T::unpack(raw[c], x + c * T::kVec);
+        if (m < kColumns) {
+#pragma unroll
+            for (int c = 0; c < kChunks; ++c) span(c).mask(x + c * T::kVec);
         }
     }
 
@@ -137,20 +157,23 @@ struct RouteRow {
 struct RouteScore {
     bool sigmoid;
     float from = 0.f, inv = 1.f;
+    // from a row's logits; their scores in s
     template <int LANES, int VALUES>
-    __device__ __forceinline__ void of_row(const float (&x)[VALUES])
+    __device__ __forceinline__ void of_row(const float (&x)[VALUES], float (&s)[VALUES])
     {
-        if (sigmoid) return;
-        float top = x[0];
-#pragma unroll
-        for (int v = 1; v < VALUES; ++v) top = max_nan(top, x[v]);
-        top = row_all<OpMaxF, LANES>(top);
+        if (sigmoid) {
+            (*this)(x, s);
+            return;
+        }
+        const float top = row_all<OpMaxF, LANES>(largest(x));
         from = top == -kInf ? 0.f : top;
         float sum = 0.f;
 #pragma unroll
-        for (int v = 0; v < VALUES; ++v) sum += exp2_fast((x[v] - from) * kLog2e);
+        for (int v = 0; v < VALUES; ++v) sum += s[v] = exp2_fast((x[v] - from) * kLog2e);
         sum = row_all<OpSumF, LANES>(sum);
         inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+        for (int v = 0; v < VALUES; ++v) s[v] *= inv;
     }
     template <int VALUES>
     __device__ __forceinline__ void operator()(const float (&x)[VALUES], float (&s)[VALUES]) const
@@ -171,7 +194,7 @@ __global__ __launch_bounds__(kThreads) void row_route_kernel(RouteArgs A)
     using T = Score<TYPE>;
     using Row = RouteRow<TYPE, LANES, VALUES>;
     constexpr int kRows = kThreads / LANES;
-    __shared__ float held[kRows][places(Row::kColumns)];
+    __shared__ __align__(16) float held[kRows][places(Row::kColumns)];
     __shared__ float value[kRows][kMaxGroups];
     __shared__ uint32_t shut[kRows][kMaxGroups];
     const int lane = threadIdx.x & (kLanes - 1), at = threadIdx.x / LANES;
@@ -183,45 +206,54 @@ __global__ __launch_bounds__(kThreads) void row_route_kernel(RouteArgs A)
         float x[VALUES], key[VALUES];
         R.load(S, x);
         RouteScore score{A.score == REGOT_SIGMOID};
-        score.template of_row<LANES>(x);
-        // (the score itself is part of some keys only: it is formed again for what is chosen)
-        const bool keys_of_scores = A.bias && A.bias_on == REGOT_BIAS_SCORE;
         float s[VALUES];
-        if (keys_of_scores || (!A.bias && A.groups > 1)) score(x, s);
-        bool bad = false;
-        if (keys_of_scores) {
+        score.template of_row<LANES>(x, s);
+        if (A.bias) {
+            if (A.bias_on == REGOT_BIAS_SCORE) {
 #pragma unroll
-            for (int v = 0; v < VALUES; ++v) key[v] = s[v];
+                for (int v = 0; v < VALUES; ++v) key[v] = s[v];
+            } else {
+#pragma unroll
+                for (int v = 0; v < VALUES; ++v) key[v] = x[v];
+            }
+            if (A.m > 0) {
+#pragma unroll
+                for (int c = 0; c < Row::kChunks; ++c) R.span(c).add_bias(key + c * T::kVec, A.bias);
+            }
+#pragma unroll
+            for (int v = 0; v < VALUES; ++v) key[v] = x[v] == -kInf ? -kInf : key[v];
         } else {
 #pragma unroll
             for (int v = 0; v < VALUES; ++v) key[v] = x[v];
         }
-        if (A.bias && A.m > 0) {
-#pragma unroll
-            for (int c = 0; c < Row::kChunks; ++c) R.span(c).add_bias(key + c * T::kVec, A.bias);
-        }
-#pragma unroll
-        for (int v = 0; v < VALUES; ++v) {
-            key[v] = x[v] == -kInf ? -kInf : key[v];
-            bad |= key[v] != key[v];
-        }
+        const float any_nan = largest(key);
+        bool bad = any_nan != any_nan;
         bad |= score.inv != score.inv;
         const uint64_t bad_lanes = __ballot(bad);
         bad = LANES == kLanes ? bad_lanes != 0 : (bad_lanes >> (lane / LANES * LANES) & ((1ull << (LANES % kLanes)) - 1)) != 0;
         float *const mine = held[at];
         if (A.groups > 1 && A.m > 0) {
             wave_lds();
-            if (A.bias) {
+            // (without a bias, what groups are valued by is the score, but for forbidden columns)
 #pragma unroll
-                for (int v = 0; v < VALUES; ++v) s[v] = key[v];
-            }
+            for (int v = 0; v < VALUES; ++v) s[v] = A.bias || key[v] == -kInf ? key[v] : s[v];
 #pragma unroll
             for (int c = 0; c < Row::kChunks; ++c) {
                 const Span<TYPE> span = R.span(c);
-                const bool whole = span.first == span.own;
+                float *const to = mine + place(span.first);
+                if constexpr (T::kVec > 1) {
+                    if (span.first == span.own && span.first % 4 == 0) {
+#pragma unroll
+                        for (int e = 0; e < T::kVec; e += 4) {
+                            const f32x4 four = {s[c * T::kVec + e], s[c * T::kVec + e + 1], s[c * T::kVec + e + 2], s[c * T::kVec + e + 3]};
+                            *reinterpret_cast<f32x4 *>(to + e) = four;
+                        }
+                        continue;
+                    }
+                }
 #pragma unroll
                 for (int e = 0; e < T::kVec; ++e)
-                    if (whole || span.first + e >= span.own) mine[place(span.first + e)] = key[c * T::kVec + e] == -kInf ? -kInf : s[c * T::kVec + e];
+                    if (span.first + e >= span.own) mine[place(span.first + e)] = s[c * T::kVec + e];
             }
             wave_lds();
             // the value of each group, by group_lanes lanes
@@ -230,10 +262,21 @@ __global__ __launch_bounds__(kThreads) void row_route_kernel(RouteArgs A)
             for (int g = R.l / lanes; g < A.groups; g += LANES / lanes) {
                 const uint32_t from = g * A.group_size + part * each, to = min(from + each, (uint32_t)(g + 1) * A.group_size);
                 float first = -kInf, second = -kInf;
-                for (uint32_t j = from; j < to; ++j) {
-                    const float c = mine[place(j)];
-                    second = fmaxf(second, fminf(first, c));
-                    first = fmaxf(first, c);
+                if ((A.group_size | each) % 4 == 0) {
+                    for (uint32_t j = from; j < to; j += 4) {
+                        const f32x4 c = *reinterpret_cast<const f32x4 *>(mine + place(j));
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            second = __builtin_amdgcn_fmed3f(first, second, c[e]);  // (first >= second)
+                            first = fmaxf(first, c[e]);
+                        }
+                    }
+                } else {
+                    for (uint32_t j = from; j < to; ++j) {
+                        const float c = mine[place(j)];
+                        second = __builtin_amdgcn_fmed3f(first, second, c);
+                        first = fmaxf(first, c);
+                    }
                 }
                 for (int d = 1; d < lanes; d *= 2) {
                     const float first_o = __shfl_xor(first, d), second_o = __shfl_xor(second, d);
@@ -265,7 +308,7 @@ __global__ __launch_bounds__(kThreads) void row_route_kernel(RouteArgs A)
             constexpr int kList = VALUES < KEPT ? VALUES : KEPT;
             double list[VALUES];
 #pragma unroll
-            for (int v = 0; v < VALUES; ++v) list[v] = key[v] > -kInf ? choice(key[v], R.column(v)) : no_choice();
+            for (int v = 0; v < VALUES; ++v) list[v] = choice(key[v], R.column(v));
 #pragma unroll
             for (int i = 0; i < VALUES; i += kList) sort_down<kList>(list + i);
 #pragma unroll
@@ -289,7 +332,7 @@ __global__ __launch_bounds__(kThreads) void row_route_kernel(RouteArgs A)
             double c = no_choice();
 #pragma unroll
             for (int i = r * LANES; i < KEPT && i < (r + 1) * LANES; ++i) c = R.l == i - r * LANES ? best[i] : c;
-            const bool is = !bad && r * LANES + R.l < A.k && (uint64_t)__double_as_longlong(c) != kNoChoiceBits;
+            const bool is = !bad && r * LANES + R.l < A.k && is_choice(c);
             column[r] = is ? (int)chosen_column(c) : -1;
             at_chosen[r] = is ? T::get(S[column[r]]) : 0.f;
         }
@@ -337,11 +380,11 @@ __global__ __launch_bounds__(kThreads) void row_route_grad_kernel(RouteArgs A)
 #pragma unroll
         for (int r = 0; r < kRounds; ++r) at_listed[r] = column[r] < A.m ? T::get(S[column[r]]) : 0.f;
         RouteScore score{A.score == REGOT_SIGMOID};
-        score.template of_row<LANES>(x);
+        float s[VALUES];
+        score.template of_row<LANES>(x, s);
         float *const mine = held[at];
-        float c[kRounds], s[VALUES], Z = 0.f, gs = 0.f, any = 0.f;
+        float c[kRounds], Z = 0.f, gs = 0.f, any = 0.f;
         score(at_listed, c);
-        score(x, s);
 #pragma unroll
         for (int r = 0; r < kRounds; ++r) {
             c[r] = column[r] < A.m ? c[r] : 0.f;
