@@ -96,7 +96,7 @@ RowPlan plan_rows(int64_t n, int64_t m, int k, int few = kFewRows)
 template <int TYPE, bool BIAS, bool TOP>
 void launch_logprob(const RowArgs &A, const RowPlan &P, hipStream_t s)
 {
-    constexpr int kVecs = BIAS || TYPE == REGOT_F32 ? 4 : 8;  // 16-byte loads in flight: two slices, one of fp32 (1500 x 10007 fp32, 32 alternatives: 8 loads 23.8 us, 4 18.6) or with a bias
+    constexpr int kVecs = 4;  // 16-byte loads in flight (8: 4096 x 131072 bf16, 20 alternatives 179 us and 181, but 10000 x 5000 77 and 59)
     constexpr uint32_t kLoad = kLanes * Score<TYPE>::kVec;  // columns of a wave's load
     const dim3 threads(kThreads);
     const auto grid = [](int64_t blocks) { return dim3((unsigned)std::min(blocks, kMaxGrid)); };

@@ -127,10 +127,11 @@ struct Span {
             for (int e = 0; e < T::kVec; ++e) x[e] = from + e >= own ? x[e] : -kInf;
         }
     }
+    __device__ __forceinline__ void load_bias(float *b, const float *bias) const { __builtin_memcpy(b, bias + first, T::kVec * sizeof(float)); }
     __device__ __forceinline__ void add_bias(float *x, const float *bias) const
     {
         float b[T::kVec];
-        __builtin_memcpy(b, bias + first, sizeof(b));
+        load_bias(b, bias);
 #pragma unroll
         for (int e = 0; e < T::kVec; ++e) x[e] += b[e];
     }

@@ -149,6 +149,20 @@ struct RowScores {
         if constexpr (BIAS) span.add_bias(x, bias);
         span.mask(x);
     }
+    // the same with the bias that was asked for beside the chunk (b: nothing without a bias)
+    __device__ __forceinline__ void ask_bias(uint32_t j, float *b) const
+    {
+        if constexpr (BIAS) Span<TYPE>(j, m).load_bias(b, bias);
+    }
+    __device__ __forceinline__ void unpack(Chunk chunk, const float *b, uint32_t j, float *x) const
+    {
+        T::unpack(chunk, x);
+        if constexpr (BIAS) {
+#pragma unroll
+            for (int e = 0; e < T::kVec; ++e) x[e] += b[e];
+        }
+        Span<TYPE>(j, m).mask(x);
+    }
     __device__ __forceinline__ void read(uint32_t j, float *x) const { unpack(ask<false>(j), j, x); }
 };
 
@@ -314,15 +328,19 @@ __global__ __launch_bounds__(kThreads) void row_logprob_kernel(RowArgs A)
         };
         for (uint32_t j0 = begin; j0 < end; j0 += VECS * kStep) {
             typename T::Chunk raw[VECS];
+            float bias[VECS][T::kVec];
 #pragma unroll
             for (int u = 0; u < VECS; ++u)
-                if (j0 + u / kVecsOfGroup * kSlice < end) raw[u] = scores.template ask<true>(j0 + u * kStep + at);
+                if (j0 + u / kVecsOfGroup * kSlice < end) {
+                    raw[u] = scores.template ask<true>(j0 + u * kStep + at);
+                    scores.ask_bias(j0 + u * kStep + at, bias[u]);
+                }
 #pragma unroll
             for (int g = 0; g < kGroups; ++g) {
                 if (j0 + g * kSlice < end) {
                     float x[kGroup];
 #pragma unroll
-                    for (int v = 0; v < kVecsOfGroup; ++v) scores.unpack(raw[g * kVecsOfGroup + v], j0 + (g * kVecsOfGroup + v) * kStep + at, x + v * T::kVec);
+                    for (int v = 0; v < kVecsOfGroup; ++v) scores.unpack(raw[g * kVecsOfGroup + v], bias[g * kVecsOfGroup + v], j0 + (g * kVecsOfGroup + v) * kStep + at, x + v * T::kVec);
                     const float top = largest(x);
                     soft.add(x, top, A.log2_scale);
                     if constexpr (TOP) {

@@ -108,3 +108,29 @@ def test_wrong_sizes_are_refused():
         RowDistill(4, 100, 3, dtype=torch.bfloat16).distill(S, torch.zeros(4, 3, dtype=torch.int32, device="cuda"), torch.zeros(4, 3, device="cuda"))
     with pytest.raises(TypeError):
         RowRoute(4, 100, 3).route(S, bias=torch.zeros(100, dtype=torch.float64, device="cuda"))
+
+
+def test_more_rows_than_a_grid_has():
+    """Rows of one column, 17 million: every workgroup goes on to further rows."""
+    n = 17_000_000
+    S = torch.randn(n, 1, device="cuda")
+    target = torch.zeros(n, 1, dtype=torch.int32, device="cuda")
+    op = RowLogprob(n, 1, k=1, targets=1, dtype=torch.float32)
+    for t in (op.logprob_out, op.entropy, op.top_logprob):
+        t.fill_(5.0)
+    op.logprob(S, target)
+    assert torch.equal(op.stats[:, :1], S)
+    for t in (op.stats[:, 1], op.logprob_out, op.entropy, op.top_idx, op.top_logprob):
+        assert int(t.count_nonzero()) == 0
+    g = torch.ones(n, 1, device="cuda")
+    op.dS = torch.full_like(S, 5.0)
+    assert float(op.grad(S, target, g, g[:, 0]).abs().max()) == 0.0
+    learn = RowDistill(n, 1, 1, dtype=torch.float32)
+    learn.loss.fill_(5.0)
+    learn.grad.fill_(5.0)
+    learn.distill(S, target, S)
+    assert int(learn.loss.count_nonzero()) == 0 and int(learn.grad.count_nonzero()) == 0
+    route = RowRoute(n, 1, 1, dtype=torch.float32)
+    route.idx.fill_(5)
+    route.route(S)
+    assert int(route.idx.count_nonzero()) == 0 and bool((route.weight == 1.0).all())
