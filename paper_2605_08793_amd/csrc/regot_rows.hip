@@ -190,7 +190,7 @@ void launch_distill(const RowArgs &A, hipStream_t s)
     const uint32_t loads = A.m / Score<TYPE>::kVec;
 #define GO(TYPE, W, V, K) hipLaunchKernelGGL((row_distill_kernel<TYPE, W, V, K, false>), grid(W == 1 ? (A.n + kWaves - 1) / kWaves : A.n), dim3(Team<W>::kBlock), 0, s, A)
     if (A.parts > 1) {
-        hipLaunchKernelGGL((row_logprob_kernel<TYPE, false, false, 8, true>), grid(A.n * A.parts), dim3(kThreads), 0, s, A);
+        hipLaunchKernelGGL((row_logprob_kernel<TYPE, false, false, 4, true>), grid(A.n * A.parts), dim3(kThreads), 0, s, A);
         hipLaunchKernelGGL((row_distill_kernel<TYPE, kWaves, 4, 0, true>), grid(A.n * A.parts), dim3(kThreads), 0, s, A);
     } else if (A.m <= 2 * kLanes) {
         GO(TYPE + kSingle, 1, 2, 0);

@@ -205,6 +205,25 @@ __device__ __forceinline__ uint64_t best_before(const RowScores<TYPE, BIAS> &sco
     return best;
 }
 
+// push(a) for each of a thread's columns that does not come behind `bound`.
+template <int TYPE, bool BIAS, typename F>
+__device__ __forceinline__ void each_from(const RowScores<TYPE, BIAS> &scores, uint64_t bound, int thread, int threads, F push)
+{
+    using T = Score<TYPE>;
+    const float least = score_of(bound);
+    for (uint32_t j = thread * T::kVec; j < scores.m; j += threads * T::kVec) {
+        float x[T::kVec];
+        scores.read(j, x);
+        if (!(largest(x) >= least)) continue;
+        const uint32_t first = Span<TYPE>(j, scores.m).first;
+#pragma unroll
+        for (int e = 0; e < T::kVec; ++e) {
+            const uint64_t a = alternative(x[e], first + e);
+            if (a >= bound && a > kForbidden) push(a);
+        }
+    }
+}
+
 struct TopShared {
     float lane_max[kThreads];
     uint32_t hot[kThreads], block[kList];
@@ -216,8 +235,9 @@ struct TopShared {
 // The k best columns of a row, by a workgroup that knows the maximum of each thread's columns in each block of the row
 // (block_max[b], thread t having the 16 bytes number t, t + kThreads, ... of the row): k columns are at or above the
 // k-th largest of the threads' maxima, and little more than k are, in little more than k of the (block, thread) pairs.
-// Those are read again.  Where more than fit the lists may be among the best (many equal scores), the
-// best are found one by one, each thread offering the best of its columns that is behind the last one found.
+// Those are read again.  Where more than fit the lists may be among the best (many equal scores), the bound is made of scores and
+// columns; where that does not do either, the best are found one by one, each thread offering the best of its columns that is behind the last
+// one found.  (A row of one value, 131072 columns, 20 alternatives: 467 us one by one, 38 us with the second bound; 10 us where scores differ.)
 template <int TYPE, bool BIAS>
 __device__ __forceinline__ void best_columns(const RowArgs &A, const RowOut &out, const RowScores<TYPE, BIAS> &scores, float my_max,
                                              const float (*block_max)[kThreads], TopShared &L)
@@ -269,8 +289,27 @@ __device__ __forceinline__ void best_columns(const RowArgs &A, const RowOut &out
         __syncthreads();
         count = L.count;
         if (pairs > kList || count > kList) {
+            // once more with a bound that tells equal scores apart: the k-th of the threads' best columns
             uint64_t mine = best_before(scores, ~0ull, threadIdx.x, kThreads);
-            for (count = 0; count < A.k; ++count) {
+            __syncthreads();  // (the counts are read)
+            L.list[threadIdx.x] = mine;
+            if (threadIdx.x == 0) L.best[0] = kForbidden, L.count = 0;
+            __syncthreads();
+            int better = 0;
+#pragma unroll 8
+            for (int o = 0; o < kThreads; ++o) better += L.list[o] > mine;
+            if (better == A.k - 1 && mine != 0) L.best[0] = mine;
+            __syncthreads();
+            const uint64_t from = L.best[0];
+            each_from(scores, from, threadIdx.x, kThreads, [&](uint64_t a) {
+                const int at = atomicAdd(&L.count, 1);
+                if (at < kList) L.list[at] = a;
+            });
+            __syncthreads();
+            count = L.count;
+            if (count <= kList) {
+                rank_all(L.list, count, threadIdx.x, kThreads, A.k, [&](int rank, uint64_t a) { out.top(rank, a); });
+            } else for (count = 0; count < A.k; ++count) {
                 uint64_t best = mine;
 #pragma unroll
                 for (int d = 1; d < kLanes; d *= 2) {
@@ -294,8 +333,9 @@ __device__ __forceinline__ void best_columns(const RowArgs &A, const RowOut &out
 }
 
 // A row, or a part of one, by a workgroup.  VECS: 16-byte loads a lane has in flight.
+// (Six workgroups to a compute unit, which is one register less than without the bound: 10000 x 5000 bf16, 20 alternatives 66 us and 59.)
 template <int TYPE, bool BIAS, bool TOP, int VECS, bool PARTS>
-__global__ __launch_bounds__(kThreads) void row_logprob_kernel(RowArgs A)
+__global__ __launch_bounds__(kThreads, BIAS ? 5 : 6) void row_logprob_kernel(RowArgs A)
 {
     using T = Score<TYPE>;
     using Scores = RowScores<TYPE, BIAS>;
@@ -413,6 +453,7 @@ __global__ __launch_bounds__(kThreads) void row_logprob_narrow_kernel(RowArgs A)
     constexpr uint32_t kStep = kLanes * T::kVec;
     constexpr int kHeld = 256;
     __shared__ uint16_t pair[kWaves][VECS * kLanes];
+    __shared__ int counts[kWaves];
     __shared__ __align__(16) uint64_t list[kWaves][kHeld + kRankPad];
     const int lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes;
     const uint32_t at = lane * T::kVec;
@@ -480,7 +521,23 @@ __global__ __launch_bounds__(kThreads) void row_logprob_narrow_kernel(RowArgs A)
                 if (count <= kHeld) {
                     rank_all(list[wave], count, lane, kLanes, A.k, [&](int rank, uint64_t a) { out.top(rank, a); });
                 } else {
+                    uint64_t mine = best_before(scores, ~0ull, lane, kLanes);
+                    int better = 0;
+                    for (int l = 0; l < kLanes; ++l) better += __shfl((unsigned long long)mine, l) > mine;
+                    const uint64_t kth = __ballot(better == A.k - 1 && mine != 0);
+                    const uint64_t from = kth != 0 ? __shfl((unsigned long long)mine, __builtin_ctzll(kth)) : kForbidden;
+                    if (lane == 0) counts[wave] = 0;
+                    wave_lds();
+                    each_from(scores, from, lane, kLanes, [&](uint64_t a) {
+                        const int to = atomicAdd(&counts[wave], 1);
+                        if (to < kHeld) list[wave][to] = a;
+                    });
+                    wave_lds();
+                    count = counts[wave];
                     uint64_t last = ~0ull;
+                    if (count <= kHeld) {
+                        rank_all(list[wave], count, lane, kLanes, A.k, [&](int rank, uint64_t a) { out.top(rank, a); });
+                    } else
                     for (count = 0; count < A.k; ++count) {
                         uint64_t best = best_before(scores, last, lane, kLanes);
 #pragma unroll
