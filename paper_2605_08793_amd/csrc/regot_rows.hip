@@ -54,11 +54,11 @@ constexpr int64_t kMaxGrid = 1 << 22;  // (rows beyond are the same workgroups')
 // How the rows of a call are shared out: a few long rows are several workgroups' each, whose findings a second launch joins.  (One
 // workgroup takes 5.5 us and 0.45 for each slice of 4096 columns, the two launches 10.5 us and the reading.  us, one workgroup a row / parts, bf16, 20
 // alternatives: 1 x 131072 19.7 / 10.6, 8 x 131072 20.3 / 11.2, 64 x 50000 11.8 / 10.8, 128 x 32768 10.5 / 11.7, 256 x 131072 25.9 / 26.8.)
-constexpr int kFewRows = 192, kLongRow = 13, kPlaces = 512, kLeastParts = 8;
+constexpr int kFewRows = 192, kLongRow = 13, kPlaces = 512, kLeastParts = 8, kMostParts = 64;
 
 struct RowPlan {
-    int block = 1, blocks = 1, parts = 1, part_blocks = 1;
-    size_t max = 0, total = 0;                     // workspace
+    int block = 1, blocks = 1, parts = 1, part_blocks = 1;  // slices of a block, blocks of a row, workgroups of a row, blocks of each
+    size_t max = 0, total = 0;                              // workspace: where the maxima are, and all of it
 };
 
 int64_t power_of_two(int64_t least)
@@ -73,10 +73,13 @@ RowPlan plan_rows(int64_t n, int64_t m, int k, int few = kFewRows)
     RowPlan P;
     const int64_t slices = std::max<int64_t>((m + kSlice - 1) / kSlice, 1);
     int64_t parts = 1;
-    if (n <= few && slices >= kLongRow) parts = std::min<int64_t>({slices, kPartBlocks, std::max<int64_t>(kPlaces / n, kLeastParts)});
+    // (alternatives: the second launch looks through all blocks of a row.  1 x 131072 bf16 16 blocks 9.5 us, 32 9.7, 64 9.9; 64 rows of them 12.7, 13.9, 13.9;
+    // 4 x 1000000 19.1, 15.6, 14.3)
+    const int64_t most_blocks = k == 0 ? kMostParts : slices <= 32 ? kPartBlocks / 2 : kPartBlocks;
+    if (n > 0 && n <= few && slices >= kLongRow) parts = std::min<int64_t>({slices, most_blocks, std::max<int64_t>(kPlaces / n, kLeastParts)});
     if (parts > 1) {
         const int64_t of_part = (slices + parts - 1) / parts;  // slices of a part
-        const int64_t most = std::max<int64_t>(kPartBlocks / parts, 1);   // blocks of a part
+        const int64_t most = std::max<int64_t>(most_blocks / parts, 1);   // blocks of a part
         P.block = (int)power_of_two((of_part + most - 1) / most);
         P.part_blocks = (int)((of_part + P.block - 1) / P.block);
         P.blocks = (int)((slices + P.block - 1) / P.block);

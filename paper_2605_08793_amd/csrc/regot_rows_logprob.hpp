@@ -35,7 +35,7 @@ struct RowArgs {
 constexpr int kGroup = 16;                    // scores a lane works on at a time
 constexpr uint32_t kSlice = kThreads * kGroup;  // columns of a row that a workgroup works on at a time
 constexpr int kWholeBlocks = 16;              // blocks of a row that one workgroup reads
-constexpr int kPartBlocks = 64;               // of one that several do, at most
+constexpr int kPartBlocks = 32;               // of one that several do, at most
 constexpr int kList = 512;                    // blocks, and columns, that may hold the best k; beyond, they are found one by one
 
 // A column and its score as one number: larger for what comes first among a row's alternatives.  0 is none.

@@ -68,7 +68,22 @@ def test_refused(name, changed, status):
 
 @pytest.mark.parametrize("name", sorted(CALLS))
 def test_nothing_to_do_is_fine(name):
-    assert call(name, n=0) == 0
+    for m in (0, 8, 1000, 1 << 20, (1 << 31) - 1):
+        if m > 1024 and "route" in name:
+            continue
+        changed = dict(n=0, m=m, ldS=m)
+        if "ldD" in CALLS[name]:
+            changed["ldD"] = m
+        assert call(name, **changed) == 0
+
+
+def test_workspaces_of_all_sizes():
+    """Asked for on the host for any size; for k alternatives no smaller than for none, and a small part of the scores."""
+    for n in (0, 1, 2, 63, 96, 97, 192, 193, 10 ** 6):
+        for m in (0, 1, 4097, 53248, 131072, 10 ** 6, (1 << 31) - 1):
+            none, some = B.regot_row_logprob_workspace_bytes(n, m, 0), B.regot_row_logprob_workspace_bytes(n, m, 20)
+            assert 256 <= none <= some <= 256 + n * (64 * 12 + 32 * 1024) + 512
+            assert 256 <= B.regot_row_distill_workspace_bytes(n, m, 20) <= 256 + n * 64 * 12 + 512
 
 
 def test_workspaces():
