@@ -553,8 +553,8 @@ int regot_splr_direction(int64_t n, int64_t m,
  * experts, balanced by the same duals), with their gradients to S.
  *   - `type` is the type of S and of a gradient dS: REGOT_F32, REGOT_BF16 or REGOT_F16.  Everything else is fp32 and
  *     int32; maxima, sums and exponents are held in fp32 and a gradient is rounded to its type once.  S and dS are row-major with
- *     leading dimensions ldS, ldD >= m in elements, aligned to their elements (wide loads are used from each row's first
- *     16-byte boundary on, whatever the row's start is).
+ *     leading dimensions ldS, ldD >= m in elements, aligned to their elements: 16-byte loads and stores are used wherever a row
+ *     starts.  A gradient must not overlap S.
  *   - Lists per row (targets, teacher entries, choices, alternatives) are dense arrays of n rows.  An index outside
  *     [0, m), such as -1, is no entry.  A column listed twice counts twice.
  *   - A score of -inf (a mask), or a bias of -inf, is a forbidden column: p = 0.  A row that has no other score (or m = 0) has no distribution: its
@@ -574,7 +574,8 @@ enum { REGOT_F32 = 0, REGOT_BF16 = 1, REGOT_F16 = 2 };
  *     top_idx, top_logprob[i*k ..]  the k columns of largest x_ij, the largest first, equal ones by ascending column,
  *                              and their ln p; -1 and -inf where the row has fewer that are not forbidden
  * targets = 0 (target and logprob may be NULL) and k = 0 (top_* may be NULL) leave that part out.
- * 0 <= targets <= REGOT_ROW_MAX_LIST, 0 <= k <= REGOT_ROW_MAX_TOP.  S is read once.
+ * 0 <= targets <= REGOT_ROW_MAX_LIST, 0 <= k <= REGOT_ROW_MAX_TOP.  S is read once, and the few blocks of it that hold the
+ * alternatives a second time (a row of many equal scores up to three times).  eta has to be such that 1 / eta is an fp32 number other than 0.
  */
 #define REGOT_ROW_MAX_LIST 1024
 #define REGOT_ROW_MAX_TOP 128
@@ -690,7 +691,7 @@ int regot_stream_read_probe(int64_t n, int64_t m,
 int regot_placement_probe(int grid, uint32_t *ids /* device, [2 * grid] out */, regot_stream_t stream);
 
 /*
- * Profiling aid, not part of the method.  The next call of any entry point above made by the
+ * Profiling aid, not part of the method.  The next call of any entry point above but the row calls made by the
  * calling host thread records `start_event` on its stream just before, and `stop_event` just
  * after, the launch of its streaming kernel (the single pass over M; the small combine / scatter
  * kernels that follow are outside the pair; for regot_topk_threshold it is the first pass over M).  Both are hipEvent_t handles owned by the caller,
