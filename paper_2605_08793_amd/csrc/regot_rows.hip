@@ -1,6 +1,6 @@
-// Row operators: log probabilities, entropy and alternatives; distillation; routing; and their gradients.
-//
-// Every kernel here gives a workgroup (log probabilities, distillation) or a wave (routing) one row.
+// Row operators on a model's scores: log probabilities, entropy and alternatives; distillation; routing; and their gradients.
+// Checks of arguments, how rows are shared out, launches.  The kernels are in regot_rows_logprob.hpp, regot_rows_grad.hpp and
+// regot_rows_route.hpp.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>

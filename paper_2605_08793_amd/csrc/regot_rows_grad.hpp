@@ -33,7 +33,8 @@ struct Team {
 // with the sum over all entries of its column (columns listed twice are written twice, with the same number).
 
 // dS of log probabilities and entropy.  With t = log2 p, a = (sum g + h H) / eta and b = h ln 2 / eta:  -p (a + b t), and
-// g / eta more at the given columns.
+// g / eta more at the given columns.  The sums are known, so a row is cut into as many parts as there are loads for; each
+// reads and writes its columns once.  Bound by memory: 4096 x 131072 bf16 350 us = 6.1 TB/s, 2048 x 40000 57 us = 5.7 TB/s.
 template <int TYPE, bool BIAS, int WAVES, int VECS>
 __global__ __launch_bounds__(Team<WAVES>::kBlock) void row_logprob_grad_kernel(RowArgs A)
 {
@@ -99,8 +100,10 @@ __global__ __launch_bounds__(Team<WAVES>::kBlock) void row_logprob_grad_kernel(R
 
 // The loss against a sparse target, and dS = w (p - q) / eta.
 //
-// Two reads of a row, one where a thread can hold its columns (HELD: VECS 16-byte loads of them), or one here and one by the kernel
-// that left the sums of the row's parts (PARTS).
+// The sum over a row comes before its first gradient, so a row is read twice (PARTS: here, and by the kernel that left the sums
+// of its parts).  Backwards the second time: the last stretch of VECS loads a thread is still in registers, the first KEPT loads of the one before are in
+// LDS, and what is before that is likeliest in the caches.  Bound by traffic: 4096 x 131072 bf16 441 us for 2.1 GB that have to move and 0.5 that is
+// read again (6.1 TB/s); 518 without KEPT.  Shorter rows by the chain of each row (target, sum, loss, list) and the rows under way.
 template <int TYPE, int WAVES, int VECS, int KEPT, bool PARTS>
 __global__ __launch_bounds__(Team<WAVES>::kBlock) void row_distill_kernel(RowArgs A)
 {

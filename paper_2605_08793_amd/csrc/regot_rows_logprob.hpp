@@ -332,7 +332,11 @@ __device__ __forceinline__ void best_columns(const RowArgs &A, const RowOut &out
     for (int i = count + threadIdx.x; i < A.k; i += kThreads) out.no_top(i);
 }
 
-// A row, or a part of one, by a workgroup.  VECS: 16-byte loads a lane has in flight.
+// A row, or a part of one, by a workgroup: one pass with a running maximum in every thread, whose sums are brought together at
+// the end, and the threads' maxima in each block for the alternatives.  VECS: 16-byte loads a lane has in flight.
+// Bound by memory for long rows: 4096 x 131072 bf16 170 us = 6.3 TB/s, with 20 alternatives 174-182; about 10 vector
+// instructions a score, four of them the exponential's, would take 130 us.  For rows of one or two slices by what comes behind the pass:
+// 10000 x 5000 bf16 33 us, with 20 alternatives 59.
 // (Six workgroups to a compute unit, which is one register less than without the bound: 10000 x 5000 bf16, 20 alternatives 66 us and 59.)
 template <int TYPE, bool BIAS, bool TOP, int VECS, bool PARTS>
 __global__ __launch_bounds__(kThreads, BIAS ? 5 : 6) void row_logprob_kernel(RowArgs A)
@@ -408,7 +412,8 @@ __global__ __launch_bounds__(kThreads, BIAS ? 5 : 6) void row_logprob_kernel(Row
     }
 }
 
-// A row's parts joined: a workgroup a row.
+// A row's parts joined: a workgroup a row.  A chain of latencies: 6.2 us at 1 x 131072 bf16 with 20 alternatives (about: the maxima 1.2, the sums
+// 1.0, the bound 0.7, the blocks 0.4, the second read 1.3, the ranks 1.0), 2 without.
 template <int TYPE, bool BIAS, bool TOP>
 __global__ __launch_bounds__(kThreads) void row_logprob_join_kernel(RowArgs A)
 {
@@ -444,7 +449,8 @@ __global__ __launch_bounds__(kThreads) void row_logprob_join_kernel(RowArgs A)
     }
 }
 
-// Narrow rows: a wave a row, which is held in registers as it was read: VECS 16-byte loads a lane.
+// Narrow rows: a wave a row, which is held in registers as it was read: VECS 16-byte loads a lane.  Bound by instructions: 16384 x 2000
+// bf16 17 us = 3.8 TB/s, with 10 alternatives 39; by workgroups of four waves a row 42 and 137.
 template <int TYPE, bool BIAS, bool TOP, int VECS>
 __global__ __launch_bounds__(kThreads) void row_logprob_narrow_kernel(RowArgs A)
 {
