@@ -182,6 +182,18 @@ RowPlan plan_distill(int64_t n, int64_t m) { return plan_rows(n, m, 0, kFewDisti
 
 constexpr int kCUs = 256;
 
+template <int TYPE, int WAVES, int VECS, int KEPT>
+void launch_team(const RowArgs &A, hipStream_t s)
+{
+    const dim3 grid((unsigned)std::min(WAVES == 1 ? (A.n + kWaves - 1) / kWaves : A.n, kMaxGrid)), threads(Team<WAVES>::kBlock);
+    if constexpr (WAVES == 1)
+        if (A.k <= 128) {
+            hipLaunchKernelGGL((row_distill_kernel<TYPE, WAVES, VECS, KEPT, false, 128>), grid, threads, 0, s, A);
+            return;
+        }
+    hipLaunchKernelGGL((row_distill_kernel<TYPE, WAVES, VECS, KEPT, false>), grid, threads, 0, s, A);
+}
+
 template <int TYPE>
 void launch_distill(const RowArgs &A, hipStream_t s)
 {
@@ -191,28 +203,26 @@ void launch_distill(const RowArgs &A, hipStream_t s)
     // 51, 8 waves 70; 999 x 33333 4 waves 44, 8 waves holding 40; 4096 x 131072 4 waves 530, 8 waves 518, holding 441, 16 waves holding 488;
     // 256 x 131072 8 waves holding 39, 16 waves holding 32; 256 x 10000 fp32 4 waves 11.0, 8 waves 9.4.
     const uint32_t loads = A.m / Score<TYPE>::kVec;
-#define GO(TYPE, W, V, K) hipLaunchKernelGGL((row_distill_kernel<TYPE, W, V, K, false>), grid(W == 1 ? (A.n + kWaves - 1) / kWaves : A.n), dim3(Team<W>::kBlock), 0, s, A)
     if (A.parts > 1) {
         hipLaunchKernelGGL((row_logprob_kernel<TYPE, false, false, 4, true>), grid(A.n * A.parts), dim3(kThreads), 0, s, A);
         hipLaunchKernelGGL((row_distill_kernel<TYPE, kWaves, 4, 0, true>), grid(A.n * A.parts), dim3(kThreads), 0, s, A);
     } else if (A.m <= 2 * kLanes) {
-        GO(TYPE + kSingle, 1, 2, 0);
+        launch_team<TYPE + kSingle, 1, 2, 0>(A, s);
     } else if (A.n > 512 && loads <= 2 * kLanes) {
-        GO(TYPE, 1, 2, 0);
+        launch_team<TYPE, 1, 2, 0>(A, s);
     } else if (A.n > 512 && loads <= 4 * kLanes) {
-        GO(TYPE, 1, 4, 0);
+        launch_team<TYPE, 1, 4, 0>(A, s);
     } else if (A.n > 512 && loads <= 8 * kLanes) {
-        GO(TYPE, 1, 8, 0);
+        launch_team<TYPE, 1, 8, 0>(A, s);
     } else if (loads <= (A.n > 512 ? 64 : 8) * kLanes) {
-        GO(TYPE, 4, 2, 0);
+        launch_team<TYPE, 4, 2, 0>(A, s);
     } else if (loads <= 64 * kLanes) {
-        GO(TYPE, 8, 4, 0);
+        launch_team<TYPE, 8, 4, 0>(A, s);
     } else if (A.n > kCUs) {
-        GO(TYPE, 8, 8, 8);
+        launch_team<TYPE, 8, 8, 8>(A, s);
     } else {
-        GO(TYPE, 16, 8, 8);
+        launch_team<TYPE, 16, 8, 8>(A, s);
     }
-#undef GO
 }
 
 void launch_distill(const RowArgs &A, int type, hipStream_t s)

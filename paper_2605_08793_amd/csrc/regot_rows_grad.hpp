@@ -104,7 +104,8 @@ __global__ __launch_bounds__(Team<WAVES>::kBlock) void row_logprob_grad_kernel(R
 // of its parts).  Backwards the second time: the last stretch of VECS loads a thread is still in registers, the first KEPT loads of the one before are in
 // LDS, and what is before that is likeliest in the caches.  Bound by traffic: 4096 x 131072 bf16 441 us for 2.1 GB that have to move and 0.5 that is
 // read again (6.1 TB/s); 518 without KEPT.  Shorter rows by the chain of each row (target, sum, loss, list) and the rows under way.
-template <int TYPE, int WAVES, int VECS, int KEPT, bool PARTS>
+// LIST: the room for a row's entries (a wave a row: 128 where they fit, 16384 x 400 fp32 24.2 us with 1024 and 21.2 with 128).
+template <int TYPE, int WAVES, int VECS, int KEPT, bool PARTS, int LIST = REGOT_ROW_MAX_LIST>
 __global__ __launch_bounds__(Team<WAVES>::kBlock) void row_distill_kernel(RowArgs A)
 {
     using T = Score<TYPE>;
@@ -112,8 +113,8 @@ __global__ __launch_bounds__(Team<WAVES>::kBlock) void row_distill_kernel(RowArg
     constexpr uint32_t kStep = (uint32_t)Row::kSize * T::kVec;
     __shared__ float team_lds[3 * WAVES];
     __shared__ typename T::Chunk kept[KEPT > 0 ? KEPT : 1][KEPT > 0 ? Row::kBlock : 1];
-    __shared__ uint32_t list_column[Row::kRows][REGOT_ROW_MAX_LIST];
-    __shared__ float list_q[Row::kRows][REGOT_ROW_MAX_LIST];
+    __shared__ uint32_t list_column[Row::kRows][LIST];
+    __shared__ float list_q[Row::kRows][LIST];
     const int thread = Row::thread(), lane = threadIdx.x & (kLanes - 1), team = Row::row();
     const int64_t tasks = PARTS ? A.n * A.parts : A.n;
     for (int64_t task = (int64_t)blockIdx.x * Row::kRows + team; task < tasks; task += (int64_t)gridDim.x * Row::kRows) {
@@ -190,6 +191,8 @@ __global__ __launch_bounds__(Team<WAVES>::kBlock) void row_distill_kernel(RowArg
         const float weight = (A.row_weight ? A.row_weight[row] : 1.f) * A.inv_eta;
         const float of_p = bad ? kNan : none ? 0.f : weight / soft.sum;
         float loss = 0.f;
+        const uint32_t first_column = my_column;
+        const float first_x = my_x;
         for (int l = thread; l < A.k; l += Row::kSize) {
             if (l != thread) {
                 my_column = (uint32_t)target[l];
@@ -235,11 +238,12 @@ __global__ __launch_bounds__(Team<WAVES>::kBlock) void row_distill_kernel(RowArg
             __threadfence_block();
             Row::sync();
             for (int l = thread; l < A.k; l += Row::kSize) {
-                const uint32_t j = list_column[team][l];
+                const uint32_t j = l == thread ? first_column : list_column[team][l];
                 if (j < begin || j >= end) continue;
                 float q = 0.f;
+#pragma unroll 8
                 for (int u = 0; u < A.k; ++u) q += list_column[team][u] == j ? list_q[team][u] : 0.f;
-                out[j] = T::put(p_weighted(scores(j)) - (bad ? kNan : weight) * q);
+                out[j] = T::put(p_weighted(l == thread ? first_x : scores(j)) - (bad ? kNan : weight) * q);
             }
         }
         Row::sync();  // the list and the sums are read

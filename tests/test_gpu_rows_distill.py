@@ -48,7 +48,8 @@ def compare(S_host, got, t_idx, t_score, eta, w, dtype, what):
 
 
 @pytest.mark.parametrize("n,m,k", [(1, 1, 1), (3, 2, 4), (5, 63, 9), (65, 128, 16), (40, 1000, 50), (600, 301, 5), (9, 4097, 100),
-                                   (200, 3001, 32), (4, 33333, 64), (3, 70001, 300), (2, 131072, 64), (1, 200003, 1024)])
+                                   (200, 3001, 32), (4, 33333, 64), (3, 70001, 300), (2, 131072, 64), (1, 200003, 1024),
+                                   (520, 301, 200), (530, 1900, 129), (513, 3500, 40), (600, 100, 90), (514, 9000, 20), (97, 53300, 20), (300, 70001, 20)])
 @pytest.mark.parametrize("dtype", TYPES, ids=TYPE_IDS)
 def test_sizes(n, m, k, dtype):
     S = scores(n, m, dtype, n + m)

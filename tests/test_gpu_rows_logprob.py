@@ -82,7 +82,8 @@ def targets_for(n, m, count, seed):
 
 
 SIZES = [(1, 1, 1), (3, 2, 5), (5, 7, 3), (64, 63, 8), (17, 64, 64), (3, 65, 1), (2, 257, 20), (129, 1000, 10), (40, 2049, 128),
-         (9, 4097, 33), (300, 3001, 5), (7, 16385, 20), (3, 70001, 64), (1, 131072, 20), (2, 200003, 128), (2500, 129, 4)]
+         (9, 4097, 33), (300, 3001, 5), (7, 16385, 20), (3, 70001, 64), (1, 131072, 20), (2, 200003, 128), (2500, 129, 4),
+         (97, 53300, 20), (193, 53300, 9), (5, 600001, 40), (130, 4096, 50)]
 
 
 @pytest.mark.parametrize("n,m,k", SIZES)
