@@ -199,9 +199,9 @@ void launch_distill(const RowArgs &A, hipStream_t s)
 {
     const auto grid = [](int64_t blocks) { return dim3((unsigned)std::min(blocks, kMaxGrid)); };
     // Teams of more waves hold more of a row between its two reads (the last stretch in registers, the one before in LDS) and
-    // make less of the traffic; of fewer, they keep more rows under way.  us: 16384 x 1000 bf16 1 wave 29, 4 waves 64; 4096 x 10000 4 waves
-    // 51, 8 waves 70; 999 x 33333 4 waves 44, 8 waves holding 40; 4096 x 131072 4 waves 530, 8 waves 518, holding 441, 16 waves holding 488;
-    // 256 x 131072 8 waves holding 39, 16 waves holding 32; 256 x 10000 fp32 4 waves 11.0, 8 waves 9.4.
+    // make less of the traffic; of fewer, they keep more rows under way.  us: 16384 x 1000 bf16 1 wave 25, 4 waves 63; 4096 x 10000 4 waves
+    // 47, 8 waves 78; 4096 x 32768 4 waves 123, 8 waves holding 134; 999 x 33333 4 waves 43, 8 waves holding 39; 4096 x 131072 4 waves 526, 8
+    // waves 513, holding 431, 16 waves holding 468; 256 x 131072 8 waves holding 40, 16 waves holding 33; 256 x 10000 fp32 4 waves 9.9, 8 waves 8.9.
     const uint32_t loads = A.m / Score<TYPE>::kVec;
     if (A.parts > 1) {
         hipLaunchKernelGGL((row_logprob_kernel<TYPE, false, false, 4, true>), grid(A.n * A.parts), dim3(kThreads), 0, s, A);
@@ -239,9 +239,11 @@ void launch_logprob(const RowArgs &A, int type, const RowPlan &P, hipStream_t s)
     else launch_logprob<REGOT_F16>(A, P, s);
 }
 
-// Rows of a route by their length: 16 lanes with 4, 8 or 16 scores each, or a wave with 16 (65536 x 128 bf16, 6 choices: 16 lanes with 16 scores
-// each 28 us, with 8 19 us).  Loads of 16 bytes where the columns of
-// each lie in one group; otherwise, and for short rows, a score at a time.
+// Rows of a route by their length: 8 lanes with 4, 8 or 16 scores each, 16 with 8 or 16, 32 with 16, or a wave with 16.  Fewer lanes with more
+// scores each merge less, and hide less of a row's latency.  us: 65536 x 32 bf16, 4 choices 8 lanes 6.5, 16 lanes 11.0; 65536 x 64 fp32, 2 choices 8 lanes
+// 7.7, 16 lanes 11.4; 65536 x 128 bf16, 8 choices 8 lanes 13.4, 16 lanes 17.5, but 1 row 3.6 and 3.3, 512 rows 4.5 and 4.0; 65536 x 256 fp32,
+// 8 choices 8 lanes 29, 16 lanes 27; 16384 x 512 fp32, 8 choices 16 lanes 13.7, 32 lanes 15.6, a wave 20.3, but 1 row 5.6, 4.0 and 3.7.
+// Loads of 16 bytes where the columns of each lie in one group; otherwise, and for short rows, a score at a time (65536 x 64 fp32: 8.7 us).
 template <int TYPE, int LANES, int VALUES>
 void launch_route(const RouteArgs &A, hipStream_t s)
 {
@@ -256,11 +258,15 @@ template <int TYPE>
 void launch_route(RouteArgs &A, hipStream_t s)
 {
     const bool wide = A.m >= Score<TYPE>::kVec && (A.groups == 1 || A.group_size % Score<TYPE>::kVec == 0);
-    const int lanes = A.m <= 256 ? 16 : kLanes;
+    const bool many = A.n > 4096;
+    const int lanes = A.m <= 64 || (A.m <= 128 && wide && many) ? 8 : A.m <= 256 ? 16 : A.m <= 512 ? 32 : kLanes;
     A.group_lanes = (int)std::max<int64_t>(lanes / power_of_two(A.groups), 1);
-    if (A.m <= 64) launch_route<TYPE + kSingle, 16, 4>(A, s);
-    else if (A.m <= 128 && wide) launch_route<TYPE, 16, 8>(A, s);
+    if (A.m <= 32) launch_route<TYPE + kSingle, 8, 4>(A, s);
+    else if (A.m <= 64) wide ? launch_route<TYPE, 8, 8>(A, s) : launch_route<TYPE + kSingle, 8, 8>(A, s);
+    else if (A.m <= 128 && wide && many) launch_route<TYPE, 8, 16>(A, s);
+    else if (A.m <= 128) wide ? launch_route<TYPE, 16, 8>(A, s) : launch_route<TYPE + kSingle, 16, 8>(A, s);
     else if (A.m <= 256) wide ? launch_route<TYPE, 16, 16>(A, s) : launch_route<TYPE + kSingle, 16, 16>(A, s);
+    else if (A.m <= 512) wide ? launch_route<TYPE, 32, 16>(A, s) : launch_route<TYPE + kSingle, 32, 16>(A, s);
     else wide ? launch_route<TYPE, kLanes, 16>(A, s) : launch_route<TYPE + kSingle, kLanes, 16>(A, s);
 }
 
@@ -275,15 +281,18 @@ template <int TYPE, int LANES, int VALUES>
 void launch_route_grad(const RouteArgs &A, hipStream_t s)
 {
     const dim3 grid((unsigned)std::min((A.n + kThreads / LANES - 1) / (kThreads / LANES), kMaxGrid));
-    hipLaunchKernelGGL((row_route_grad_kernel<TYPE, LANES, VALUES>), grid, dim3(kThreads), 0, s, A);
+    if (A.k <= 8) hipLaunchKernelGGL((row_route_grad_kernel<TYPE, LANES, VALUES, 8>), grid, dim3(kThreads), 0, s, A);
+    else hipLaunchKernelGGL((row_route_grad_kernel<TYPE, LANES, VALUES, REGOT_ROW_MAX_CHOICES>), grid, dim3(kThreads), 0, s, A);
 }
 
 template <int TYPE>
 void launch_route_grad(const RouteArgs &A, hipStream_t s)
 {
-    if (A.m <= 64) launch_route_grad<TYPE + kSingle, 16, 4>(A, s);
+    if (A.m <= 32) launch_route_grad<TYPE + kSingle, 8, 4>(A, s);
+    else if (A.m <= 64) launch_route_grad<TYPE, 8, 8>(A, s);
     else if (A.m <= 128) launch_route_grad<TYPE, 16, 8>(A, s);
     else if (A.m <= 256) launch_route_grad<TYPE, 16, 16>(A, s);
+    else if (A.m <= 512) launch_route_grad<TYPE, 32, 16>(A, s);
     else launch_route_grad<TYPE, kLanes, 16>(A, s);
 }
 

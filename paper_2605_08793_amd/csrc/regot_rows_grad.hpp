@@ -102,8 +102,8 @@ __global__ __launch_bounds__(Team<WAVES>::kBlock) void row_logprob_grad_kernel(R
 //
 // The sum over a row comes before its first gradient, so a row is read twice (PARTS: here, and by the kernel that left the sums
 // of its parts).  Backwards the second time: the last stretch of VECS loads a thread is still in registers, the first KEPT loads of the one before are in
-// LDS, and what is before that is likeliest in the caches.  Bound by traffic: 4096 x 131072 bf16 441 us for 2.1 GB that have to move and 0.5 that is
-// read again (6.1 TB/s); 518 without KEPT.  Shorter rows by the chain of each row (target, sum, loss, list) and the rows under way.
+// LDS, and what is before that is likeliest in the caches.  Bound by traffic: 4096 x 131072 bf16 431 us for 2.1 GB that have to move and 0.5 that is
+// read again (6.2 TB/s); 513 without KEPT.  Shorter rows by the chain of each row (target, sum, loss, list) and the rows under way.
 // LIST: the room for a row's entries (a wave a row: 128 where they fit, 16384 x 400 fp32 24.2 us with 1024 and 21.2 with 128).
 template <int TYPE, int WAVES, int VECS, int KEPT, bool PARTS, int LIST = REGOT_ROW_MAX_LIST>
 __global__ __launch_bounds__(Team<WAVES>::kBlock) void row_distill_kernel(RowArgs A)

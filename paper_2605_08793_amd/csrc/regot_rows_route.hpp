@@ -3,8 +3,8 @@
 // A row is LANES lanes', which hold VALUES of its scores each; a wave has 64 / LANES rows, a workgroup four waves.  The k best
 // come out of a network without branches: each lane sorts what it has to a list of its KEPT best, and lists of
 // pairs of lanes are merged until every lane has the row's.  Keys and columns are one number, so that ties need nothing
-// of their own.  Bound by instructions: 890 of the vector unit for four rows of 256 (the network of 8 of 16 values about 400, keys and scores
-// the rest), 1030 with groups.  65536 rows of 256 fp32 scores 27 us, sigmoid in 8 groups 36 us, where reading them takes 10; a wave a row and k rounds
+// of their own.  Bound by instructions: 870 of the vector unit for four rows of 256 (the network of 8 of 16 values about 380, keys and scores
+// the rest), 1010 with groups.  65536 rows of 256 fp32 scores 27 us, sigmoid in 8 groups 36 us, where reading them takes 10; a wave a row and k rounds
 // of the largest left: choice and gradient 323 us, now 56.
 #pragma once
 
@@ -78,16 +78,28 @@ __device__ __forceinline__ void merge_down(double *a)
     }
 }
 
+// Batcher's odd-even merge sort: 19 comparisons for 8 values, where merges of sequences that rise and fall take 24.
+// (even_odd: every STEP-th of COUNT values, both halves of which are in descending order)
+template <int COUNT, int STEP>
+__device__ __forceinline__ void even_odd(double *a)
+{
+    if constexpr (2 * STEP < COUNT) {
+        even_odd<COUNT, 2 * STEP>(a);
+        even_odd<COUNT, 2 * STEP>(a + STEP);
+#pragma unroll
+        for (int i = STEP; i + STEP < COUNT; i += 2 * STEP) in_order(a[i], a[i + STEP]);
+    } else {
+        in_order(a[0], a[STEP]);
+    }
+}
+
 template <int COUNT>
 __device__ __forceinline__ void sort_down(double *a)
 {
     if constexpr (COUNT > 1) {
         sort_down<COUNT / 2>(a);
         sort_down<COUNT / 2>(a + COUNT / 2);
-#pragma unroll
-        for (int i = 0; i < COUNT / 2; ++i) in_order(a[i], a[COUNT - 1 - i]);
-        merge_down<COUNT / 2>(a);
-        merge_down<COUNT / 2>(a + COUNT / 2);
+        even_odd<COUNT, 1>(a);
     }
 }
 
@@ -111,7 +123,9 @@ __device__ __forceinline__ float row_all(float v)
     v = Op::apply(v, dpp_f32<kDppXor1>(v));
     v = Op::apply(v, dpp_f32<kDppXor2>(v));
     v = Op::apply(v, dpp_f32<kDppHalfMirror>(v));
-    return Op::apply(v, dpp_f32<kDppMirror>(v));
+    if constexpr (LANES > 8) v = Op::apply(v, dpp_f32<kDppMirror>(v));
+    if constexpr (LANES == 32) v = Op::apply(v, __shfl_xor(v, 16));
+    return v;
 }
 
 // Where column j of a row is kept in LDS: rows of 16 apart by four more, so that lanes that go through neighbouring groups do not
@@ -320,11 +334,9 @@ __global__ __launch_bounds__(kThreads) void row_route_kernel(RouteArgs A)
         merge_lists<KEPT>(best, [&](int i) { return dpp_f64<kDppXor1>(best[i]); });
         merge_lists<KEPT>(best, [&](int i) { return dpp_f64<kDppXor2>(best[i]); });
         merge_lists<KEPT>(best, [&](int i) { return dpp_f64<kDppHalfMirror>(best[i]); });
-        merge_lists<KEPT>(best, [&](int i) { return dpp_f64<kDppMirror>(best[i]); });
-        if constexpr (LANES == kLanes) {
-            merge_lists<KEPT>(best, [&](int i) { return __shfl_xor(best[i], 16); });
-            merge_lists<KEPT>(best, [&](int i) { return __shfl_xor(best[i], 32); });
-        }
+        if constexpr (LANES > 8) merge_lists<KEPT>(best, [&](int i) { return dpp_f64<kDppMirror>(best[i]); });
+        if constexpr (LANES > 16) merge_lists<KEPT>(best, [&](int i) { return __shfl_xor(best[i], 16); });
+        if constexpr (LANES == kLanes) merge_lists<KEPT>(best, [&](int i) { return __shfl_xor(best[i], 32); });
         constexpr int kRounds = (KEPT + LANES - 1) / LANES;
         int column[kRounds];
         float w[kRounds], at_chosen[kRounds], sum = 0.f;
@@ -353,16 +365,17 @@ __global__ __launch_bounds__(kThreads) void row_route_kernel(RouteArgs A)
 }
 
 // dS at given choices: the row's scores again, the chosen columns' parts through LDS, one read and one write of the row.  Bound by
-// memory: 65536 x 256 fp32, 8 choices 22-24 us = 5.6-5.9 TB/s of reads and writes.
-template <int TYPE, int LANES, int VALUES>
+// memory: 65536 x 256 fp32, 8 choices 22-23 us = 5.8-6.1 TB/s of reads and writes.
+// LIST: the room for a row's choices (8 or all there can be: 65536 x 64 fp32, 2 choices 5.5 us and 6.9).
+template <int TYPE, int LANES, int VALUES, int LIST>
 __global__ __launch_bounds__(kThreads) void row_route_grad_kernel(RouteArgs A)
 {
     using T = Score<TYPE>;
     using Row = RouteRow<TYPE, LANES, VALUES>;
-    constexpr int kRows = kThreads / LANES, kRounds = (REGOT_ROW_MAX_CHOICES + LANES - 1) / LANES;
+    constexpr int kRows = kThreads / LANES, kRounds = (LIST + LANES - 1) / LANES;
     __shared__ float held[kRows][Row::kColumns];
-    __shared__ uint32_t listed[kRows][REGOT_ROW_MAX_CHOICES];
-    __shared__ float gradient[kRows][REGOT_ROW_MAX_CHOICES];
+    __shared__ uint32_t listed[kRows][LIST];
+    __shared__ float gradient[kRows][LIST];
     const int at = threadIdx.x / LANES;
     const Row R{A.m, (int)(threadIdx.x % LANES)};
     for (int64_t row0 = (int64_t)blockIdx.x * kRows; row0 < A.n; row0 += (int64_t)gridDim.x * kRows) {

@@ -65,7 +65,8 @@ def inputs(n, m, dtype, seed, bias):
 
 
 SHAPES = [(1, 1, 1), (3, 2, 2), (5, 8, 2), (100, 16, 4), (7, 17, 5), (1000, 60, 4), (9, 63, 8), (130, 64, 6), (33, 65, 1), (1, 256, 8),
-          (500, 256, 8), (20, 257, 16), (40, 511, 10), (9, 1000, 32), (3, 1024, 32)]
+          (500, 256, 8), (20, 257, 16), (40, 511, 10), (9, 1000, 32), (3, 1024, 32),
+          (70, 32, 20), (40, 64, 32), (4100, 64, 3), (5000, 128, 8), (4200, 101, 20), (4096, 127, 4), (30, 300, 32), (50, 512, 3)]
 
 
 @pytest.mark.parametrize("n,m,k", SHAPES)
@@ -80,7 +81,8 @@ def test_sizes(n, m, k, score, dtype):
 
 
 @pytest.mark.parametrize("m,groups,kept,k", [(8, 4, 2, 3), (60, 6, 2, 5), (64, 64, 10, 8), (256, 8, 4, 8), (256, 8, 8, 8), (96, 3, 1, 20), (1024, 32, 5, 32),
-                                             (160, 8, 3, 6), (990, 9, 4, 12)])
+                                             (160, 8, 3, 6), (990, 9, 4, 12), (64, 8, 3, 8), (32, 32, 9, 4), (512, 8, 4, 10), (333, 3, 2, 5), (111, 37, 20, 9),
+                                             (480, 60, 13, 17)])
 @pytest.mark.parametrize("group_by", ["max", "top2"])
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
 def test_groups(m, groups, kept, k, group_by, score):
@@ -91,6 +93,19 @@ def test_groups(m, groups, kept, k, group_by, score):
                 break
         op = route(S.cuda(), k, None if bias is None else bias.cuda(), bias_on, score=score, groups=groups, groups_kept=kept, group_by=group_by)
         check(S, op, k, bias, bias_on, score, groups, kept, group_by, True, 1.0, f"{m} in {groups}, {bias_on}")
+
+
+@pytest.mark.parametrize("m,groups,kept,k", [(128, 8, 4, 8), (120, 15, 4, 20), (72, 3, 1, 3), (100, 50, 11, 6)])
+@pytest.mark.parametrize("group_by", ["max", "top2"])
+def test_groups_of_many_rows(m, groups, kept, k, group_by):
+    # each row is copied 90 times, so that the group values of 50 rows have to be apart
+    for seed in range(20):
+        S, bias = inputs(50, m, torch.float32, m + 100 * seed, 0.1)
+        if ref.route_keys(S, bias, "score", "sigmoid", groups, kept, group_by)[1] > 1e-5:
+            break
+    S = S.repeat(90, 1)
+    op = route(S.cuda(), k, bias.cuda(), "score", score="sigmoid", groups=groups, groups_kept=kept, group_by=group_by)
+    check(S, op, k, bias, "score", "sigmoid", groups, kept, group_by, True, 1.0, f"{m} in {groups}")
 
 
 def test_ties_go_to_the_lower_index():
