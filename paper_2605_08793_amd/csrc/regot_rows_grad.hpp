@@ -104,9 +104,11 @@ __global__ __launch_bounds__(Team<WAVES>::kBlock) void row_logprob_grad_kernel(R
 // of its parts).  Backwards the second time: the last stretch of VECS loads a thread is still in registers, the first KEPT loads of the one before are in
 // LDS, and what is before that is likeliest in the caches.  Bound by traffic: 4096 x 131072 bf16 431 us for 2.1 GB that have to move and 0.5 that is
 // read again (6.2 TB/s); 513 without KEPT.  Shorter rows by the chain of each row (target, sum, loss, list) and the rows under way.
+// Four waves to a SIMD, as the LDS allows, and columns that are computed where they are used: fp32 178 registers otherwise, and 40 of
+// them in memory with 16 waves (256 x 131072 fp32 71 us against 63, 999 x 33333 74 against 68).
 // LIST: the room for a row's entries (a wave a row: 128 where they fit, 16384 x 400 fp32 24.2 us with 1024 and 21.2 with 128).
 template <int TYPE, int WAVES, int VECS, int KEPT, bool PARTS, int LIST = REGOT_ROW_MAX_LIST>
-__global__ __launch_bounds__(Team<WAVES>::kBlock) void row_distill_kernel(RowArgs A)
+__global__ __launch_bounds__(Team<WAVES>::kBlock, KEPT > 0 ? 4 : 1) void row_distill_kernel(RowArgs A)
 {
     using T = Score<TYPE>;
     using Row = Team<WAVES>;
@@ -168,7 +170,7 @@ __global__ __launch_bounds__(Team<WAVES>::kBlock) void row_distill_kernel(RowArg
                         float x[kVecsOfGroup * T::kVec];
 #pragma unroll
                         for (int v = 0; v < kVecsOfGroup; ++v) {
-                            const uint32_t j = j0 + (g * kVecsOfGroup + v) * kStep + thread * T::kVec;
+                            const uint32_t j = here(j0 + (g * kVecsOfGroup + v) * kStep + thread * T::kVec);
                             if (v > 0 && j0 + (g * kVecsOfGroup + v) * kStep >= end) {
 #pragma unroll
                                 for (int e = 0; e < T::kVec; ++e) x[v * T::kVec + e] = -kInf;
@@ -223,7 +225,7 @@ __global__ __launch_bounds__(Team<WAVES>::kBlock) void row_distill_kernel(RowArg
 #pragma unroll
             for (int u = 0; u < VECS; ++u) {
                 if (j0 + u * kStep >= end) continue;
-                const Span<TYPE> span(j0 + u * kStep + thread * T::kVec, A.m);
+                const Span<TYPE> span(here(j0 + u * kStep + thread * T::kVec), A.m);
                 if (span.own >= end) continue;
                 float x[T::kVec] = {};
                 if (!none) {
