@@ -215,12 +215,13 @@ struct Softmax {
     float max = -kInf, base = 0.f;  // base: what is subtracted, 0 while there is no maximum
     float sum = 0.f, weighted = 0.f;
 
-    // brings the sums to the maximum `to`, which is no less than max
+    // brings the sums to the maximum `to`, which is no less than max.  (Where f is 0 nothing is left of them; a mask of the type's
+    // lowest value makes d, or sum d, -inf there, and f times that a NaN.)
     __device__ __forceinline__ void raise(float to, float c)
     {
         const bool empty = max == -kInf;
         const float d = (max - to) * c, f = exp2_fast(d);
-        weighted = empty ? 0.f : f * fmaf(sum, d, weighted);
+        weighted = empty || f == 0.f ? 0.f : f * fmaf(sum, d, weighted);
         sum = empty ? 0.f : sum * f;
         max = to;
         base = to == -kInf ? 0.f : to;
