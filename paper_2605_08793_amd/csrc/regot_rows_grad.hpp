@@ -210,7 +210,10 @@ __global__ __launch_bounds__(Team<WAVES>::kBlock, KEPT > 0 ? 4 : 1) void row_dis
         }
         loss = Row::template all<OpSumF>(loss, team_lds + 2 * WAVES);
         if (thread == 0 && begin == 0) A.loss[row] = bad ? kNan : loss;
-        if (!out) continue;
+        if (!out) {
+            Row::sync();  // the loss's sums are read
+            continue;
+        }
         const auto p_weighted = [&](float x) { return exp2_fast((x - max) * A.log2_scale) * of_p; };
         // backwards: the columns read last are still here, those before them in the caches
         const int stretches = (int)((end - begin + VECS * kStep - 1) / (VECS * kStep));
