@@ -575,7 +575,10 @@ enum { REGOT_F32 = 0, REGOT_BF16 = 1, REGOT_F16 = 2 };
  *                              and their ln p; -1 and -inf where the row has fewer that are not forbidden
  * targets = 0 (target and logprob may be NULL) and k = 0 (top_* may be NULL) leave that part out.
  * 0 <= targets <= REGOT_ROW_MAX_LIST, 0 <= k <= REGOT_ROW_MAX_TOP.  S is read once, and the few blocks of it that hold the
- * alternatives a second time (a row of many equal scores up to three times).  eta has to be such that 1 / eta is an fp32 number other than 0.
+ * alternatives a second time.  Rows whose alternatives cannot be told from a few maxima are looked through again, from the caches where they
+ * fit: rows of up to 2048 (fp32) or 4096 columns, where they have many equal scores or k is near the number of their 16-byte blocks
+ * or of 128, at most 30 times; longer ones of many equal scores twice, and where that is not enough (about k > 60), in part once for each
+ * alternative.  eta has to be such that 1 / eta is an fp32 number other than 0.
  */
 #define REGOT_ROW_MAX_LIST 1024
 #define REGOT_ROW_MAX_TOP 128

@@ -224,6 +224,68 @@ __device__ __forceinline__ void each_from(const RowScores<TYPE, BIAS> &scores, u
     }
 }
 
+// The k best of a row of at most VECS loads a lane, by a wave: the k-th largest by bisection over the scores in their order, two
+// bits a round, each round counting over the row again (from the caches, so that no registers are held for it): 16 bits
+// first, the rest if more than HELD columns are still in, then over the columns that have the score that all k are at or above.
+// push(is, a) is called by all lanes at once, for at most HELD columns in all, the k best among them.
+template <int HELD, int VECS, int TYPE, bool BIAS, typename F>
+__device__ __forceinline__ void best_by_bisection(const RowScores<TYPE, BIAS> &scores, int k, uint32_t at, F push)
+{
+    using T = Score<TYPE>;
+    constexpr uint32_t kStep = kLanes * T::kVec;
+    constexpr int kAtOnce = VECS < 8 ? 1 : 2;  // loads in flight (4: 169 registers where the rest of the kernel has 155)
+    const auto each = [&](auto look) {
+#pragma unroll 1
+        for (uint32_t begin = 0; begin < scores.m; begin += kAtOnce * kStep) {
+            const uint32_t j0 = here(begin + at);
+            float x[kAtOnce][T::kVec];
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) scores.read(j0 + u * kStep, x[u]);
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) {
+                const uint32_t first = Span<TYPE>(j0 + u * kStep, scores.m).first;
+#pragma unroll
+                for (int e = 0; e < T::kVec; ++e) look(ordered(x[u][e] + 0.f), first + e);
+            }
+        }
+    };
+    const auto count = [&](auto in) {
+        int have = 0;
+        each([&](uint32_t o, uint32_t column) { have += __builtin_popcountll(__ballot(in(o, column))); });
+        return have;
+    };
+    // the two bits of v above `shift`: how many of v + 1, 2, 3 << shift hold(.) is true of
+    const auto two_bits = [&](uint32_t &v, int shift, auto in, auto hold) {
+        int have[3] = {0, 0, 0};
+        const uint32_t step = 1u << shift, base = v;
+        each([&](uint32_t o, uint32_t column) {
+#pragma unroll
+            for (int q = 0; q < 3; ++q) have[q] += __builtin_popcountll(__ballot(in(o, column, base + (q + 1) * step)));
+        });
+        for (int q = 0; q < 3; ++q) v += hold(have[q]) ? step : 0;
+    };
+    constexpr uint32_t kLeast = 0x00800000u;  // (-inf, which is forbidden, comes just before)
+    uint32_t least = 0, last = 0xffffffffu;   // k columns are at or above `least`; of those equal to it, columns up to `last` are taken
+    const auto reach = [](uint32_t o, uint32_t, uint32_t middle) { return o >= middle; };
+    const auto enough = [&](int have) { return have >= k; };
+#pragma unroll 1
+    for (int shift = 30; shift >= 0; shift -= 2) {
+        if (shift == 14 && count([&](uint32_t o, uint32_t) { return o >= max(least, kLeast); }) <= HELD) break;
+        two_bits(least, shift, reach, enough);
+    }
+    least = max(least, kLeast);
+    if (count([&](uint32_t o, uint32_t) { return o >= least; }) > HELD) {
+        // the largest number below which fewer equal columns are than are wanted: that column is the last one
+        const int wanted = k - count([&](uint32_t o, uint32_t) { return o > least; });
+        last = 0;
+#pragma unroll 1
+        for (int shift = (cbits((int64_t)VECS * kStep) - 1) / 2 * 2; shift >= 0; shift -= 2)
+            two_bits(last, shift, [&](uint32_t o, uint32_t column, uint32_t middle) { return o == least && column < middle; },
+                     [&](int have) { return have < wanted; });
+    }
+    each([&](uint32_t o, uint32_t column) { push(o > least || (o == least && column <= last), (uint64_t)o << 32 | (uint32_t)~column); });
+}
+
 struct TopShared {
     float lane_max[kThreads];
     uint32_t hot[kThreads], block[kList];
@@ -491,71 +553,71 @@ __global__ __launch_bounds__(kThreads) void row_logprob_narrow_kernel(RowArgs A)
             // as in best_columns, with two maxima a lane for the bound, and (load, lane) for (block, thread)
             int count = 0;
             if (!out.bad && !out.none) {
-                constexpr int kHalves = VECS == 1 ? 1 : 2;
-                float half[kHalves];
-#pragma unroll
-                for (int u = 0; u < VECS; ++u) half[u % kHalves] = u < kHalves ? top[u] : max_nan(half[u % kHalves], top[u]);
-                const float bound = kth_largest_bound(half, A.k);
-                int pairs = 0;
-                wave_lds();
-#pragma unroll
-                for (int u = 0; u < VECS; ++u) {
-                    const bool is = top[u] >= bound && top[u] > -kInf;
+                const auto push = [&](bool is, uint64_t a) {
                     const uint64_t mask = __ballot(is);
-                    if (is) pair[wave][pairs + lanes_below(mask)] = u * kLanes + lane;
-                    pairs += __builtin_popcountll(mask);
-                }
+                    const int to = count + lanes_below(mask);
+                    if (is && to < kHeld) list[wave][to] = a;
+                    count += __builtin_popcountll(mask);
+                };
+                // Where k is more than three quarters of the maxima that the bound comes from (13 of 16 for 8 loads, whose rounds of
+                // counting are longer), so many columns of ordinary scores pass it that counting is faster, or does not
+                // even fit the list.  us, 8192 rows bf16, bound / counting: 512 columns k = 49 21 / 22, k = 56 32 / 22; 2000 columns
+                // k = 96 77 / 95, k = 104 96 / 95, k = 105 (some lists too short) over 150 / 95; 4096 columns k = 96 83 / 158, k = 104 115 / 158.
+                constexpr int kHalves = VECS == 1 ? 1 : 2;
+                const int maxima = min((A.m + T::kVec - 1) / T::kVec, (uint32_t)kHalves * kLanes);
+                bool found = T::kVec == 1 || 16 * A.k <= (VECS == 8 ? 13 : 12) * maxima;
                 wave_lds();
-                for (int i0 = 0; i0 < pairs; i0 += kLanes) {
-                    float x[T::kVec];
-                    uint32_t first = 0;
-                    if (i0 + lane < pairs) {
-                        const uint32_t j = pair[wave][i0 + lane] * T::kVec;
-                        scores.read(j, x);
-                        first = Span<TYPE>(j, A.m).first;
-                    }
+                if (found) {
+                    float half[kHalves];
 #pragma unroll
-                    for (int e = 0; e < T::kVec; ++e) {
-                        const bool is = i0 + lane < pairs && x[e] >= bound && x[e] > -kInf;
+                    for (int u = 0; u < VECS; ++u) half[u % kHalves] = u < kHalves ? top[u] : max_nan(half[u % kHalves], top[u]);
+                    const float bound = kth_largest_bound(half, A.k);
+                    int pairs = 0;
+#pragma unroll
+                    for (int u = 0; u < VECS; ++u) {
+                        const bool is = top[u] >= bound && top[u] > -kInf;
                         const uint64_t mask = __ballot(is);
-                        const int to = count + lanes_below(mask);
-                        if (is && to < kHeld) list[wave][to] = alternative(x[e], first + e);
-                        count += __builtin_popcountll(mask);
+                        if (is) pair[wave][pairs + lanes_below(mask)] = u * kLanes + lane;
+                        pairs += __builtin_popcountll(mask);
                     }
-                }
-                wave_lds();
-                if (count <= kHeld) {
-                    rank_all(list[wave], count, lane, kLanes, A.k, [&](int rank, uint64_t a) { out.top(rank, a); });
-                } else {
-                    uint64_t mine = best_before(scores, ~0ull, lane, kLanes);
-                    int better = 0;
-                    for (int l = 0; l < kLanes; ++l) better += __shfl((unsigned long long)mine, l) > mine;
-                    const uint64_t kth = __ballot(better == A.k - 1 && mine != 0);
-                    const uint64_t from = kth != 0 ? __shfl((unsigned long long)mine, __builtin_ctzll(kth)) : kForbidden;
-                    if (lane == 0) counts[wave] = 0;
                     wave_lds();
-                    each_from(scores, from, lane, kLanes, [&](uint64_t a) {
-                        const int to = atomicAdd(&counts[wave], 1);
-                        if (to < kHeld) list[wave][to] = a;
-                    });
-                    wave_lds();
-                    count = counts[wave];
-                    uint64_t last = ~0ull;
-                    if (count <= kHeld) {
-                        rank_all(list[wave], count, lane, kLanes, A.k, [&](int rank, uint64_t a) { out.top(rank, a); });
-                    } else
-                    for (count = 0; count < A.k; ++count) {
-                        uint64_t best = best_before(scores, last, lane, kLanes);
-#pragma unroll
-                        for (int d = 1; d < kLanes; d *= 2) {
-                            const uint64_t other = __shfl_xor((unsigned long long)best, d);
-                            best = other > best ? other : best;
+                    for (int i0 = 0; i0 < pairs; i0 += kLanes) {
+                        float x[T::kVec];
+                        uint32_t first = 0;
+                        if (i0 + lane < pairs) {
+                            const uint32_t j = pair[wave][i0 + lane] * T::kVec;
+                            scores.read(j, x);
+                            first = Span<TYPE>(j, A.m).first;
                         }
-                        if (best == 0) break;
-                        if (lane == 0) out.top(count, best);
-                        last = best;
+#pragma unroll
+                        for (int e = 0; e < T::kVec; ++e) push(i0 + lane < pairs && x[e] >= bound && x[e] > -kInf, alternative(x[e], first + e));
+                    }
+                    wave_lds();
+                    found = count <= kHeld;
+                    // (of equal scores, the bound by columns too would leave kVec for each of the k)
+                    if (!found && (A.k - 1) * T::kVec < kHeld) {
+                        const uint64_t mine = best_before(scores, ~0ull, lane, kLanes);
+                        int better = 0;
+                        for (int l = 0; l < kLanes; ++l) better += __shfl((unsigned long long)mine, l) > mine;
+                        const uint64_t kth = __ballot(better == A.k - 1 && mine != 0);
+                        const uint64_t from = kth != 0 ? __shfl((unsigned long long)mine, __builtin_ctzll(kth)) : kForbidden;
+                        if (lane == 0) counts[wave] = 0;
+                        wave_lds();
+                        each_from(scores, from, lane, kLanes, [&](uint64_t a) {
+                            const int to = atomicAdd(&counts[wave], 1);
+                            if (to < kHeld) list[wave][to] = a;
+                        });
+                        wave_lds();
+                        count = counts[wave];
+                        found = count <= kHeld;
                     }
                 }
+                if (!found) {
+                    count = 0;
+                    best_by_bisection<kHeld, VECS>(scores, A.k, at, push);
+                    wave_lds();
+                }
+                rank_all(list[wave], count, lane, kLanes, A.k, [&](int rank, uint64_t a) { out.top(rank, a); });
             }
             for (int i = count + lane; i < A.k; i += kLanes) out.no_top(i);
         }
