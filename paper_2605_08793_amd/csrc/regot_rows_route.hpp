@@ -396,11 +396,19 @@ __global__ __launch_bounds__(kThreads) void row_route_grad_kernel(RouteArgs A)
 #pragma unroll
         for (int r = 0; r < kRounds; ++r) at_listed[r] = column[r] < A.m ? T::get(S[column[r]]) : 0.f;
         RouteScore score{A.score == REGOT_SIGMOID};
+        const bool sigmoid = score.sigmoid;
         float s[VALUES];
         score.template of_row<LANES>(x, s);
         float *const mine = held[at];
         float c[kRounds], Z = 0.f, gs = 0.f, any = 0.f;
         score(at_listed, c);
+        // sigmoid: s (1 - s), 1 - s being the score of -x (a difference of 1 and a score near it has lost its digits)
+        float slope[kRounds];
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) slope[r] = -at_listed[r];
+        score(slope, slope);
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) slope[r] = sigmoid ? slope[r] * c[r] : 1.f;
 #pragma unroll
         for (int r = 0; r < kRounds; ++r) {
             c[r] = column[r] < A.m ? c[r] : 0.f;
@@ -420,7 +428,7 @@ __global__ __launch_bounds__(kThreads) void row_route_grad_kernel(RouteArgs A)
             all += column[r] < A.m ? g[r] * c[r] : 0.f;
         }
         all = A.score == REGOT_SOFTMAX ? row_all<OpSumF, LANES>(all) : 0.f;
-        // each column's part, a column listed twice having the sum of its entries'
+        // each column's part (sigmoid: all of its gradient), a column listed twice having the sum of its entries'
 #pragma unroll
         for (int r = 0; r < kRounds; ++r) {
             const int i = r * LANES + R.l;
@@ -435,11 +443,10 @@ __global__ __launch_bounds__(kThreads) void row_route_grad_kernel(RouteArgs A)
             if (r * LANES >= A.k) continue;
             float sum = 0.f;
             for (int o = 0; o < A.k; ++o) sum += listed[at][o] == column[r] ? gradient[at][o] : 0.f;
-            if (column[r] < A.m) mine[column[r]] = sum;
+            if (column[r] < A.m) mine[column[r]] = sum * slope[r];
         }
         wave_lds();
         typename T::Raw *const out = static_cast<typename T::Raw *>(A.dS) + row * A.ldD;
-        const bool sigmoid = score.sigmoid;
 #pragma unroll
         for (int ch = 0; ch < Row::kChunks; ++ch) {
             const Span<TYPE> span = R.span(ch);
@@ -447,8 +454,8 @@ __global__ __launch_bounds__(kThreads) void row_route_grad_kernel(RouteArgs A)
             float d[T::kVec];
 #pragma unroll
             for (int e = 0; e < T::kVec; ++e) {
-                const float p = s[ch * T::kVec + e];
-                d[e] = p * (mine[span.first + e] * (sigmoid ? 1.f - p : 1.f) - all);  // (all: 0 for sigmoid)
+                const float own = mine[span.first + e];
+                d[e] = sigmoid ? own : s[ch * T::kVec + e] * (own - all);
             }
             if (any == 0.f) {
 #pragma unroll
