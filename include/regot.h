@@ -639,7 +639,8 @@ int regot_row_distill(int64_t n, int64_t m,
  *             REGOT_GROUP_MAX) or the sum of its two largest (REGOT_GROUP_TOP2), of s_ij in place of key_ij where bias is NULL; the groups_kept groups
  *             of largest value stay, the columns of the others are not chosen
  *     idx[i*k ..]     the k columns of largest key, the largest first; equal keys, and equal groups, by ascending index
- *     weight[i*k ..]  scale * s_ij, divided by the sum of the chosen s where renormalise = 1 (0 where that sum is 0): the bias only chooses
+ *     weight[i*k ..]  scale * s_ij, divided by the sum of the chosen s where renormalise = 1 (0 where that sum is 0, as it is for scores
+ *                     below the smallest normal fp32 number): the bias only chooses
  * Keys are compared as fp32 numbers.  A column whose score or key is -inf is not chosen and is left out of its group's value; idx is -1 and weight 0 where
  * fewer than k can be.  A row with a NaN key, or that has no softmax, has idx -1 and weight NaN.
  * 0 <= m <= REGOT_ROW_MAX_EXPERTS, 1 <= k <= REGOT_ROW_MAX_CHOICES, 1 <= groups_kept <= groups <= 64, groups divides m.

@@ -353,13 +353,14 @@ __global__ __launch_bounds__(kThreads) void row_route_kernel(RouteArgs A)
 #pragma unroll
         for (int r = 0; r < kRounds; ++r) sum += w[r] = column[r] < 0 ? 0.f : w[r];
         sum = row_all<OpSumF, LANES>(sum);
-        const float factor = !A.renormalise ? A.scale : sum > 0.f ? A.scale / sum : 0.f;
 #pragma unroll
         for (int r = 0; r < kRounds; ++r) {
             const int i = r * LANES + R.l;
             if (!there || i >= A.k) continue;
             A.idx[row * A.k + i] = column[r];
-            A.weight[row * A.k + i] = bad ? kNan : w[r] * factor;
+            // (divided first: scale / sum is beyond 32 bits for the smallest sums)
+            const float part = !A.renormalise ? w[r] : sum > 0.f ? w[r] / sum : 0.f;
+            A.weight[row * A.k + i] = bad ? kNan : part * A.scale;
         }
     }
 }
@@ -400,7 +401,7 @@ __global__ __launch_bounds__(kThreads) void row_route_grad_kernel(RouteArgs A)
         float s[VALUES];
         score.template of_row<LANES>(x, s);
         float *const mine = held[at];
-        float c[kRounds], Z = 0.f, gs = 0.f, any = 0.f;
+        float c[kRounds], Z = 0.f, any = 0.f;
         score(at_listed, c);
         // sigmoid: s (1 - s), 1 - s being the score of -x (a difference of 1 and a score near it has lost its digits)
         float slope[kRounds];
@@ -408,27 +409,38 @@ __global__ __launch_bounds__(kThreads) void row_route_grad_kernel(RouteArgs A)
         for (int r = 0; r < kRounds; ++r) slope[r] = -at_listed[r];
         score(slope, slope);
 #pragma unroll
-        for (int r = 0; r < kRounds; ++r) slope[r] = sigmoid ? slope[r] * c[r] : 1.f;
-#pragma unroll
         for (int r = 0; r < kRounds; ++r) {
+            slope[r] = sigmoid ? slope[r] : 1.f;
             c[r] = column[r] < A.m ? c[r] : 0.f;
             Z += c[r];
-            gs += column[r] < A.m ? g[r] * c[r] : 0.f;
             any += column[r] < A.m ? 1.f : 0.f;
         }
         any = row_all<OpSumF, LANES>(any);
-        if (A.renormalise) {
-            Z = row_all<OpSumF, LANES>(Z);
-            gs = row_all<OpSumF, LANES>(gs) / Z;
-        }
         float all = 0.f;
+        if (A.renormalise) {
+            // the chosen columns' part (g - sum g c / Z) c / Z, with c / Z formed first (g / Z is beyond 32 bits for the smallest sums); softmax has
+            // nothing elsewhere: the parts add up to 0
+            Z = row_all<OpSumF, LANES>(Z);
+            float gs = 0.f;
 #pragma unroll
-        for (int r = 0; r < kRounds; ++r) {
-            if (A.renormalise) g[r] = column[r] < A.m && !(Z <= 0.f) ? (g[r] - gs) / Z : 0.f;
-            all += column[r] < A.m ? g[r] * c[r] : 0.f;
+            for (int r = 0; r < kRounds; ++r) {
+                c[r] = Z <= 0.f ? 0.f : c[r] / Z;
+                slope[r] *= c[r];
+                gs += column[r] < A.m ? g[r] * c[r] : 0.f;
+            }
+            gs = row_all<OpSumF, LANES>(gs);
+#pragma unroll
+            for (int r = 0; r < kRounds; ++r) g[r] -= gs;
+        } else if (sigmoid) {
+#pragma unroll
+            for (int r = 0; r < kRounds; ++r) slope[r] *= c[r];
+        } else {
+#pragma unroll
+            for (int r = 0; r < kRounds; ++r) all += column[r] < A.m ? g[r] * c[r] : 0.f;
+            all = row_all<OpSumF, LANES>(all);
         }
-        all = A.score == REGOT_SOFTMAX ? row_all<OpSumF, LANES>(all) : 0.f;
-        // each column's part (sigmoid: all of its gradient), a column listed twice having the sum of its entries'
+        const bool whole = sigmoid || A.renormalise;  // what is at a chosen column is all of its gradient
+        // each column's part, a column listed twice having the sum of its entries'
 #pragma unroll
         for (int r = 0; r < kRounds; ++r) {
             const int i = r * LANES + R.l;
@@ -455,7 +467,7 @@ __global__ __launch_bounds__(kThreads) void row_route_grad_kernel(RouteArgs A)
 #pragma unroll
             for (int e = 0; e < T::kVec; ++e) {
                 const float own = mine[span.first + e];
-                d[e] = sigmoid ? own : s[ch * T::kVec + e] * (own - all);
+                d[e] = whole ? own : s[ch * T::kVec + e] * (own - all);
             }
             if (any == 0.f) {
 #pragma unroll
