@@ -642,7 +642,7 @@ int regot_row_distill(int64_t n, int64_t m,
  *     weight[i*k ..]  scale * s_ij, divided by the sum of the chosen s where renormalise = 1 (0 where that sum is 0, as it is for scores
  *                     below the smallest normal fp32 number): the bias only chooses
  * Keys are compared as fp32 numbers.  A column whose score or key is -inf is not chosen and is left out of its group's value; idx is -1 and weight 0 where
- * fewer than k can be.  A row with a NaN key, or that has no softmax, has idx -1 and weight NaN.
+ * fewer than k can be.  A row with a NaN key, or a NaN or +inf that leaves it no softmax, has idx -1 and weight NaN; for sigmoid +inf is a score like any other (s = 1).
  * 0 <= m <= REGOT_ROW_MAX_EXPERTS, 1 <= k <= REGOT_ROW_MAX_CHOICES, 1 <= groups_kept <= groups <= 64, groups divides m.
  */
 #define REGOT_ROW_MAX_EXPERTS 1024
@@ -662,6 +662,8 @@ int regot_row_route(int64_t n, int64_t m,
  * The gradient of sum g_weight * weight to S at the choices idx (which are not differentiated, and may come from elsewhere): with
  * c the chosen columns, ds_c = scale g_c, or scale (g_c - sum_c g_c s_c / Z) / Z with Z = sum_c s_c where renormalise = 1 (0 where Z = 0),
  *     dS_ij = s_ij (ds_ij - sum_c ds_c s_c)   (softmax),     ds_ij s_ij (1 - s_ij)   (sigmoid),   ds = 0 outside c.
+ * A row that holds a NaN (softmax: or +inf) has the gradient NaN, whatever idx is; a row without choices otherwise 0, also where it was a NaN in the
+ * bias of regot_row_route, which is not looked at here, that left it none.
  */
 int regot_row_route_grad(int64_t n, int64_t m,
                          const void *S, int type, int64_t ldS, int score,

@@ -128,6 +128,16 @@ __device__ __forceinline__ float row_all(float v)
     return v;
 }
 
+// whether `is` holds in any of the LANES lanes of a row, in all of them
+template <int LANES>
+__device__ __forceinline__ bool row_any(bool is)
+{
+    const uint64_t lanes = __ballot(is);
+    if constexpr (LANES == kLanes) return lanes != 0;
+    else return (lanes >> ((threadIdx.x & (kLanes - 1)) / LANES * LANES) & ((1ull << LANES) - 1)) != 0;
+}
+__device__ __forceinline__ bool is_nan(float v) { return v != v; }
+
 // Where column j of a row is kept in LDS: rows of 16 apart by four more, so that lanes that go through neighbouring groups do not
 // meet, and 16 bytes stay together.
 __device__ __forceinline__ uint32_t place(uint32_t j) { return j + (j >> 4) * 4; }
@@ -212,7 +222,7 @@ __global__ __launch_bounds__(kThreads) void row_route_kernel(RouteArgs A)
     __shared__ __align__(16) float held[kRows][places(Row::kColumns)];
     __shared__ float value[kRows][kMaxGroups];
     __shared__ uint32_t shut[kRows][kMaxGroups];
-    const int lane = threadIdx.x & (kLanes - 1), at = threadIdx.x / LANES;
+    const int at = threadIdx.x / LANES;
     const Row R{A.m, (int)(threadIdx.x % LANES)};
     for (int64_t row0 = (int64_t)blockIdx.x * kRows; row0 < A.n; row0 += (int64_t)gridDim.x * kRows) {
         const bool there = row0 + at < A.n;
@@ -241,11 +251,7 @@ __global__ __launch_bounds__(kThreads) void row_route_kernel(RouteArgs A)
 #pragma unroll
             for (int v = 0; v < VALUES; ++v) key[v] = x[v];
         }
-        const float any_nan = largest(key);
-        bool bad = any_nan != any_nan;
-        bad |= score.inv != score.inv;
-        const uint64_t bad_lanes = __ballot(bad);
-        bad = LANES == kLanes ? bad_lanes != 0 : (bad_lanes >> (lane / LANES * LANES) & ((1ull << (LANES % kLanes)) - 1)) != 0;
+        const bool bad = row_any<LANES>(is_nan(largest(key)) || is_nan(score.inv));
         float *const mine = held[at];
         if (A.groups > 1 && A.m > 0) {
             wave_lds();
@@ -400,6 +406,7 @@ __global__ __launch_bounds__(kThreads) void row_route_grad_kernel(RouteArgs A)
         const bool sigmoid = score.sigmoid;
         float s[VALUES];
         score.template of_row<LANES>(x, s);
+        const bool bad = row_any<LANES>(is_nan(largest(x)) || is_nan(score.inv));  // (inv: a softmax with a score of +inf)
         float *const mine = held[at];
         float c[kRounds], Z = 0.f, any = 0.f;
         score(at_listed, c);
@@ -469,9 +476,9 @@ __global__ __launch_bounds__(kThreads) void row_route_grad_kernel(RouteArgs A)
                 const float own = mine[span.first + e];
                 d[e] = whole ? own : s[ch * T::kVec + e] * (own - all);
             }
-            if (any == 0.f) {
+            if (bad || any == 0.f) {
 #pragma unroll
-                for (int e = 0; e < T::kVec; ++e) d[e] = 0.f;
+                for (int e = 0; e < T::kVec; ++e) d[e] = bad ? kNan : 0.f;
             }
             span.store(out, d);
         }
