@@ -404,11 +404,13 @@ __global__ __launch_bounds__(kThreads) void row_route_grad_kernel(RouteArgs A)
         for (int r = 0; r < kRounds; ++r) at_listed[r] = column[r] < A.m ? T::get(S[column[r]]) : 0.f;
         RouteScore score{A.score == REGOT_SIGMOID};
         const bool sigmoid = score.sigmoid;
+        const bool nan = is_nan(largest(x));
         float s[VALUES];
         score.template of_row<LANES>(x, s);
-        const bool bad = row_any<LANES>(is_nan(largest(x)) || is_nan(score.inv));  // (inv: a softmax with a score of +inf)
+        const bool bad = row_any<LANES>(nan || is_nan(score.inv));  // (inv: a softmax with a score of +inf)
         float *const mine = held[at];
-        float c[kRounds], Z = 0.f, any = 0.f;
+        float c[kRounds], Z = 0.f;
+        bool any = false;
         score(at_listed, c);
         // sigmoid: s (1 - s), 1 - s being the score of -x (a difference of 1 and a score near it has lost its digits)
         float slope[kRounds];
@@ -420,22 +422,24 @@ __global__ __launch_bounds__(kThreads) void row_route_grad_kernel(RouteArgs A)
             slope[r] = sigmoid ? slope[r] : 1.f;
             c[r] = column[r] < A.m ? c[r] : 0.f;
             Z += c[r];
-            any += column[r] < A.m ? 1.f : 0.f;
+            any |= column[r] < A.m;
         }
-        any = row_all<OpSumF, LANES>(any);
+        any = row_any<LANES>(any);
         float all = 0.f;
         if (A.renormalise) {
-            // the chosen columns' part (g - sum g c / Z) c / Z, with c / Z formed first (g / Z is beyond 32 bits for the smallest sums); softmax has
-            // nothing elsewhere: the parts add up to 0
-            Z = row_all<OpSumF, LANES>(Z);
+            // the chosen columns' part (g - sum g c / Z) c / Z, with c / Z formed first (g / Z is beyond 32 bits for the smallest sums) and
+            // scores 2^40 times as large, so that g c and 1 / Z keep their digits; softmax has nothing elsewhere: the parts add up to 0
             float gs = 0.f;
 #pragma unroll
             for (int r = 0; r < kRounds; ++r) {
-                c[r] = Z <= 0.f ? 0.f : c[r] / Z;
-                slope[r] *= c[r];
+                c[r] *= 0x1p40f;
                 gs += column[r] < A.m ? g[r] * c[r] : 0.f;
             }
-            gs = row_all<OpSumF, LANES>(gs);
+            Z = row_all<OpSumF, LANES>(Z) * 0x1p40f;
+            const float inv_Z = Z <= 0.f ? 0.f : __builtin_amdgcn_rcpf(Z);
+            gs = row_all<OpSumF, LANES>(gs) * inv_Z;
+#pragma unroll
+            for (int r = 0; r < kRounds; ++r) slope[r] *= c[r] * inv_Z;
 #pragma unroll
             for (int r = 0; r < kRounds; ++r) g[r] -= gs;
         } else if (sigmoid) {
@@ -446,7 +450,10 @@ __global__ __launch_bounds__(kThreads) void row_route_grad_kernel(RouteArgs A)
             for (int r = 0; r < kRounds; ++r) all += column[r] < A.m ? g[r] * c[r] : 0.f;
             all = row_all<OpSumF, LANES>(all);
         }
-        const bool whole = sigmoid || A.renormalise;  // what is at a chosen column is all of its gradient
+        if (sigmoid || A.renormalise) {  // what is at a chosen column is all of its gradient
+#pragma unroll
+            for (int v = 0; v < VALUES; ++v) s[v] = 1.f;
+        }
         // each column's part, a column listed twice having the sum of its entries'
 #pragma unroll
         for (int r = 0; r < kRounds; ++r) {
@@ -468,15 +475,14 @@ __global__ __launch_bounds__(kThreads) void row_route_grad_kernel(RouteArgs A)
         typename T::Raw *const out = static_cast<typename T::Raw *>(A.dS) + row * A.ldD;
 #pragma unroll
         for (int ch = 0; ch < Row::kChunks; ++ch) {
-            const Span<TYPE> span = R.span(ch);
+            const Span<TYPE> span(here((uint32_t)(ch * LANES + R.l) * T::kVec), A.m);  // (R.span(ch), but nothing of it kept since the load: 80 registers, not 85)
             if (!there || span.own >= A.m) continue;
             float d[T::kVec];
 #pragma unroll
             for (int e = 0; e < T::kVec; ++e) {
-                const float own = mine[span.first + e];
-                d[e] = whole ? own : s[ch * T::kVec + e] * (own - all);
+                d[e] = s[ch * T::kVec + e] * (mine[span.first + e] - all);
             }
-            if (bad || any == 0.f) {
+            if (bad || !any) {
 #pragma unroll
                 for (int e = 0; e < T::kVec; ++e) d[e] = bad ? kNan : 0.f;
             }
