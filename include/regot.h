@@ -554,7 +554,8 @@ int regot_splr_direction(int64_t n, int64_t m,
  *   - `type` is the type of S and of a gradient dS: REGOT_F32, REGOT_BF16 or REGOT_F16.  Everything else is fp32 and
  *     int32; maxima, sums and exponents are held in fp32 and a gradient is rounded to its type once.  S and dS are row-major with
  *     leading dimensions ldS, ldD >= m in elements, aligned to their elements: 16-byte loads and stores are used wherever a row
- *     starts.  A gradient must not overlap S.
+ *     starts.  A gradient that shares an element with S is refused (REGOT_ERR_ARG); its rows may lie
+ *     between those of S.
  *   - Lists per row (targets, teacher entries, choices, alternatives) are dense arrays of n rows.  An index outside
  *     [0, m), such as -1, is no entry.  A column listed twice counts twice.
  *   - A score of -inf (a mask), or a bias of -inf, is a forbidden column: p = 0.  A row that has no other score (or m = 0) has no distribution: its

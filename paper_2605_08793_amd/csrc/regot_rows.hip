@@ -8,6 +8,7 @@
 #include <algorithm>
 
 #include "regot.h"
+#include "regot_overlap.hpp"
 #include "regot_rows_grad.hpp"
 #include "regot_rows_logprob.hpp"
 #include "regot_rows_route.hpp"
@@ -359,6 +360,7 @@ int regot_row_logprob_grad(int64_t n, int64_t m, const void *S, int type, int64_
         misaligned(g_entropy, 4) || misaligned(dS, element_bytes(type)))
         return REGOT_ERR_ALIGN;
     if (n == 0 || m == 0) return REGOT_OK;
+    if (overlap(n, m, S, ldS, dS, ldD, element_bytes(type))) return REGOT_ERR_ARG;
     RowArgs A = row_args(n, m, S, ldS, bias, eta);
     A.target = target;
     A.targets = targets;
@@ -398,6 +400,7 @@ int regot_row_distill(int64_t n, int64_t m, const void *S, int type, int64_t ldS
     if (misaligned(workspace, kAlign)) return REGOT_ERR_ALIGN;
     if (workspace_bytes < P.total) return REGOT_ERR_WORKSPACE;
     if (n == 0) return REGOT_OK;
+    if (dS && overlap(n, m, S, ldS, dS, ldD, element_bytes(type))) return REGOT_ERR_ARG;
     RowArgs A = row_args(n, m, S, ldS, nullptr, eta);
     A.target = t_idx;
     A.t_score = t_score;
@@ -461,6 +464,7 @@ int regot_row_route_grad(int64_t n, int64_t m, const void *S, int type, int64_t 
     if (ldD < m) return REGOT_ERR_LD;
     if (misaligned(idx, 4) || misaligned(g_weight, 4) || misaligned(dS, element_bytes(type))) return REGOT_ERR_ALIGN;
     if (n == 0 || m == 0) return REGOT_OK;
+    if (overlap(n, m, S, ldS, dS, ldD, element_bytes(type))) return REGOT_ERR_ARG;
     RouteArgs A{};
     A.n = n;
     A.m = (uint32_t)m;
