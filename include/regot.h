@@ -617,7 +617,9 @@ int regot_row_logprob_grad(int64_t n, int64_t m,
  *     loss[i] = sum_l q_il (ln q_il - ln p_ij),  j = t_idx[i*k + l]
  *     dS_ij   = (row_weight_i / eta) (p_ij - sum of q_il over l with t_idx = j)
  * t_score may be scores or log probabilities (top_idx and top_logprob of regot_row_logprob are a target): a constant added
- * to a row's list changes nothing.  row_weight [n] is d(total loss)/d loss_i, NULL for 1.  dS NULL: the loss alone.
+ * to a row's list changes nothing.  It is divided by the eta of this call, whatever it is: log probabilities are scores at temperature 1,
+ * also those of a regot_row_logprob at another eta, so that q is proportional to p of that call with eta = 1 here, and to p^(1/eta) otherwise.
+ * (The scores x at top_idx are top_logprob times the eta of that call, but for a constant.)  row_weight [n] is d(total loss)/d loss_i, NULL for 1.  dS NULL: the loss alone.
  * A row without entries, or whose entries all have the score -inf, is padding: loss 0, gradient 0, whatever S holds there.
  * A forbidden column that the target gives weight makes the loss +inf.
  * 1 <= k <= REGOT_ROW_MAX_LIST.

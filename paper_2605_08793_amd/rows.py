@@ -101,7 +101,9 @@ class RowDistill(_Rows):
         self._out = [_address(self.loss), _address(self.grad), self.m, _address(self.workspace), self.workspace.numel()]
 
     def distill(self, S, t_idx, t_score, eta=1.0, row_weight=None):
-        """t_idx (n, k) int32, -1 for no entry; t_score (n, k): the teacher's scores or log probabilities there."""
+        """t_idx (n, k) int32, -1 for no entry; t_score (n, k): the teacher's scores or log probabilities there, which are
+        divided by eta: log probabilities (RowLogprob.top_logprob, of whatever eta) are scores at temperature 1, and belong
+        to eta = 1, or are multiplied by their own eta first."""
         B._check(B.load().regot_row_distill(
             *self._scores(S), float(eta), B._list(t_idx, self.n, self.k, "t_idx", torch.int32),
             B._list(t_score, self.n, self.k, "t_score"), self.k, B._list(row_weight, self.n, 1, "row_weight", optional=True),
