@@ -4,8 +4,8 @@ The model's side of the plan that the solver works on: `RowLogprob` gives log pr
 and the best columns of each row under column duals (`bias`), `RowDistill` the loss of a model's rows against such sparse
 targets with its gradient, `RowRoute` the k columns (experts) that each row goes to, with their weights.  As in the driver,
 no arithmetic happens here, and the results stay on the device, in buffers that the next call of the same object writes
-again.  (The buffers' addresses are looked up once, which is a fifth of a small call: an object writes to the buffers that it was made with, also
-where another tensor has been assigned to their name.)
+again.  (The buffers' addresses are looked up once, which is a fifth of a small call: the outputs cannot be replaced by
+other tensors.  Only .dS can be, by a tensor that `grad` checks at each call.)  Before the first call they hold anything.
 """
 import torch
 
@@ -14,6 +14,10 @@ from . import binding as B
 
 def _address(t):
     return 0 if t is None else t.data_ptr()
+
+
+def _output(name):
+    return property(lambda self: getattr(self, name), doc="a buffer of the object, which its calls write")
 
 
 class _Rows:
@@ -26,13 +30,13 @@ class _Rows:
         self.device = torch.empty(0, device=device).device
         self._kept = []
 
-    def _buffer(self, *shape, dtype=torch.float32, zeros=True):
-        t = (torch.zeros if zeros else torch.empty)(*shape, dtype=dtype, device=self.device)
+    def _buffer(self, *shape, dtype=torch.float32):
+        t = torch.empty(*shape, dtype=dtype, device=self.device)
         self._kept.append(t)
         return t
 
     def _workspace(self, size):
-        return self._buffer(max(size, 256), dtype=torch.uint8, zeros=False)
+        return self._buffer(max(size, 256), dtype=torch.uint8)
 
     def _scores(self, S):
         """(n, m, address, type, leading dimension) of a call's scores, which have to be of the object's size, type and device."""
@@ -43,7 +47,7 @@ class _Rows:
 
     def _gradient(self, S):
         if self.dS is None:
-            self.dS = self._buffer(self.n, self.m, dtype=self.dtype, zeros=False)
+            self.dS = self._buffer(self.n, self.m, dtype=self.dtype)
         return B._same_scores(self.dS, S)[::-1]
 
 
@@ -52,16 +56,18 @@ class RowLogprob(_Rows):
 
     After `logprob`: .logprob_out (n, targets), .entropy (n), .stats (n, 2: the maximum, and the logarithm of the sum
     relative to it), .top_idx and .top_logprob (n, k).  After `grad`: .dS (n, m)."""
+    logprob_out, entropy, stats, top_idx, top_logprob = map(_output, ("_logprob_out", "_entropy", "_stats", "_top_idx", "_top_logprob"))
+    workspace = _output("_work")
 
     def __init__(self, n: int, m: int, k: int = 0, targets: int = 1, dtype=torch.bfloat16, device="cuda"):
         super().__init__(n, m, dtype, device)
         self.k, self.targets = int(k), int(targets)
-        self.workspace = self._workspace(B.regot_row_logprob_workspace_bytes(n, m, k))
-        self.logprob_out = self._buffer(n, targets) if targets else None
-        self.entropy = self._buffer(n)
-        self.stats = self._buffer(n, 2)
-        self.top_idx = self._buffer(n, k, dtype=torch.int32) if k else None
-        self.top_logprob = self._buffer(n, k) if k else None
+        self._work = self._workspace(B.regot_row_logprob_workspace_bytes(n, m, k))
+        self._logprob_out = self._buffer(n, targets) if targets else None
+        self._entropy = self._buffer(n)
+        self._stats = self._buffer(n, 2)
+        self._top_idx = self._buffer(n, k, dtype=torch.int32) if k else None
+        self._top_logprob = self._buffer(n, k) if k else None
         self.dS = None
         self._out = [_address(t) for t in (self.logprob_out, self.entropy, self.stats, self.top_idx, self.top_logprob, self.workspace)]
         self._out.append(self.workspace.numel())
@@ -91,13 +97,14 @@ class RowDistill(_Rows):
     """Loss of n rows of m scores against lists of k teacher entries, with the gradient (unless grad=False).
 
     After `distill`: .loss (n), .grad (n, m) of S's type."""
+    loss, grad, workspace = map(_output, ("_loss", "_grad", "_work"))
 
     def __init__(self, n: int, m: int, k: int, dtype=torch.bfloat16, device="cuda", grad=True):
         super().__init__(n, m, dtype, device)
         self.k = int(k)
-        self.workspace = self._workspace(B.regot_row_distill_workspace_bytes(n, m, k))
-        self.loss = self._buffer(n)
-        self.grad = self._buffer(n, m, dtype=dtype, zeros=False) if grad else None
+        self._work = self._workspace(B.regot_row_distill_workspace_bytes(n, m, k))
+        self._loss = self._buffer(n)
+        self._grad = self._buffer(n, m, dtype=dtype) if grad else None
         self._out = [_address(self.loss), _address(self.grad), self.m, _address(self.workspace), self.workspace.numel()]
 
     def distill(self, S, t_idx, t_score, eta=1.0, row_weight=None):
@@ -112,6 +119,7 @@ class RowDistill(_Rows):
 
 class RowRoute(_Rows):
     """The k columns of n rows of m scores, and their weights: .idx, .weight (n, k); .dS (n, m) after `grad`."""
+    idx, weight = map(_output, ("_idx", "_weight"))
 
     def __init__(self, n: int, m: int, k: int, score="softmax", bias_on=None, groups=1, groups_kept=1, group_by="max",
                  renormalise=True, scale=1.0, dtype=torch.float32, device="cuda"):
@@ -120,8 +128,8 @@ class RowRoute(_Rows):
         self._score, self._bias_on = B.SCORE_KINDS[score], B.BIAS_ON[bias_on]
         self._choose = self._bias_on, self._score, int(groups), int(groups_kept), B.GROUP_BY[group_by], self.k
         self._weigh = int(bool(renormalise)), float(scale)
-        self.idx = self._buffer(n, k, dtype=torch.int32)
-        self.weight = self._buffer(n, k)
+        self._idx = self._buffer(n, k, dtype=torch.int32)
+        self._weight = self._buffer(n, k)
         self.dS = None
         self._out = self.idx.data_ptr(), self.weight.data_ptr()
 
