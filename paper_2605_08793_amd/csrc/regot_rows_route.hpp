@@ -304,7 +304,8 @@ __global__ __launch_bounds__(kThreads) void row_route_kernel(RouteArgs A)
                     second = fmaxf(fmaxf(second, second_o), fminf(first, first_o));
                     first = fmaxf(first, first_o);
                 }
-                if (part == 0) value[at][g] = A.group_by == REGOT_GROUP_TOP2 && second > -kInf ? first + second : first;
+                // (two keys of the type's lowest value are still a group, which comes before one that has none)
+                if (part == 0) value[at][g] = A.group_by == REGOT_GROUP_TOP2 && second > -kInf ? fmaxf(first + second, -__FLT_MAX__) : first;
             }
             wave_lds();
             for (int g = R.l; g < A.groups; g += LANES) {
