@@ -210,45 +210,43 @@ __global__ __launch_bounds__(Team<WAVES>::kBlock, KEPT > 0 ? 4 : 1) void row_dis
         }
         loss = Row::template all<OpSumF>(loss, team_lds + 2 * WAVES);
         if (thread == 0 && begin == 0) A.loss[row] = bad ? kNan : loss;
-        if (!out) {
-            Row::sync();  // the loss's sums are read
-            continue;
-        }
-        const auto p_weighted = [&](float x) { return exp2_fast((x - max) * A.log2_scale) * of_p; };
-        // backwards: the columns read last are still here, those before them in the caches
-        const int stretches = (int)((end - begin + VECS * kStep - 1) / (VECS * kStep));
-        for (int i = 0; i < stretches; ++i) {
-            const uint32_t j0 = begin + (PARTS ? i : stretches - 1 - i) * VECS * kStep;
-            if (KEPT > 0 && i == 1) {
+        if (out) {
+            const auto p_weighted = [&](float x) { return exp2_fast((x - max) * A.log2_scale) * of_p; };
+            // backwards: the columns read last are still here, those before them in the caches
+            const int stretches = (int)((end - begin + VECS * kStep - 1) / (VECS * kStep));
+            for (int i = 0; i < stretches; ++i) {
+                const uint32_t j0 = begin + (PARTS ? i : stretches - 1 - i) * VECS * kStep;
+                if (KEPT > 0 && i == 1) {
 #pragma unroll
-                for (int u = 0; u < VECS; ++u) raw[u] = u < KEPT ? kept[u < KEPT ? u : 0][threadIdx.x] : scores.template ask<true>(j0 + u * kStep + thread * T::kVec);
-            } else if (i > 0 && !none) {
-                ask(j0, std::true_type{});
-            }
-#pragma unroll
-            for (int u = 0; u < VECS; ++u) {
-                if (j0 + u * kStep >= end) continue;
-                const Span<TYPE> span(here(j0 + u * kStep + thread * T::kVec), A.m);
-                if (span.own >= end) continue;
-                float x[T::kVec] = {};
-                if (!none) {
-                    scores.unpack(raw[u], span.own, x);
-#pragma unroll
-                    for (int e = 0; e < T::kVec; ++e) x[e] = p_weighted(x[e]);
+                    for (int u = 0; u < VECS; ++u) raw[u] = u < KEPT ? kept[u < KEPT ? u : 0][threadIdx.x] : scores.template ask<true>(j0 + u * kStep + thread * T::kVec);
+                } else if (i > 0 && !none) {
+                    ask(j0, std::true_type{});
                 }
-                span.store(out, x);
+#pragma unroll
+                for (int u = 0; u < VECS; ++u) {
+                    if (j0 + u * kStep >= end) continue;
+                    const Span<TYPE> span(here(j0 + u * kStep + thread * T::kVec), A.m);
+                    if (span.own >= end) continue;
+                    float x[T::kVec] = {};
+                    if (!none) {
+                        scores.unpack(raw[u], span.own, x);
+#pragma unroll
+                        for (int e = 0; e < T::kVec; ++e) x[e] = p_weighted(x[e]);
+                    }
+                    span.store(out, x);
+                }
             }
-        }
-        if (!none) {
-            __threadfence_block();
-            Row::sync();
-            for (int l = thread; l < A.k; l += Row::kSize) {
-                const uint32_t j = l == thread ? first_column : list_column[team][l];
-                if (j < begin || j >= end) continue;
-                float q = 0.f;
+            if (!none) {
+                __threadfence_block();
+                Row::sync();
+                for (int l = thread; l < A.k; l += Row::kSize) {
+                    const uint32_t j = l == thread ? first_column : list_column[team][l];
+                    if (j < begin || j >= end) continue;
+                    float q = 0.f;
 #pragma unroll 8
-                for (int u = 0; u < A.k; ++u) q += list_column[team][u] == j ? list_q[team][u] : 0.f;
-                out[j] = T::put(p_weighted(l == thread ? first_x : scores(j)) - (bad ? kNan : weight) * q);
+                    for (int u = 0; u < A.k; ++u) q += list_column[team][u] == j ? list_q[team][u] : 0.f;
+                    out[j] = T::put(p_weighted(l == thread ? first_x : scores(j)) - (bad ? kNan : weight) * q);
+                }
             }
         }
         Row::sync();  // the list and the sums are read
