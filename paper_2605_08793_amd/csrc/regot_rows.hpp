@@ -216,12 +216,12 @@ struct Softmax {
     float sum = 0.f, weighted = 0.f;
 
     // brings the sums to the maximum `to`, which is no less than max.  (Where f is 0 nothing is left of them; a mask of the type's
-    // lowest value makes d, or sum d, -inf there, and f times that a NaN.)
+    // lowest value makes d, or sum d, -inf there, and f times that a NaN.  Where f is NaN the maximum or the sum says so.)
     __device__ __forceinline__ void raise(float to, float c)
     {
         const bool empty = max == -kInf;
         const float d = (max - to) * c, f = exp2_fast(d);
-        weighted = empty || f == 0.f ? 0.f : f * fmaf(sum, d, weighted);
+        weighted = f > 0.f ? f * fmaf(sum, d, weighted) : 0.f;
         sum = empty ? 0.f : sum * f;
         max = to;
         base = to == -kInf ? 0.f : to;
