@@ -215,14 +215,14 @@ struct Softmax {
     float max = -kInf, base = 0.f;  // base: what is subtracted, 0 while there is no maximum
     float sum = 0.f, weighted = 0.f;
 
-    // brings the sums to the maximum `to`, which is no less than max.  (Where f is 0 nothing is left of them; a mask of the type's
-    // lowest value makes d, or sum d, -inf there, and f times that a NaN.  Where f is NaN the maximum or the sum says so.)
+    // brings the sums to the maximum `to`, which is no less than max.  From a distance of 150 on nothing is left of them: it is kept
+    // finite, so that it is 0 times a number that is left (a mask of the type's lowest value, or no score yet, make it -inf, two
+    // maxima of -inf a NaN; where the sums have to be NaN, max or sum is).
     __device__ __forceinline__ void raise(float to, float c)
     {
-        const bool empty = max == -kInf;
-        const float d = (max - to) * c, f = exp2_fast(d);
-        weighted = f > 0.f ? f * fmaf(sum, d, weighted) : 0.f;
-        sum = empty ? 0.f : sum * f;
+        const float d = fmaxf((max - to) * c, -1024.f), f = exp2_fast(d);
+        weighted = f * fmaf(sum, d, weighted);
+        sum *= f;
         max = to;
         base = to == -kInf ? 0.f : to;
     }

@@ -566,13 +566,13 @@ __global__ __launch_bounds__(kThreads) void row_logprob_narrow_kernel(RowArgs A)
                 constexpr int kHalves = VECS == 1 ? 1 : 2;
                 const int maxima = min((A.m + T::kVec - 1) / T::kVec, (uint32_t)kHalves * kLanes);
                 bool found = T::kVec == 1 || 16 * A.k <= (VECS == 8 ? 13 : 12) * maxima;
-                wave_lds();
                 if (found) {
                     float half[kHalves];
 #pragma unroll
                     for (int u = 0; u < VECS; ++u) half[u % kHalves] = u < kHalves ? top[u] : max_nan(half[u % kHalves], top[u]);
                     const float bound = kth_largest_bound(half, A.k);
                     int pairs = 0;
+                    wave_lds();
 #pragma unroll
                     for (int u = 0; u < VECS; ++u) {
                         const bool is = top[u] >= bound && top[u] > -kInf;
@@ -614,6 +614,7 @@ __global__ __launch_bounds__(kThreads) void row_logprob_narrow_kernel(RowArgs A)
                 }
                 if (!found) {
                     count = 0;
+                    wave_lds();
                     best_by_bisection<kHeld, VECS>(scores, A.k, at, push);
                     wave_lds();
                 }
