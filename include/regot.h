@@ -578,8 +578,8 @@ enum { REGOT_F32 = 0, REGOT_BF16 = 1, REGOT_F16 = 2 };
  * 0 <= targets <= REGOT_ROW_MAX_LIST, 0 <= k <= REGOT_ROW_MAX_TOP.  S is read once, and the few blocks of it that hold the
  * alternatives a second time.  Rows whose alternatives cannot be told from a few maxima are looked through again, from the caches where they
  * fit: rows of up to 2048 (fp32) or 4096 columns, where they have many equal scores or k is near the number of their 16-byte blocks
- * or of 128, at most 30 times; longer ones of many equal scores twice, and where that is not enough (about k > 60), in part once for each
- * alternative.  eta has to be such that 1 / eta is an fp32 number other than 0.
+ * or of 128, at most 30 times; longer ones of many equal scores, or of few open columns, twice, and where
+ * the open columns are few of each 2048 (1024 for fp32) in the same places, in part once for each alternative.  eta has to be such that 1 / eta is an fp32 number other than 0.
  */
 #define REGOT_ROW_MAX_LIST 1024
 #define REGOT_ROW_MAX_TOP 128

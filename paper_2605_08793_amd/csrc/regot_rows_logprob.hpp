@@ -36,7 +36,7 @@ constexpr int kGroup = 16;                    // scores a lane works on at a tim
 constexpr uint32_t kSlice = kThreads * kGroup;  // columns of a row that a workgroup works on at a time
 constexpr int kWholeBlocks = 16;              // blocks of a row that one workgroup reads
 constexpr int kPartBlocks = 32;               // of one that several do, at most
-constexpr int kList = 512;                    // blocks, and columns, that may hold the best k; beyond, they are found one by one
+constexpr int kList = 512;                    // blocks, and columns, that may hold the best k
 
 // A column and its score as one number: larger for what comes first among a row's alternatives.  0 is none.
 __device__ __forceinline__ uint64_t alternative(float x, uint32_t column) { return (uint64_t)ordered(x + 0.f) << 32 | (uint32_t)~column; }
@@ -297,12 +297,14 @@ struct TopShared {
 // The k best columns of a row, by a workgroup that knows the maximum of each thread's columns in each block of the row
 // (block_max[b], thread t having the 16 bytes number t, t + kThreads, ... of the row): k columns are at or above the
 // k-th largest of the threads' maxima, and little more than k are, in little more than k of the (block, thread) pairs.
-// Those are read again.  Where more than fit the lists may be among the best (many equal scores), the bound is made of scores and
-// columns; where that does not do either, the best are found one by one, each thread offering the best of its columns that is behind the last
-// one found.  (A row of one value, 131072 columns, 20 alternatives: 467 us one by one, 38 us with the second bound; 10 us where scores differ.)
+// Those are read again.  Where more than fit the lists may be among the best (many equal scores, or open columns that are the columns of
+// fewer than k threads), the bound is made of scores and columns, and the list in the place of the maxima, which has room for the columns
+// of 16 bytes for each of k threads; where that does not do either, the best are found one by one, each thread offering the best of
+// its columns that is behind the last one found.  (A row of one value, 131072 columns, 20 alternatives: 467 us one by one, 71 us with the second
+// bound; 9 us where scores differ.)
 template <int TYPE, bool BIAS>
 __device__ __forceinline__ void best_columns(const RowArgs &A, const RowOut &out, const RowScores<TYPE, BIAS> &scores, float my_max,
-                                             const float (*block_max)[kThreads], TopShared &L)
+                                             float (*block_max)[kThreads], TopShared &L)
 {
     using T = Score<TYPE>;
     const int lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes;
@@ -363,14 +365,17 @@ __device__ __forceinline__ void best_columns(const RowArgs &A, const RowOut &out
             if (better == A.k - 1 && mine != 0) L.best[0] = mine;
             __syncthreads();
             const uint64_t from = L.best[0];
+            constexpr int kWide = kWholeBlocks * kThreads * (int)sizeof(float) / (int)sizeof(uint64_t) - kRankPad;
+            static_assert(kWide >= REGOT_ROW_MAX_TOP * 8, "16 bytes of 16-bit scores for each of k threads");
+            uint64_t *const list = reinterpret_cast<uint64_t *>(block_max);  // (nothing reads the maxima any more)
             each_from(scores, from, threadIdx.x, kThreads, [&](uint64_t a) {
                 const int at = atomicAdd(&L.count, 1);
-                if (at < kList) L.list[at] = a;
+                if (at < kWide) list[at] = a;
             });
             __syncthreads();
             count = L.count;
-            if (count <= kList) {
-                rank_all(L.list, count, threadIdx.x, kThreads, A.k, [&](int rank, uint64_t a) { out.top(rank, a); });
+            if (count <= kWide) {
+                rank_all(list, count, threadIdx.x, kThreads, A.k, [&](int rank, uint64_t a) { out.top(rank, a); });
             } else for (count = 0; count < A.k; ++count) {
                 uint64_t best = mine;
 #pragma unroll
@@ -407,7 +412,7 @@ __global__ __launch_bounds__(kThreads, BIAS ? 5 : 6) void row_logprob_kernel(Row
     using Scores = RowScores<TYPE, BIAS>;
     constexpr uint32_t kStep = kThreads * T::kVec;
     constexpr int kVecsOfGroup = Scores::kGroupVecs, kGroups = VECS / kVecsOfGroup;
-    __shared__ float block_max[kWholeBlocks][kThreads];  // (TOP and whole rows)
+    __shared__ __align__(16) float block_max[kWholeBlocks][kThreads];  // (TOP and whole rows)
     __shared__ float team_sums[3 * kWaves];
     __shared__ TopShared shared;
     const uint32_t at = threadIdx.x * T::kVec;
@@ -481,7 +486,7 @@ __global__ __launch_bounds__(kThreads) void row_logprob_join_kernel(RowArgs A)
 {
     __shared__ float team_sums[3 * kWaves];
     __shared__ TopShared shared;
-    __shared__ float block_max[kPartBlocks][kThreads];
+    __shared__ __align__(16) float block_max[kPartBlocks][kThreads];
     for (int64_t row = blockIdx.x; row < A.n; row += gridDim.x) {
         const RowScores<TYPE, BIAS> scores(A, row);
         Given<TYPE, BIAS> given;
