@@ -525,6 +525,7 @@ __global__ __launch_bounds__(kThreads) void row_logprob_narrow_kernel(RowArgs A)
     using Scores = RowScores<TYPE, BIAS>;
     constexpr uint32_t kStep = kLanes * T::kVec;
     constexpr int kHeld = 256;
+    static_assert(T::kVec > 1 || VECS * kLanes <= kHeld, "all columns of a row of single loads");
     __shared__ uint16_t pair[kWaves][VECS * kLanes];
     __shared__ int counts[kWaves];
     __shared__ __align__(16) uint64_t list[kWaves][kHeld + kRankPad];
@@ -598,9 +599,9 @@ __global__ __launch_bounds__(kThreads) void row_logprob_narrow_kernel(RowArgs A)
                         for (int e = 0; e < T::kVec; ++e) push(i0 + lane < pairs && x[e] >= bound && x[e] > -kInf, alternative(x[e], first + e));
                     }
                     wave_lds();
-                    found = count <= kHeld;
+                    found = T::kVec == 1 || count <= kHeld;  // (rows of single loads have no more than kHeld columns)
                     // (of equal scores, the bound by columns too would leave kVec for each of the k)
-                    if (!found && (A.k - 1) * T::kVec < kHeld) {
+                    if (T::kVec > 1 && !found && (A.k - 1) * T::kVec < kHeld) {
                         const uint64_t mine = best_before(scores, ~0ull, lane, kLanes);
                         int better = 0;
                         for (int l = 0; l < kLanes; ++l) better += __shfl((unsigned long long)mine, l) > mine;
@@ -617,11 +618,13 @@ __global__ __launch_bounds__(kThreads) void row_logprob_narrow_kernel(RowArgs A)
                         found = count <= kHeld;
                     }
                 }
-                if (!found) {
-                    count = 0;
-                    wave_lds();
-                    best_by_bisection<kHeld, VECS>(scores, A.k, at, push);
-                    wave_lds();
+                if constexpr (T::kVec > 1) {
+                    if (!found) {
+                        count = 0;
+                        wave_lds();
+                        best_by_bisection<kHeld, VECS>(scores, A.k, at, push);
+                        wave_lds();
+                    }
                 }
                 rank_all(list[wave], count, lane, kLanes, A.k, [&](int rank, uint64_t a) { out.top(rank, a); });
             }
