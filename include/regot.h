@@ -14,12 +14,13 @@
  * finds it inside the fused pass: one pass for both), and calls that work
  * on the sparse pattern only (pattern_*, hessian_*, pcg_solve, pcg_solve2, splr_direction)
  * or on vectors (dual_metrics, choose_candidate).  The row calls (row_logprob, row_distill, row_route) take a
- * model's scores in fp32, bf16 or fp16 in place of M.
+ * model's scores in fp32, bf16 or fp16 in place of M, and the expert calls (expert_order, expert_product, ..., with grad_norm and grad_clip)
+ * do what its router's choices are for.
  *
  * Conventions common to all calls
  *   - All array arguments are DEVICE pointers (HBM of the current HIP device)
  *     unless the parameter comment says "host".  Everything is fp64 (but for the row
- *     calls, which say what they take); indices
+ *     and expert calls, which say what they take); indices
  *     are int32 (columns) and int64 (row offsets).
  *   - M is row-major with leading dimension ldM >= m (in elements).  When M is
  *     16-byte aligned and ldM is even the kernels use 128-bit loads; otherwise
@@ -676,6 +677,119 @@ int regot_row_route_grad(int64_t n, int64_t m,
                          regot_stream_t stream);
 
 /*
+ * ---- What follows a router's choices ----
+ *
+ * regot_row_route gives k columns (experts) for each of n tokens, and their weights.  The calls below put the choices into the order
+ * of the experts, multiply each expert's rows by its own weights (with the gate of a gated layer), add a token's rows up again, and form the
+ * gradients of all of this; g_weight of regot_expert_combine_grad is what regot_row_route_grad takes.  The norm over all gradients, and clipping, close
+ * the step.
+ *   - `type` is REGOT_F32, REGOT_BF16 or REGOT_F16.  Products are summed in fp32, and a result is rounded to its type once.  Matrices are row-major
+ *     with leading dimensions in elements, aligned to their elements.  (Products whose matrices begin at multiples of 16 bytes, with
+ *     rows of whole multiples of 16 bytes, are faster: they go from memory to LDS without registers between.)
+ *   - Rows that belong to one expert are a run: start[e] .. start[e+1] - 1.  Rows in front of start[0] and from start[experts] on belong to none:
+ *     they are not read and not written.  start[] has to ascend; what lies outside 0 .. rows is not followed.
+ *   - Outputs that share memory with an input or with each other are refused (REGOT_ERR_ARG); the rows of one may lie between those of the other,
+ *     at the same distance.  Non-finite numbers follow IEEE arithmetic within their row (weight gradients: within their expert).
+ *   - Sums are added up in a fixed order: the same call gives the same bits.  0 <= experts <= REGOT_ROW_MAX_EXPERTS, 1 <= k <= REGOT_ROW_MAX_CHOICES.
+ */
+
+/*
+ * The choices idx[i*k + l] (slot i*k + l, expert 0 .. experts - 1, or anything else for none) by expert:
+ *     start[e]   how many choices have an expert below e; start[experts]: all that have one
+ *     order[r]   the slots by expert, those of one expert ascending: row r is the choice order[r] of token order[r] / k; -1 from start[experts] on
+ *     place[s]   the row of slot s, -1 where its choice is none
+ * An expert that a token has twice gives it two rows.  n * k < 2^31.
+ */
+int regot_expert_order_workspace_bytes(int64_t n, int k, int64_t experts, size_t *bytes /* host, out */);
+int regot_expert_order(int64_t n, int k, int64_t experts,
+                       const int32_t *idx,                       /* [n * k] */
+                       int64_t *start,                           /* [experts + 1] out */
+                       int32_t *order, int32_t *place,           /* [n * k] out */
+                       void *workspace, size_t workspace_bytes, regot_stream_t stream);
+
+/*
+ * Products grouped by expert: for each row r of the run of expert e
+ *     z_rj = sum_c X[src(r)][c] W_e[j][c],    src(r) = order[r] / k, or r where order is NULL
+ *     act = REGOT_ACT_NONE        Y[r][j] = z_rj,  j < m
+ *           REGOT_ACT_GATE        W_e has 2 m rows: Y[r][j] = g s(g) u with g = z_rj, u = z_r,m+j, s(g) = 1/(1 + exp(-g)), all in fp32;
+ *                                 saved[r] = the 2 m numbers z_r (optional, may be NULL)
+ *           REGOT_ACT_GATE_GRAD   the gradient to such a z: with (g, u) = saved[r][j], saved[r][m+j] read,
+ *                                 Y[r][j] = z_rj u s(g) (1 + g (1 - s(g))),  Y[r][m+j] = z_rj g s(g);  Y has 2 m columns
+ * W_e begins at W + e strideW; w_by = REGOT_W_OUTPUTS: W_e[j][c] at j ldW + c; REGOT_W_INPUTS: at c ldW + j (an input's numbers for all outputs
+ * are neighbours).  So dX = dY W_e, the gradient to the rows of a product with weights by outputs, is the product of dY with the same weights by inputs.
+ * `rows` is how many rows Y, saved and order have (start[experts] <= rows); x_rows those of X.  d = 0: sums of 0.
+ */
+enum { REGOT_ACT_NONE = 0, REGOT_ACT_GATE = 1, REGOT_ACT_GATE_GRAD = 2 };
+enum { REGOT_W_OUTPUTS = 0, REGOT_W_INPUTS = 1 };
+int regot_expert_product(int64_t rows, int64_t m, int64_t d, int64_t experts,
+                         const int64_t *start,                   /* [experts + 1] */
+                         const void *X, int type, int64_t ldX, int64_t x_rows,
+                         const int32_t *order, int k,            /* [rows], optional */
+                         const void *W, int w_by, int64_t ldW, int64_t strideW,
+                         int act,
+                         void *Y, int64_t ldY,                   /* [rows][ldY] out */
+                         void *saved, int64_t ldSaved,           /* [rows][ldSaved] out (GATE) or in (GATE_GRAD) */
+                         regot_stream_t stream);
+
+/*
+ * The gradient to the weights of such a product:
+ *     dW_e[j][c] = sum over the rows r of expert e of dY[r][j] X[src(r)][c],  j < m, c < d;  0 for an expert without rows
+ * of type out_type, which is `type` or REGOT_F32; dW_e[j][c] at dW + e strideW + j ldW + c, strideW >= (m - 1) ldW + d.
+ * Few tiles with long sums are summed in parts, in the workspace.
+ */
+int regot_expert_weight_grad_workspace_bytes(int64_t rows, int64_t m, int64_t d, int64_t experts, size_t *bytes /* host, out */);
+int regot_expert_weight_grad(int64_t rows, int64_t m, int64_t d, int64_t experts,
+                             const int64_t *start,               /* [experts + 1] */
+                             const void *dY, int type, int64_t ldY,
+                             const void *X, int64_t ldX, int64_t x_rows,
+                             const int32_t *order, int k,        /* [rows], optional */
+                             void *dW, int out_type, int64_t ldW, int64_t strideW,  /* out */
+                             void *workspace, size_t workspace_bytes, regot_stream_t stream);
+
+/*
+ * The rows of each token, weighted and added up, l ascending (a choice without a row, place outside 0 .. rows - 1, is left out):
+ *     out[i][j] = sum_l weight[i*k + l] Y[place[i*k + l]][j]           weight NULL: 1 (the gradient of rows that were taken by order)
+ * and the gradient: with r = place[i*k + l]
+ *     dY[r][j] = weight[i*k + l] g_out[i][j],   g_weight[i*k + l] = sum_j g_out[i][j] Y[r][j], 0 where there is no row
+ * Rows of dY that no choice has are left as they were.  g_weight NULL (then Y too) leaves that part out.  A row is at most one choice's.
+ */
+int regot_expert_combine(int64_t n, int k, int64_t m, int64_t rows,
+                         const void *Y, int type, int64_t ldY,
+                         const int32_t *place, const float *weight,  /* [n * k]; weight optional */
+                         void *out, int64_t ldO,                 /* [n][ldO] out */
+                         regot_stream_t stream);
+int regot_expert_combine_grad(int64_t n, int k, int64_t m, int64_t rows,
+                              const void *g_out, int type, int64_t ldG,
+                              const void *Y, int64_t ldY,
+                              const int32_t *place, const float *weight,
+                              void *dY, int64_t ldD,             /* [rows][ldD] out */
+                              float *g_weight,                   /* [n * k] out, optional */
+                              regot_stream_t stream);
+
+/*
+ * The norm over many tensors, and clipping:
+ *     norm[0]   = sqrt(sum of the squares of all numbers of all tensors), squares and sums in fp64
+ *     factor[0] = max_norm / norm where norm > max_norm, else 1; 1 too where the norm is not finite: a program looks at norm and leaves the step out
+ *     out       = factor * data, rounded once, for each tensor; out may be data, and is then not written where factor is 1
+ * `list` is a HOST array, read during the call; each tensor is `count` numbers without gaps.  Types may differ.  regot_grad_norm does not look at
+ * `out`.  Tensors whose outputs share memory with each other, or with another's numbers, are refused: they would be scaled twice.
+ * max_norm > 0 (inf: nothing is scaled).  The workspace's size depends on the tensors' counts.
+ */
+typedef struct {
+    const void *data;  /* device */
+    void *out;         /* device */
+    int64_t count;
+    int32_t type;
+} regot_tensor;
+int regot_grad_norm_workspace_bytes(int64_t count, const regot_tensor *list /* host */, size_t *bytes /* host, out */);
+int regot_grad_norm(int64_t count, const regot_tensor *list /* host */,
+                    float *norm,                                 /* [1] out */
+                    void *workspace, size_t workspace_bytes, regot_stream_t stream);
+int regot_grad_clip(int64_t count, const regot_tensor *list /* host */, double max_norm,
+                    float *norm, float *factor,                  /* [1], [1] out */
+                    void *workspace, size_t workspace_bytes, regot_stream_t stream);
+
+/*
  * Measurement aid, not part of the method: one pass over M with the tiling and the loads of the dense
  * calls (the g_r x g_c cut of regot_plan_geometry(n, m, -1), 128-bit non-temporal loads, four rows per
  * wave in flight) that only adds the entries up.  sum[0] = sum of all M_ij (fixed order).  Its duration
@@ -700,7 +814,7 @@ int regot_stream_read_probe(int64_t n, int64_t m,
 int regot_placement_probe(int grid, uint32_t *ids /* device, [2 * grid] out */, regot_stream_t stream);
 
 /*
- * Profiling aid, not part of the method.  The next call of any entry point above but the row calls made by the
+ * Profiling aid, not part of the method.  The next call of any entry point above but the row and expert calls made by the
  * calling host thread records `start_event` on its stream just before, and `stop_event` just
  * after, the launch of its streaming kernel (the single pass over M; the small combine / scatter
  * kernels that follow are outside the pair; for regot_topk_threshold it is the first pass over M).  Both are hipEvent_t handles owned by the caller,

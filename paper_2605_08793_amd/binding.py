@@ -49,6 +49,16 @@ SYMBOLS = (
     "regot_row_distill",
     "regot_row_route",
     "regot_row_route_grad",
+    "regot_expert_order_workspace_bytes",
+    "regot_expert_order",
+    "regot_expert_product",
+    "regot_expert_weight_grad_workspace_bytes",
+    "regot_expert_weight_grad",
+    "regot_expert_combine",
+    "regot_expert_combine_grad",
+    "regot_grad_norm_workspace_bytes",
+    "regot_grad_norm",
+    "regot_grad_clip",
     "regot_profile_stage1",
     "regot_sweep_patience",
     "regot_stream_read_probe",
@@ -116,6 +126,16 @@ def load():
     lib.regot_row_distill.argtypes = [i64, i64, p, c_int, i64, dbl, p, p, c_int, p, p, p, i64, p, sz, p]
     lib.regot_row_route.argtypes = [i64, i64, p, c_int, i64, p, c_int, c_int, c_int, c_int, c_int, c_int, c_int, dbl, p, p, p]
     lib.regot_row_route_grad.argtypes = [i64, i64, p, c_int, i64, c_int, p, c_int, c_int, dbl, p, p, i64, p]
+    lib.regot_expert_order_workspace_bytes.argtypes = [i64, c_int, i64, ctypes.POINTER(sz)]
+    lib.regot_expert_order.argtypes = [i64, c_int, i64, p, p, p, p, p, sz, p]
+    lib.regot_expert_product.argtypes = [i64, i64, i64, i64, p, p, c_int, i64, i64, p, c_int, p, c_int, i64, i64, c_int, p, i64, p, i64, p]
+    lib.regot_expert_weight_grad_workspace_bytes.argtypes = [i64, i64, i64, i64, ctypes.POINTER(sz)]
+    lib.regot_expert_weight_grad.argtypes = [i64, i64, i64, i64, p, p, c_int, i64, p, i64, i64, p, c_int, p, c_int, i64, i64, p, sz, p]
+    lib.regot_expert_combine.argtypes = [i64, c_int, i64, i64, p, c_int, i64, p, p, p, i64, p]
+    lib.regot_expert_combine_grad.argtypes = [i64, c_int, i64, i64, p, c_int, i64, p, i64, p, p, p, i64, p, p]
+    lib.regot_grad_norm_workspace_bytes.argtypes = [i64, p, ctypes.POINTER(sz)]
+    lib.regot_grad_norm.argtypes = [i64, p, p, p, sz, p]
+    lib.regot_grad_clip.argtypes = [i64, p, dbl, p, p, p, sz, p]
     lib.regot_profile_stage1.argtypes = [p, p]
     lib.regot_sweep_patience.argtypes = [ctypes.c_int]
     lib.regot_stream_read_probe.argtypes = [i64, i64, p, i64, p, p, sz, p]
@@ -611,6 +631,157 @@ def regot_row_route_grad(S, idx, g_weight, dS, *, score="softmax", renormalise=T
     _check(load().regot_row_route_grad(
         n, m, at, kind, ld, SCORE_KINDS[score], _list(idx, n, k, "idx", torch.int32), k, int(bool(renormalise)), float(scale),
         _list(g_weight, n, k, "g_weight"), to, ldD, _row_stream(S, stream)), "regot_row_route_grad")
+
+
+# ---- what follows a router's choices ---------------------------------------------------------------------------------
+
+ACTS = {None: 0, "gate": 1, "gate_grad": 2}
+
+
+def _weights(W: torch.Tensor, name="W"):
+    """(experts, outputs, inputs, w_by, ldW, strideW, address) of (experts, outputs, inputs) weights, of which either the inputs or
+    the outputs are neighbours in memory (W, or W.transpose(1, 2) of one that lies the other way)."""
+    if not isinstance(W, torch.Tensor) or not W.is_cuda or W.dim() != 3 or W.dtype not in SCORE_TYPES:
+        raise TypeError(f"{name} must be a 3-D float32, bfloat16 or float16 CUDA tensor")
+    experts, outputs, inputs = W.shape
+    stride, by_output, by_input = W.stride()
+    if by_input == 1 or inputs <= 1:
+        by, ld, least, single = 0, by_output, inputs, outputs <= 1
+    elif by_output == 1 or outputs <= 1:
+        by, ld, least, single = 1, by_input, outputs, inputs <= 1
+    else:
+        raise TypeError(f"{name}: the numbers of an output, or those of an input, must be neighbours")
+    if single or W.numel() == 0:
+        ld = max(least, 1)
+    if ld < least:
+        raise TypeError(f"{name} must have a distance of at least {least} between neighbouring rows")
+    return experts, outputs, inputs, by, ld, stride, W.data_ptr()
+
+
+def regot_expert_order_workspace_bytes(n: int, k: int, experts: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().regot_expert_order_workspace_bytes(int(n), int(k), int(experts), ctypes.byref(out)), "regot_expert_order_workspace_bytes")
+    return int(out.value)
+
+
+def regot_expert_order(idx, start, order, place, *, workspace, stream=None) -> None:
+    """idx, place (n, k), order (n * k): int32; start (experts + 1): int64."""
+    if not isinstance(idx, torch.Tensor) or idx.dim() not in (1, 2):
+        raise TypeError("idx must be a 1-D or 2-D int32 CUDA tensor")
+    n, k = idx.shape[0], _width(idx, idx.shape[0], "idx")
+    experts = start.numel() - 1
+    _check(load().regot_expert_order(
+        n, k, experts, _list(idx, n, k, "idx", torch.int32), _list(start, experts + 1, 1, "start", torch.int64),
+        _list(order, n, k, "order", torch.int32), _list(place, n, k, "place", torch.int32), *_ws(workspace), _row_stream(idx, stream)),
+        "regot_expert_order")
+
+
+def regot_expert_product(X, W, start, Y, *, order=None, k=1, act=None, saved=None, stream=None) -> None:
+    """X (x_rows, d), W (experts, m or 2 m, d), Y (rows, m or 2 m), saved (rows, 2 m): one type; order (rows): int32, start: int64."""
+    x_rows, d, kind, ldX, at = _scores(X, "X")
+    experts, wide, inputs, by, ldW, stride, w_at = _weights(W)
+    rows, out, _, ldY, to = _scores(Y, "Y")
+    m = wide // 2 if act == "gate" else wide
+    if inputs != d or out != (2 * m if act == "gate_grad" else m) or (act == "gate" and wide % 2):
+        raise TypeError("W must be (experts, outputs, inputs) of X's inputs and Y's outputs")
+    ldS, s_at = 2 * m, 0
+    if saved is not None:
+        s_rows, s_cols, _, ldS, s_at = _scores(saved, "saved")
+        if s_rows != rows or s_cols != 2 * m:
+            raise TypeError(f"saved must be {rows} x {2 * m}")
+    if any(t is not None and t.dtype != X.dtype for t in (W, Y, saved)):
+        raise TypeError("X, W, Y and saved must be of one type")
+    _check(load().regot_expert_product(
+        rows, m, d, experts, _list(start, experts + 1, 1, "start", torch.int64), at, kind, ldX, x_rows,
+        _list(order, rows, 1, "order", torch.int32, optional=True), int(k), w_at, by, ldW, stride, ACTS[act], to, ldY, s_at, ldS,
+        _row_stream(X, stream)), "regot_expert_product")
+
+
+def regot_expert_weight_grad_workspace_bytes(rows: int, m: int, d: int, experts: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().regot_expert_weight_grad_workspace_bytes(int(rows), int(m), int(d), int(experts), ctypes.byref(out)),
+           "regot_expert_weight_grad_workspace_bytes")
+    return int(out.value)
+
+
+def regot_expert_weight_grad(dY, X, start, dW, *, order=None, k=1, workspace, stream=None) -> None:
+    """dY (rows, m) and X (x_rows, d) of one type, dW (experts, m, d) of that type or float32, the numbers of its last dimension neighbours."""
+    rows, m, kind, ldY, g_at = _scores(dY, "dY")
+    x_rows, d, _, ldX, at = _scores(X, "X")
+    experts, outputs, inputs, by, ldW, stride, to = _weights(dW, "dW")
+    if (outputs, inputs) != (m, d) or (by != 0 and dW.numel()) or X.dtype != dY.dtype:
+        raise TypeError(f"dW must be (experts, {m}, {d}) with rows of neighbours, dY and X of one type")
+    _check(load().regot_expert_weight_grad(
+        rows, m, d, experts, _list(start, experts + 1, 1, "start", torch.int64), g_at, kind, ldY, at, ldX, x_rows,
+        _list(order, rows, 1, "order", torch.int32, optional=True), int(k), to, SCORE_TYPES[dW.dtype], ldW, stride, *_ws(workspace),
+        _row_stream(X, stream)), "regot_expert_weight_grad")
+
+
+def regot_expert_combine(Y, place, weight, out, *, stream=None) -> None:
+    """Y (rows, m), out (n, m); place (n, k) int32, weight (n, k) or None."""
+    rows, m, kind, ldY, at = _scores(Y, "Y")
+    n, cols, _, ldO, to = _scores(out, "out")
+    if cols != m or out.dtype != Y.dtype:
+        raise TypeError("out must have the columns and the type of Y")
+    k = _width(place, n, "place")
+    _check(load().regot_expert_combine(
+        n, k, m, rows, at, kind, ldY, _list(place, n, k, "place", torch.int32), _list(weight, n, k, "weight", optional=True), to, ldO,
+        _row_stream(Y, stream)), "regot_expert_combine")
+
+
+def regot_expert_combine_grad(g_out, Y, place, weight, dY, g_weight=None, *, stream=None) -> None:
+    """g_out (n, m), dY (rows, m); Y (rows, m) and g_weight (n, k), or both None."""
+    n, m, kind, ldG, g_at = _scores(g_out, "g_out")
+    rows, cols, _, ldD, to = _scores(dY, "dY")
+    if cols != m or dY.dtype != g_out.dtype:
+        raise TypeError("dY must have the columns and the type of g_out")
+    ldY, at = (m, 0) if Y is None else _same_scores(Y, dY, "Y")
+    k = _width(place, n, "place")
+    _check(load().regot_expert_combine_grad(
+        n, k, m, rows, g_at, kind, ldG, at, ldY, _list(place, n, k, "place", torch.int32), _list(weight, n, k, "weight", optional=True),
+        to, ldD, _list(g_weight, n, k, "g_weight", optional=True), _row_stream(g_out, stream)), "regot_expert_combine_grad")
+
+
+class _Tensor(ctypes.Structure):
+    """regot_tensor"""
+    _fields_ = [("data", ctypes.c_void_p), ("out", ctypes.c_void_p), ("count", ctypes.c_int64), ("type", ctypes.c_int32)]
+
+
+def _tensors(tensors, out=None):
+    """A host list of tensors without gaps, all on one device, and of what they become (themselves where out is None)."""
+    out = tensors if out is None else out
+    if len(out) != len(tensors):
+        raise TypeError("there must be an output for each tensor")
+    made = (_Tensor * max(len(tensors), 1))()
+    for i, (t, o) in enumerate(zip(tensors, out)):
+        for v in (t, o):
+            if not isinstance(v, torch.Tensor) or not v.is_cuda or v.dtype not in SCORE_TYPES or not v.is_contiguous() or v.device != tensors[0].device:
+                raise TypeError("tensors must be contiguous float32, bfloat16 or float16 CUDA tensors on one device")
+        if o.dtype != t.dtype or o.shape != t.shape:
+            raise TypeError("an output must have the shape and type of its tensor")
+        made[i] = _Tensor(t.data_ptr(), o.data_ptr(), t.numel(), SCORE_TYPES[t.dtype])
+    return made
+
+
+def _list_stream(tensors, stream):
+    return _row_stream(tensors[0], stream) if len(tensors) else _stream(stream)
+
+
+def regot_grad_norm_workspace_bytes(tensors) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().regot_grad_norm_workspace_bytes(len(tensors), _tensors(tensors), ctypes.byref(out)), "regot_grad_norm_workspace_bytes")
+    return int(out.value)
+
+
+def regot_grad_norm(tensors, norm, *, workspace, stream=None) -> None:
+    _check(load().regot_grad_norm(len(tensors), _tensors(tensors), _list(norm, 1, 1, "norm"), *_ws(workspace), _list_stream(tensors, stream)),
+           "regot_grad_norm")
+
+
+def regot_grad_clip(tensors, max_norm, norm, factor, out=None, *, workspace, stream=None) -> None:
+    _check(load().regot_grad_clip(
+        len(tensors), _tensors(tensors, out), float(max_norm), _list(norm, 1, 1, "norm"), _list(factor, 1, 1, "factor"), *_ws(workspace),
+        _list_stream(tensors, stream)), "regot_grad_clip")
 
 
 def regot_profile_stage1(start_event, stop_event) -> None:

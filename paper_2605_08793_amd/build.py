@@ -8,7 +8,8 @@ import tempfile
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SRCS = [os.path.join(HERE, "csrc", "regot.hip"), os.path.join(HERE, "csrc", "regot_pattern.hip"),
-        os.path.join(HERE, "csrc", "regot_rows.hip")]
+        os.path.join(HERE, "csrc", "regot_rows.hip"), os.path.join(HERE, "csrc", "regot_experts.hip"),
+        *(os.path.join(HERE, "csrc", f"regot_experts_{t}.hip") for t in ("bf16", "f16", "f32"))]
 LIB = os.path.join(HERE, "libregot.so")
 
 HIPCC_FLAGS = [

@@ -1,0 +1,563 @@
+// What follows a router's choices: their order by expert, products grouped by expert and their gradients, the weighted sum of the
+// experts' rows, and the norm over all gradients with clipping.  Checks of arguments, how work is shared out, launches; the products' kernels
+// are built for each type of numbers in a source of their own.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <memory>
+#include <new>
+
+#include "regot.h"
+#include "regot_experts_launch.hpp"
+#include "regot_experts_order.hpp"
+#include "regot_gradients.hpp"
+#include "regot_overlap.hpp"
+
+namespace regot {
+void expert_tiles_bf16(const GroupArgs &A, const TilePlan &P, hipStream_t s);
+void expert_tiles_f16(const GroupArgs &A, const TilePlan &P, hipStream_t s);
+void expert_tiles_f32(const GroupArgs &A, const TilePlan &P, hipStream_t s);
+}  // namespace regot
+
+namespace {
+
+using namespace regot;
+
+constexpr int64_t kMaxDim = 2147483647LL;
+constexpr int64_t kMaxGrid = 1 << 22;
+constexpr size_t kAlign = 256;
+constexpr int kCUs = 256;
+
+bool misaligned(const void *p, size_t a) { return ((uintptr_t)p % a) != 0; }
+int hip_status() { return hipGetLastError() == hipSuccess ? REGOT_OK : REGOT_ERR_HIP; }
+bool bad_type(int type) { return type != REGOT_F32 && type != REGOT_BF16 && type != REGOT_F16; }
+int element_bytes(int type) { return type == REGOT_F32 ? 4 : 2; }
+bool bad_dim(int64_t v) { return v < 0 || v > kMaxDim; }
+size_t padded(size_t bytes) { return std::max((bytes + kAlign - 1) / kAlign * kAlign, kAlign); }
+unsigned grid_of(int64_t blocks) { return (unsigned)std::min(blocks, kMaxGrid); }
+
+// ---- the order of choices ----
+
+constexpr int kOneGroup = 16384;  // choices that one workgroup puts in order, in one launch
+constexpr int kMostGroups = 128;
+
+struct OrderPlan {
+    int64_t each = 0;
+    int groups = 1;
+    size_t total = 0;
+};
+
+OrderPlan plan_order(int64_t count, int64_t experts)
+{
+    OrderPlan P;
+    P.each = count;
+    if (count > kOneGroup) {
+        P.each = std::max<int64_t>((count + kMostGroups - 1) / kMostGroups, 4096);
+        P.groups = (int)((count + P.each - 1) / P.each);
+    }
+    P.total = padded(P.groups > 1 ? (size_t)P.groups * (experts + 1) * sizeof(uint32_t) : 0);
+    return P;
+}
+
+int check_order(int64_t n, int k, int64_t experts)
+{
+    if (n < 0 || experts < 0 || experts > REGOT_ROW_MAX_EXPERTS) return REGOT_ERR_DIM;
+    if (k < 1 || k > REGOT_ROW_MAX_CHOICES) return REGOT_ERR_ARG;
+    if (n > kMaxDim / k) return REGOT_ERR_DIM;
+    return REGOT_OK;
+}
+
+// ---- memory that two matrices share ----
+
+struct Memory {
+    const void *p;
+    int64_t n, m, ld;  // rows, numbers of each, distance of rows
+    int bytes;         // of a number
+};
+
+// Whether an element of one may be one of the other's.  Rows of one may lie between those of the other where their distances are the same.
+bool meet(const Memory &a, const Memory &b)
+{
+    typedef __int128 wide;
+    if (!a.p || !b.p || a.n == 0 || a.m == 0 || b.n == 0 || b.m == 0) return false;
+    const wide a0 = (uintptr_t)a.p, b0 = (uintptr_t)b.p, ra = (wide)a.m * a.bytes, rb = (wide)b.m * b.bytes;
+    const wide sa = (wide)a.ld * a.bytes, sb = (wide)b.ld * b.bytes;
+    if (a0 >= b0 + (b.n - 1) * sb + rb || b0 >= a0 + (a.n - 1) * sa + ra) return false;
+    if (sa != sb || a.n == 1 || b.n == 1) return true;
+    const wide off = ((b0 - a0) % sa + sa) % sa;  // where b's rows begin in a's
+    return off < ra || off + rb > sa;
+}
+
+// The matrix of a call's weights: experts blocks, as rows one after the other
+Memory blocks_of(const void *p, int64_t experts, int64_t n, int64_t m, int64_t ld, int64_t stride, int bytes)
+{
+    if (experts == 0 || n == 0 || m == 0) return {nullptr, 0, 0, 0, bytes};
+    return {p, 1, (experts - 1) * stride + (n - 1) * ld + m, 0, bytes};
+}
+
+// ---- products ----
+
+int check_group(int64_t rows, int64_t m, int64_t d, int64_t experts, const int64_t *start, int type)
+{
+    if (bad_dim(rows) || bad_dim(m) || bad_dim(d) || experts < 0 || experts > REGOT_ROW_MAX_EXPERTS) return REGOT_ERR_DIM;
+    if (bad_type(type)) return REGOT_ERR_ARG;
+    if (experts > 0 && !start) return REGOT_ERR_NULL;
+    if (misaligned(start, 8)) return REGOT_ERR_ALIGN;
+    return REGOT_OK;
+}
+
+// Rows of X that a product or a weight gradient takes
+int check_source(int64_t rows, int64_t d, const void *X, int64_t ldX, int64_t x_rows, const int32_t *order, int k, int type)
+{
+    if (bad_dim(x_rows)) return REGOT_ERR_DIM;
+    if (k < 1 || k > REGOT_ROW_MAX_CHOICES) return REGOT_ERR_ARG;
+    if (rows > 0 && d > 0 && !X) return REGOT_ERR_NULL;
+    if (rows > 0 && (order ? x_rows == 0 : x_rows < rows)) return REGOT_ERR_DIM;
+    if (ldX < d) return REGOT_ERR_LD;
+    if (misaligned(X, element_bytes(type)) || misaligned(order, 4)) return REGOT_ERR_ALIGN;
+    return REGOT_OK;
+}
+
+// Chunks of 16 bytes that begin at multiples of 16 bytes
+bool whole_chunks(const void *p, int64_t numbers, int64_t ld, int bytes)
+{
+    return !misaligned(p, 16) && numbers % (16 / bytes) == 0 && ld % (16 / bytes) == 0;
+}
+
+GroupArgs group_args(int64_t rows, int64_t m, int64_t d, int64_t experts, const int64_t *start, const void *X, int64_t ldX, int64_t x_rows,
+                     const int32_t *order, int k)
+{
+    GroupArgs A{};
+    A.start = start;
+    A.rows = rows;
+    A.experts = (int)experts;
+    A.order = order;
+    A.by_k = divide_by((uint32_t)k);
+    A.x_rows = x_rows;
+    A.X = X;
+    A.ldX = ldX;
+    A.m = m;
+    A.d = d;
+    A.splits = 1;
+    return A;
+}
+
+void launch(const GroupArgs &A, const TilePlan &P, int type, hipStream_t s)
+{
+    if (type == REGOT_F32) expert_tiles_f32(A, P, s);
+    else if (type == REGOT_BF16) expert_tiles_bf16(A, P, s);
+    else expert_tiles_f16(A, P, s);
+}
+
+// A weight gradient of few tiles is summed in parts, which a second launch adds up.
+struct GradPlan {
+    int64_t tiles_m = 0, tiles_d = 0;
+    int splits = 1;
+    size_t total = 0;
+};
+
+GradPlan plan_weight_grad(int64_t rows, int64_t m, int64_t d, int64_t experts)
+{
+    GradPlan P;
+    const TileShape T = tile_shape(kTileDirect);
+    P.tiles_m = (m + T.rows - 1) / T.rows;
+    P.tiles_d = (d + T.cols - 1) / T.cols;
+    const int64_t tiles = P.tiles_m * P.tiles_d * experts;
+    if (tiles > 0 && tiles < kCUs) P.splits = (int)std::max<int64_t>(std::min<int64_t>(2 * kCUs / tiles, rows / experts / 512), 1);
+    P.total = padded(P.splits > 1 ? (size_t)P.splits * experts * m * d * sizeof(float) : 0);
+    return P;
+}
+
+struct JoinArgs {
+    const float *parts;
+    int64_t numbers, m, d;  // of a part; of an expert's matrix
+    int splits;
+    void *out;
+    int64_t ld, stride;
+};
+
+// The parts of a weight gradient, in their order
+template <int OUT>
+__global__ void __launch_bounds__(kThreads) expert_join_kernel(const JoinArgs A)
+{
+    using T = Score<OUT>;
+    const int64_t step = (int64_t)gridDim.x * kThreads;
+    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < A.numbers; i += step) {
+        float v = 0.f;
+        for (int s = 0; s < A.splits; ++s) v += A.parts[s * A.numbers + i];
+        const int64_t row = i / A.d, c = i % A.d;
+        static_cast<typename T::Raw *>(A.out)[row / A.m * A.stride + row % A.m * A.ld + c] = T::put(v);
+    }
+}
+
+// ---- the norm ----
+
+constexpr uint32_t kLeastEach = 8 * kThreads;  // numbers of a workgroup
+constexpr int64_t kMostParts = 16384;
+constexpr uint32_t kFewParts = 1024;           // partial sums that each workgroup of the scaling adds up itself
+
+int check_tensors(int64_t count, const regot_tensor *list, bool clip)
+{
+    if (count < 0 || count > kMaxDim) return REGOT_ERR_DIM;
+    if (count > 0 && !list) return REGOT_ERR_NULL;
+    for (int64_t t = 0; t < count; ++t) {
+        if (list[t].count < 0) return REGOT_ERR_DIM;
+        if (bad_type(list[t].type)) return REGOT_ERR_ARG;
+        if (list[t].count > 0 && (!list[t].data || (clip && !list[t].out))) return REGOT_ERR_NULL;
+        if (misaligned(list[t].data, element_bytes(list[t].type)) || misaligned(list[t].out, element_bytes(list[t].type))) return REGOT_ERR_ALIGN;
+    }
+    return REGOT_OK;
+}
+
+// Numbers of a workgroup, and workgroups of all tensors: as many as a sum takes, whatever the tensors' sizes are
+struct ClipPlan {
+    uint32_t each = kLeastEach;
+    int64_t parts = 0;
+};
+
+ClipPlan plan_clip(int64_t count, const regot_tensor *list)
+{
+    ClipPlan P;
+    int64_t all = 0;
+    for (int64_t t = 0; t < count; ++t) all += list[t].count / kLeastEach + 1;
+    uint32_t times = 1;
+    while (all / times > kMostParts) times *= 2;
+    P.each = kLeastEach * times;
+    for (int64_t t = 0; t < count; ++t) P.parts += (list[t].count + P.each - 1) / P.each;
+    return P;
+}
+
+template <typename Launch>
+void for_lists(int64_t count, const regot_tensor *list, ClipArgs &A, Launch launch)
+{
+    int64_t t = 0;
+    A.part = 0;
+    while (t < count) {
+        A.tensors = 0;
+        A.blocks = 0;
+        for (; t < count && A.tensors < kListed; ++t) {
+            if (list[t].count == 0) continue;
+            A.list[A.tensors++] = {list[t].data, list[t].out, list[t].count, A.blocks, list[t].type};
+            A.blocks += (uint32_t)((list[t].count + A.each - 1) / A.each);
+        }
+        if (A.blocks > 0) launch();
+        A.part += A.blocks;
+    }
+}
+
+int clip(int64_t count, const regot_tensor *list, double max_norm, float *norm, float *factor, void *workspace, size_t workspace_bytes,
+         hipStream_t s, bool scale)
+{
+    const ClipPlan P = plan_clip(count, list);
+    if (!workspace) return REGOT_ERR_NULL;
+    if (misaligned(workspace, kAlign)) return REGOT_ERR_ALIGN;
+    if (workspace_bytes < padded(P.parts * sizeof(double))) return REGOT_ERR_WORKSPACE;
+    ClipArgs A{};
+    A.each = P.each;
+    A.parts = (uint32_t)P.parts;
+    A.max_norm = max_norm;
+    A.sums = static_cast<double *>(workspace);
+    A.norm = norm;
+    A.factor = factor;
+    for_lists(count, list, A, [&] { hipLaunchKernelGGL(grad_norm_kernel, dim3(A.blocks), dim3(kThreads), 0, s, A); });
+    const bool few = scale && P.parts > 0 && P.parts <= kFewParts;
+    if (!few) hipLaunchKernelGGL(grad_factor_kernel, dim3(1), dim3(kThreads), 0, s, A);
+    if (!scale) return hip_status();
+    A.backwards = 1;
+    for_lists(count, list, A, [&] {
+        if (few) hipLaunchKernelGGL(grad_scale_kernel<true>, dim3(A.blocks), dim3(kThreads), 0, s, A);
+        else hipLaunchKernelGGL(grad_scale_kernel<false>, dim3(A.blocks), dim3(kThreads), 0, s, A);
+    });
+    return hip_status();
+}
+
+// Memory that two tensors of a list share would be scaled twice, or read after it was written.  (REGOT_ERR_HIP: no host memory to find out with.)
+int check_apart(int64_t count, const regot_tensor *list)
+{
+    struct Part {
+        uintptr_t from, to;
+        bool out;
+    };
+    const std::unique_ptr<Part[]> parts(new (std::nothrow) Part[2 * (size_t)count + 1]);
+    if (!parts) return REGOT_ERR_HIP;
+    size_t n = 0;
+    for (int64_t t = 0; t < count; ++t) {
+        if (list[t].count == 0) continue;
+        const size_t bytes = (size_t)list[t].count * element_bytes(list[t].type);
+        const uintptr_t in = (uintptr_t)list[t].data, out = (uintptr_t)list[t].out;
+        if (out != in) parts[n++] = {in, in + bytes, false};
+        parts[n++] = {out, out + bytes, true};
+    }
+    std::sort(parts.get(), parts.get() + n, [](const Part &a, const Part &b) { return a.from < b.from; });
+    uintptr_t end = 0, out_end = 0;  // of the parts so far, and of those that are written
+    for (size_t i = 0; i < n; ++i) {
+        const Part &p = parts[i];
+        if (p.from < (p.out ? end : out_end)) return REGOT_ERR_ARG;
+        end = std::max(end, p.to);
+        if (p.out) out_end = std::max(out_end, p.to);
+    }
+    return REGOT_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int regot_expert_order_workspace_bytes(int64_t n, int k, int64_t experts, size_t *bytes)
+{
+    if (!bytes) return REGOT_ERR_NULL;
+    const int st = check_order(n, k, experts);
+    if (st != REGOT_OK) return st;
+    *bytes = plan_order(n * k, experts).total;
+    return REGOT_OK;
+}
+
+int regot_expert_order(int64_t n, int k, int64_t experts, const int32_t *idx, int64_t *start, int32_t *order, int32_t *place, void *workspace,
+                       size_t workspace_bytes, regot_stream_t stream)
+{
+    const int st = check_order(n, k, experts);
+    if (st != REGOT_OK) return st;
+    if (!start || (n > 0 && (!idx || !order || !place))) return REGOT_ERR_NULL;
+    if (misaligned(start, 8) || misaligned(idx, 4) || misaligned(order, 4) || misaligned(place, 4)) return REGOT_ERR_ALIGN;
+    const OrderPlan P = plan_order(n * k, experts);
+    if (!workspace) return REGOT_ERR_NULL;
+    if (misaligned(workspace, kAlign)) return REGOT_ERR_ALIGN;
+    if (workspace_bytes < P.total) return REGOT_ERR_WORKSPACE;
+    const Memory in{idx, 1, n * k, 0, 4}, to{order, 1, n * k, 0, 4}, back{place, 1, n * k, 0, 4}, runs{start, 1, experts + 1, 0, 8};
+    if (meet(in, to) || meet(in, back) || meet(to, back) || meet(runs, in) || meet(runs, to) || meet(runs, back)) return REGOT_ERR_ARG;
+    OrderArgs A{};
+    A.idx = idx;
+    A.count = n * k;
+    A.experts = (int)experts;
+    while ((1 << A.key_bits) <= A.experts) ++A.key_bits;
+    A.each = P.each;
+    A.groups = P.groups;
+    A.counts = static_cast<uint32_t *>(workspace);
+    A.start = start;
+    A.order = order;
+    A.place = place;
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    if (P.groups > 1) hipLaunchKernelGGL(expert_count_kernel, dim3(P.groups), dim3(kOrderThreads), 0, s, A);
+    hipLaunchKernelGGL(expert_order_kernel, dim3(P.groups), dim3(kOrderThreads), 0, s, A);
+    return hip_status();
+}
+
+int regot_expert_product(int64_t rows, int64_t m, int64_t d, int64_t experts, const int64_t *start, const void *X, int type, int64_t ldX,
+                         int64_t x_rows, const int32_t *order, int k, const void *W, int w_by, int64_t ldW, int64_t strideW, int act, void *Y,
+                         int64_t ldY, void *saved, int64_t ldSaved, regot_stream_t stream)
+{
+    int st = check_group(rows, m, d, experts, start, type);
+    if (st == REGOT_OK) st = check_source(rows, d, X, ldX, x_rows, order, k, type);
+    if (st != REGOT_OK) return st;
+    if ((w_by != REGOT_W_OUTPUTS && w_by != REGOT_W_INPUTS) || (act != REGOT_ACT_NONE && act != REGOT_ACT_GATE && act != REGOT_ACT_GATE_GRAD))
+        return REGOT_ERR_ARG;
+    const int64_t wide = act == REGOT_ACT_GATE ? 2 * m : m, out = act == REGOT_ACT_GATE_GRAD ? 2 * m : m;
+    if (2 * m > kMaxDim) return REGOT_ERR_DIM;
+    const int64_t w_rows = w_by == REGOT_W_OUTPUTS ? wide : d, w_cols = w_by == REGOT_W_OUTPUTS ? d : wide;
+    const bool work = rows > 0 && m > 0 && experts > 0;
+    if (work && (!Y || (d > 0 && !W) || (act == REGOT_ACT_GATE_GRAD && !saved))) return REGOT_ERR_NULL;
+    if (ldW < w_cols || strideW < 0 || ldY < out || (saved && ldSaved < 2 * m)) return REGOT_ERR_LD;
+    const int b = element_bytes(type);
+    if (misaligned(W, b) || misaligned(Y, b) || misaligned(saved, b)) return REGOT_ERR_ALIGN;
+    if (act == REGOT_ACT_NONE) saved = nullptr;
+    if (!work) return REGOT_OK;
+    const Memory y{Y, rows, out, ldY, b}, x{X, x_rows, d, ldX, b}, kept{saved, rows, 2 * m, ldSaved, b};
+    const Memory w = blocks_of(W, experts, w_rows, w_cols, ldW, strideW, b);
+    if (meet(y, x) || meet(y, w) || meet(y, kept) || (act == REGOT_ACT_GATE && (meet(kept, x) || meet(kept, w)))) return REGOT_ERR_ARG;
+    GroupArgs A = group_args(rows, m, d, experts, start, X, ldX, x_rows, order, k);
+    A.W = W;
+    A.ldW = ldW;
+    A.strideW = strideW;
+    A.Y = Y;
+    A.ldY = ldY;
+    A.saved = saved;
+    A.ldSaved = ldSaved;
+    TilePlan P{};
+    P.kind = act == REGOT_ACT_NONE ? kPlain : act == REGOT_ACT_GATE ? kGate : kGateGrad;
+    P.across = w_by == REGOT_W_INPUTS;
+    P.out_type = type;
+    // (results are stored 8 neighbours at a time)
+    const bool direct = d > 0 && m % 8 == 0 && whole_chunks(X, d, ldX, b) && whole_chunks(W, w_cols, ldW, b) && strideW % (16 / b) == 0 &&
+                        whole_chunks(Y, m, ldY, b) && (!saved || whole_chunks(saved, m, ldSaved, b));
+    P.tile = direct ? kTileDirect : kTileStaged;
+    const TileShape T = tile_shape(P.tile);
+    A.single = rows < rows / T.rows + experts;
+    const int64_t row_tiles = A.single ? rows : rows / T.rows + experts, col_tiles = (wide + T.cols - 1) / T.cols;
+    if (row_tiles * col_tiles > kMaxDim) return REGOT_ERR_DIM;
+    A.row_tiles = (uint32_t)row_tiles;
+    A.col_tiles = (uint32_t)col_tiles;
+    A.tiles = (uint32_t)(row_tiles * col_tiles);
+    launch(A, P, type, static_cast<hipStream_t>(stream));
+    return hip_status();
+}
+
+int regot_expert_weight_grad_workspace_bytes(int64_t rows, int64_t m, int64_t d, int64_t experts, size_t *bytes)
+{
+    if (!bytes) return REGOT_ERR_NULL;
+    if (bad_dim(rows) || bad_dim(m) || bad_dim(d) || experts < 0 || experts > REGOT_ROW_MAX_EXPERTS) return REGOT_ERR_DIM;
+    *bytes = plan_weight_grad(rows, m, d, experts).total;
+    return REGOT_OK;
+}
+
+int regot_expert_weight_grad(int64_t rows, int64_t m, int64_t d, int64_t experts, const int64_t *start, const void *dY, int type, int64_t ldY,
+                             const void *X, int64_t ldX, int64_t x_rows, const int32_t *order, int k, void *dW, int out_type, int64_t ldW,
+                             int64_t strideW, void *workspace, size_t workspace_bytes, regot_stream_t stream)
+{
+    int st = check_group(rows, m, d, experts, start, type);
+    if (st == REGOT_OK) st = check_source(rows, d, X, ldX, x_rows, order, k, type);
+    if (st != REGOT_OK) return st;
+    if (out_type != type && out_type != REGOT_F32) return REGOT_ERR_ARG;
+    const bool work = m > 0 && d > 0 && experts > 0;
+    if (work && (!dW || (rows > 0 && !dY))) return REGOT_ERR_NULL;
+    if (ldY < m || ldW < d || (experts > 1 && m > 0 && strideW < (m - 1) * ldW + d)) return REGOT_ERR_LD;
+    const int b = element_bytes(type), ob = element_bytes(out_type);
+    if (misaligned(dY, b) || misaligned(dW, ob)) return REGOT_ERR_ALIGN;
+    const GradPlan G = plan_weight_grad(rows, m, d, experts);
+    if (!workspace) return REGOT_ERR_NULL;
+    if (misaligned(workspace, kAlign)) return REGOT_ERR_ALIGN;
+    if (workspace_bytes < G.total) return REGOT_ERR_WORKSPACE;
+    if (!work) return REGOT_OK;
+    const Memory w = blocks_of(dW, experts, m, d, ldW, strideW, ob);
+    if (meet(w, {dY, rows, m, ldY, b}) || meet(w, {X, x_rows, d, ldX, b})) return REGOT_ERR_ARG;
+    GroupArgs A = group_args(rows, m, d, experts, start, X, ldX, x_rows, order, k);
+    A.W = dY;
+    A.ldW = ldY;
+    A.splits = G.splits;
+    TilePlan P{};
+    P.kind = kWeightGrad;
+    P.across = 1;
+    P.gather = order != nullptr;
+    const bool parts = G.splits > 1;
+    P.out_type = parts ? REGOT_F32 : out_type;
+    A.Y = parts ? workspace : dW;
+    A.ldY = parts ? d : ldW;
+    A.strideY = parts ? m * d : strideW;
+    const int pb = element_bytes(P.out_type);
+    const bool direct = whole_chunks(X, d, ldX, b) && whole_chunks(dY, m, ldY, b) && whole_chunks(A.Y, d, A.ldY, pb) && A.strideY % (16 / pb) == 0;
+    P.tile = direct ? kTileDirect : kTileStaged;
+    const int64_t tiles = G.tiles_m * G.tiles_d * experts * G.splits;
+    if (tiles > kMaxDim) return REGOT_ERR_DIM;
+    A.row_tiles = (uint32_t)G.tiles_m;
+    A.col_tiles = (uint32_t)G.tiles_d;
+    A.tiles = (uint32_t)tiles;
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    launch(A, P, type, s);
+    if (parts) {
+        const JoinArgs J{static_cast<const float *>(workspace), experts * m * d, m, d, G.splits, dW, ldW, strideW};
+        const dim3 grid(grid_of((J.numbers + kThreads - 1) / kThreads));
+        if (out_type == REGOT_F32) hipLaunchKernelGGL(expert_join_kernel<REGOT_F32>, grid, dim3(kThreads), 0, s, J);
+        else if (out_type == REGOT_BF16) hipLaunchKernelGGL(expert_join_kernel<REGOT_BF16>, grid, dim3(kThreads), 0, s, J);
+        else hipLaunchKernelGGL(expert_join_kernel<REGOT_F16>, grid, dim3(kThreads), 0, s, J);
+    }
+    return hip_status();
+}
+
+static int check_combine(int64_t n, int k, int64_t m, int64_t rows, int type, const void *Y, int64_t ldY, const int32_t *place, const float *weight)
+{
+    if (n < 0 || bad_dim(m) || bad_dim(rows)) return REGOT_ERR_DIM;
+    if (k < 1 || k > REGOT_ROW_MAX_CHOICES || bad_type(type)) return REGOT_ERR_ARG;
+    if (n > kMaxDim / k) return REGOT_ERR_DIM;
+    if (n > 0 && (!place || (rows > 0 && m > 0 && !Y))) return REGOT_ERR_NULL;
+    if (ldY < m) return REGOT_ERR_LD;
+    if (misaligned(Y, element_bytes(type)) || misaligned(place, 4) || misaligned(weight, 4)) return REGOT_ERR_ALIGN;
+    return REGOT_OK;
+}
+
+static CombineArgs combine_args(int64_t n, int k, int64_t m, int64_t rows, const void *Y, int64_t ldY, const int32_t *place, const float *weight)
+{
+    CombineArgs A{};
+    A.n = n;
+    A.m = m;
+    A.rows = rows;
+    A.k = k;
+    A.Y = Y;
+    A.ldY = ldY;
+    A.place = place;
+    A.weight = weight;
+    return A;
+}
+
+int regot_expert_combine(int64_t n, int k, int64_t m, int64_t rows, const void *Y, int type, int64_t ldY, const int32_t *place, const float *weight,
+                         void *out, int64_t ldO, regot_stream_t stream)
+{
+    const int st = check_combine(n, k, m, rows, type, Y, ldY, place, weight);
+    if (st != REGOT_OK) return st;
+    if (n > 0 && m > 0 && !out) return REGOT_ERR_NULL;
+    if (ldO < m) return REGOT_ERR_LD;
+    const int b = element_bytes(type);
+    if (misaligned(out, b)) return REGOT_ERR_ALIGN;
+    if (n == 0 || m == 0) return REGOT_OK;
+    if (meet({out, n, m, ldO, b}, {Y, rows, m, ldY, b})) return REGOT_ERR_ARG;
+    CombineArgs A = combine_args(n, k, m, rows, Y, ldY, place, weight);
+    A.out = out;
+    A.ldO = ldO;
+    const int64_t columns = kLanes * 16 / b;
+    A.parts = (uint32_t)((m + columns - 1) / columns);
+    const dim3 grid(grid_of((n * A.parts + kWaves - 1) / kWaves));
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    if (type == REGOT_F32) hipLaunchKernelGGL(expert_combine_kernel<REGOT_F32>, grid, dim3(kThreads), 0, s, A);
+    else if (type == REGOT_BF16) hipLaunchKernelGGL(expert_combine_kernel<REGOT_BF16>, grid, dim3(kThreads), 0, s, A);
+    else hipLaunchKernelGGL(expert_combine_kernel<REGOT_F16>, grid, dim3(kThreads), 0, s, A);
+    return hip_status();
+}
+
+int regot_expert_combine_grad(int64_t n, int k, int64_t m, int64_t rows, const void *g_out, int type, int64_t ldG, const void *Y, int64_t ldY,
+                              const int32_t *place, const float *weight, void *dY, int64_t ldD, float *g_weight, regot_stream_t stream)
+{
+    const int st = check_combine(n, k, m, rows, type, g_weight ? Y : g_out, g_weight ? ldY : m, place, weight);
+    if (st != REGOT_OK) return st;
+    if (n > 0 && m > 0 && (!g_out || (rows > 0 && !dY))) return REGOT_ERR_NULL;
+    if (ldG < m || ldD < m) return REGOT_ERR_LD;
+    const int b = element_bytes(type);
+    if (misaligned(g_out, b) || misaligned(dY, b) || misaligned(g_weight, 4)) return REGOT_ERR_ALIGN;
+    if (n == 0) return REGOT_OK;
+    const Memory d{dY, rows, m, ldD, b};
+    if (meet(d, {g_out, n, m, ldG, b}) || (g_weight && meet(d, {Y, rows, m, ldY, b}))) return REGOT_ERR_ARG;
+    CombineArgs A = combine_args(n, k, m, rows, Y, ldY, place, weight);
+    A.g = g_out;
+    A.ldG = ldG;
+    A.out = dY;
+    A.ldO = ldD;
+    A.g_weight = g_weight;
+    const dim3 grid(grid_of((n * k + kWaves - 1) / kWaves));
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    if (type == REGOT_F32) hipLaunchKernelGGL(expert_combine_grad_kernel<REGOT_F32>, grid, dim3(kThreads), 0, s, A);
+    else if (type == REGOT_BF16) hipLaunchKernelGGL(expert_combine_grad_kernel<REGOT_BF16>, grid, dim3(kThreads), 0, s, A);
+    else hipLaunchKernelGGL(expert_combine_grad_kernel<REGOT_F16>, grid, dim3(kThreads), 0, s, A);
+    return hip_status();
+}
+
+int regot_grad_norm_workspace_bytes(int64_t count, const regot_tensor *list, size_t *bytes)
+{
+    if (!bytes) return REGOT_ERR_NULL;
+    const int st = check_tensors(count, list, false);
+    if (st != REGOT_OK) return st;
+    *bytes = padded(plan_clip(count, list).parts * sizeof(double));
+    return REGOT_OK;
+}
+
+int regot_grad_norm(int64_t count, const regot_tensor *list, float *norm, void *workspace, size_t workspace_bytes, regot_stream_t stream)
+{
+    const int st = check_tensors(count, list, false);
+    if (st != REGOT_OK) return st;
+    if (!norm) return REGOT_ERR_NULL;
+    if (misaligned(norm, 4)) return REGOT_ERR_ALIGN;
+    return clip(count, list, 1.0, norm, nullptr, workspace, workspace_bytes, static_cast<hipStream_t>(stream), false);
+}
+
+int regot_grad_clip(int64_t count, const regot_tensor *list, double max_norm, float *norm, float *factor, void *workspace, size_t workspace_bytes,
+                    regot_stream_t stream)
+{
+    int st = check_tensors(count, list, true);
+    if (st != REGOT_OK) return st;
+    if (!(max_norm > 0.0)) return REGOT_ERR_ARG;
+    if (!norm || !factor) return REGOT_ERR_NULL;
+    if (misaligned(norm, 4) || misaligned(factor, 4)) return REGOT_ERR_ALIGN;
+    st = check_apart(count, list);
+    if (st != REGOT_OK) return st;
+    return clip(count, list, max_norm, norm, factor, workspace, workspace_bytes, static_cast<hipStream_t>(stream), true);
+}
+
+}  // extern "C"

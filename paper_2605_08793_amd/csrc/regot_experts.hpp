@@ -1,0 +1,102 @@
+// Products grouped by expert: what the kernels share (gfx950, wave64).
+//
+// A product's rows are runs, one for each expert: rows start[e] .. start[e + 1] - 1 of Y belong to expert e.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "regot.h"
+#include "regot_rows.hpp"
+
+namespace regot {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+
+// Division by the number k of choices of a token, for numbers below 2^31: with magic = ceil(2^shift / k), shift = 31 + ceil(log2 k), the
+// quotient's error is below number * k / 2^shift < 1 of the last place.
+struct Divide {
+    uint32_t magic, shift;
+};
+
+inline Divide divide_by(uint32_t k)
+{
+    uint32_t shift = 31;
+    while ((1ull << (shift - 31)) < k) ++shift;
+    return {(uint32_t)(((1ull << shift) + k - 1) / k), shift};
+}
+
+struct GroupArgs {
+    const int64_t *start;   // [experts + 1]
+    int64_t rows;           // what start may reach
+    int experts;
+    const int32_t *order;   // row r takes row order[r] / k of X; NULL: row r
+    Divide by_k;
+    int64_t x_rows;
+    const void *X;
+    int64_t ldX;
+    const void *W;          // weights, or the gradient dY of a weight gradient
+    int64_t ldW, strideW;
+    int64_t m, d;           // product: columns of Y (before the gate: of each half) and length of its sums; weight gradient: dW is m x d
+    void *Y;                // product: rows; weight gradient: dW, or parts of it
+    int64_t ldY, strideY;
+    void *saved;
+    int64_t ldSaved;
+    uint32_t row_tiles, col_tiles, tiles;
+    int splits;
+    int single;             // tiles are numbered by their first row (fewer rows than experts)
+};
+
+// The row of X that row r of the product takes.  (An entry that is none of X's rows is not followed beyond X.)
+__device__ __forceinline__ int64_t source_row(const GroupArgs &A, int64_t r)
+{
+    if (!A.order) return r;
+    const uint32_t slot = (uint32_t)A.order[r];
+    return min((int64_t)((uint64_t)slot * A.by_k.magic >> A.by_k.shift), A.x_rows - 1);
+}
+
+// start[e], kept within the rows there are
+__device__ __forceinline__ int64_t run_start(const GroupArgs &A, int e) { return min(max(A.start[e], (int64_t)0), A.rows); }
+
+// Which rows tile t of BM rows has.  Tiles are numbered so that no sum over the experts is needed: those of expert e begin at
+// start[e] / BM + e, which leaves each at least as many numbers as it has tiles (some of them, at most one an expert, are empty).  Where there
+// are fewer rows than experts, tile t is the one that begins at row t, if one does.  A wave counts the experts before the tile, all lanes at once.
+struct Run {
+    int expert;
+    int64_t first, end;  // rows of the tile: first .. min(first + BM, end) - 1; none where first >= end
+};
+
+template <int BM>
+__device__ __forceinline__ Run find_run(const GroupArgs &A, int64_t t)
+{
+    const int lane = threadIdx.x % kLanes;
+    int e = 0;
+    for (int i = lane; i < (A.experts + kLanes - 1) / kLanes * kLanes; i += kLanes) {
+        bool before = false;
+        if (i < A.experts) {
+            const int64_t end = run_start(A, i + 1);
+            before = A.single ? end <= t : end / BM + i + 1 <= t;
+        }
+        e += __popcll(__ballot(before));
+    }
+    if (e >= A.experts) return {0, 0, 0};
+    const int64_t s = run_start(A, e), end = run_start(A, e + 1);
+    if (A.single) return {e, t, t < s || (t - s) % BM != 0 ? t : end};
+    return {e, s + (t - s / BM - e) * BM, end};
+}
+
+// Workgroups that follow each other run on different dies: each die gets a run of tiles, so that the tiles under way on one share
+// their rows and their weights in its L2.
+__device__ __forceinline__ uint32_t die_order(uint32_t b, uint32_t n)
+{
+    constexpr uint32_t kDies = 8;
+    const uint32_t die = b % kDies, each = n / kDies, more = n % kDies;
+    return die * each + min(die, more) + b / kDies;
+}
+
+__device__ __forceinline__ float sigmoid(float g) { return 1.0f / (1.0f + __expf(-g)); }
+
+}  // namespace regot

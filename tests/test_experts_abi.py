@@ -1,0 +1,146 @@
+"""What the expert calls refuse, before anything is enqueued (no GPU needed)."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2605_08793_amd import binding as B
+from paper_2605_08793_amd.experts import ExpertCombine, ExpertOrder, ExpertProduct
+from test_rows_abi import fake
+
+P, Q, R = (ctypes.c_void_p(a) for a in (0x100000, 0x200000, 0x300000))  # never dereferenced
+ODD, HALF, QUAD = ctypes.c_void_p(0x100001), ctypes.c_void_p(0x100002), ctypes.c_void_p(0x100004)
+WS = ctypes.c_void_p(0x800000)
+BIG = 1 << 40
+NULL, DIM, LD, ALIGN, WORKSPACE, ARG = -1, -2, -4, -5, -6, -7
+
+ORDER = dict(n=4, k=2, experts=3, idx=P, start=Q, order=R, place=ctypes.c_void_p(0x400000), ws=WS, ws_bytes=BIG, stream=None)
+PRODUCT = dict(rows=8, m=16, d=24, experts=3, start=ctypes.c_void_p(0x900000), X=P, type=0, ldX=24, x_rows=4, order=ctypes.c_void_p(0xa00000), k=2, W=Q,
+               w_by=0, ldW=24, strideW=16 * 24, act=0, Y=R, ldY=32, saved=ctypes.c_void_p(0x400000), ldSaved=32, stream=None)
+WEIGHT = dict(rows=8, m=16, d=24, experts=3, start=ctypes.c_void_p(0x900000), dY=P, type=1, ldY=16, X=Q, ldX=24, x_rows=4, order=ctypes.c_void_p(0xa00000),
+              k=2, dW=R, out_type=1, ldW=24, strideW=16 * 24, ws=WS, ws_bytes=BIG, stream=None)
+COMBINE = dict(n=4, k=2, m=16, rows=8, Y=P, type=0, ldY=16, place=Q, weight=Q, out=R, ldO=16, stream=None)
+COMBINE_GRAD = dict(n=4, k=2, m=16, rows=8, g_out=P, type=0, ldG=16, Y=Q, ldY=16, place=Q, weight=Q, dY=R, ldD=16, g_weight=ctypes.c_void_p(0x400000), stream=None)
+CALLS = {"regot_expert_order": ORDER, "regot_expert_product": PRODUCT, "regot_expert_weight_grad": WEIGHT, "regot_expert_combine": COMBINE,
+         "regot_expert_combine_grad": COMBINE_GRAD}
+
+REFUSED = [("regot_expert_order", a, s) for a, s in [
+    (dict(n=-1), DIM), (dict(k=0), ARG), (dict(k=33), ARG), (dict(experts=-1), DIM), (dict(experts=1025), DIM), (dict(n=1 << 30, k=2), DIM),
+    (dict(idx=None), NULL), (dict(start=None), NULL), (dict(order=None), NULL), (dict(place=None), NULL), (dict(ws=None), NULL), (dict(ws_bytes=0), WORKSPACE),
+    (dict(ws=ctypes.c_void_p(0x800010)), ALIGN), (dict(start=QUAD), ALIGN), (dict(idx=HALF), ALIGN), (dict(order=P), ARG), (dict(place=R), ARG),
+    (dict(start=P), ARG)]] + [
+    ("regot_expert_product", a, s) for a, s in [
+        (dict(rows=-1), DIM), (dict(m=1 << 31), DIM), (dict(m=1 << 30, ldY=1 << 40), DIM), (dict(d=-1), DIM), (dict(experts=1025), DIM), (dict(x_rows=-1), DIM),
+        (dict(x_rows=0), DIM), (dict(x_rows=7, order=None), DIM), (dict(k=0), ARG), (dict(k=33), ARG), (dict(type=3), ARG), (dict(w_by=2), ARG), (dict(act=3), ARG),
+        (dict(start=None), NULL), (dict(X=None), NULL), (dict(W=None), NULL), (dict(Y=None), NULL), (dict(act=2, saved=None), NULL), (dict(ldX=23), LD),
+        (dict(ldW=23), LD), (dict(w_by=1, ldW=15), LD), (dict(w_by=1, ldW=31, act=1), LD), (dict(strideW=-1), LD), (dict(ldY=15), LD), (dict(act=2, ldY=31), LD),
+        (dict(act=1, ldSaved=31), LD), (dict(start=QUAD), ALIGN), (dict(X=HALF), ALIGN), (dict(W=ODD, type=1), ALIGN), (dict(Y=HALF), ALIGN), (dict(order=ODD), ALIGN),
+        (dict(Y=P), ARG), (dict(Y=Q), ARG), (dict(Y=R, saved=R, act=1), ARG), (dict(saved=P, act=1), ARG), (dict(Y=R, saved=R, act=2), ARG)]] + [
+    ("regot_expert_weight_grad", a, s) for a, s in [
+        (dict(rows=1 << 31), DIM), (dict(m=-1), DIM), (dict(d=1 << 31), DIM), (dict(experts=-1), DIM), (dict(x_rows=0), DIM), (dict(k=0), ARG), (dict(type=-1), ARG),
+        (dict(out_type=2), ARG), (dict(out_type=3), ARG), (dict(start=None), NULL), (dict(dY=None), NULL), (dict(X=None), NULL), (dict(dW=None), NULL),
+        (dict(ldY=15), LD), (dict(ldX=23), LD), (dict(ldW=23), LD), (dict(strideW=15 * 24 + 23), LD), (dict(dW=HALF, out_type=0), ALIGN), (dict(dY=ODD), ALIGN),
+        (dict(ws=None), NULL), (dict(ws_bytes=0), WORKSPACE), (dict(ws=ctypes.c_void_p(0x800010)), ALIGN), (dict(dW=P), ARG), (dict(dW=Q), ARG)]] + [
+    ("regot_expert_combine", a, s) for a, s in [
+        (dict(n=-1), DIM), (dict(m=-1), DIM), (dict(rows=-1), DIM), (dict(n=1 << 30), DIM), (dict(k=0), ARG), (dict(k=33), ARG), (dict(type=7), ARG), (dict(Y=None), NULL),
+        (dict(place=None), NULL), (dict(out=None), NULL), (dict(ldY=15), LD), (dict(ldO=15), LD), (dict(Y=HALF), ALIGN), (dict(weight=HALF), ALIGN), (dict(out=P), ARG)]] + [
+    ("regot_expert_combine_grad", a, s) for a, s in [
+        (dict(n=-1), DIM), (dict(k=33), ARG), (dict(g_out=None), NULL), (dict(dY=None), NULL), (dict(Y=None), NULL), (dict(place=None), NULL), (dict(ldG=15), LD),
+        (dict(ldD=15), LD), (dict(ldY=15), LD), (dict(g_weight=HALF), ALIGN), (dict(dY=P), ARG), (dict(dY=Q), ARG)]]
+
+
+def call(name, **changed):
+    args = {**CALLS[name], **changed}
+    assert set(args) == set(CALLS[name])
+    return getattr(B.load(), name)(*args.values())
+
+
+@pytest.mark.parametrize("name,changed,status", REFUSED)
+def test_refused(name, changed, status):
+    assert call(name, **changed) == status
+
+
+@pytest.mark.parametrize("name,changed", [
+    ("regot_expert_product", dict(rows=0)), ("regot_expert_product", dict(m=0)), ("regot_expert_product", dict(experts=0, start=None)),
+    ("regot_expert_weight_grad", dict(m=0)), ("regot_expert_weight_grad", dict(d=0)), ("regot_expert_weight_grad", dict(experts=0, start=None)),
+    ("regot_expert_combine", dict(n=0)), ("regot_expert_combine", dict(m=0)), ("regot_expert_combine_grad", dict(n=0))])
+def test_nothing_to_do_is_fine(name, changed):
+    assert call(name, **changed) == 0
+
+
+def test_columns_of_one_wide_matrix():
+    """An output whose rows lie between an input's is refused where an element is shared, at either end.  (Those that are not would run.)"""
+    for at in (2 * 7, 2 * 57, -2 * 7, -2 * 57):
+        assert call("regot_expert_combine", n=4, m=8, rows=4, type=1, ldY=64, out=ctypes.c_void_p(0x100000 + at), ldO=64) == ARG
+
+
+def test_workspaces():
+    out = ctypes.c_size_t()
+    f = B.load().regot_expert_order_workspace_bytes
+    assert f(10, 2, 5, None) == NULL and f(-1, 2, 5, ctypes.byref(out)) == DIM and f(10, 0, 5, ctypes.byref(out)) == ARG
+    for n in (0, 1, 8192, 10 ** 6, (1 << 31) // 32 - 1):
+        assert 256 <= B.regot_expert_order_workspace_bytes(n, 32 if n > 10 ** 6 else 8, 1024) <= 256 + 2048 * 1025 * 4
+    f = B.load().regot_expert_weight_grad_workspace_bytes
+    assert f(10, 2, 5, 1, None) == NULL and f(-1, 2, 5, 1, ctypes.byref(out)) == DIM and f(1, 2, 5, 1025, ctypes.byref(out)) == DIM
+    for rows in (0, 1, 1000, 10 ** 6, (1 << 31) - 1):
+        for m, d in ((0, 5), (1, 1), (64, 64), (4096, 4096), ((1 << 31) - 1, 1)):
+            for experts in (0, 1, 8, 1024):
+                size = B.regot_expert_weight_grad_workspace_bytes(rows, m, d, experts)
+                assert size % 256 == 0 and 256 <= size <= 256 + 1024 * max(experts, 1) * 128 * 128 * 4
+
+
+def tensor(data=0x100000, out=0x100000, count=100, type=0):
+    return B._Tensor(data, out, count, type)
+
+
+def listed(*tensors):
+    return (B._Tensor * max(len(tensors), 1))(*tensors)
+
+
+def clip(tensors, max_norm=1.0, norm=P, factor=Q, ws=WS, ws_bytes=BIG, count=None):
+    return B.load().regot_grad_clip(len(tensors) if count is None else count, listed(*tensors), max_norm, norm, factor, ws, ws_bytes, None)
+
+
+def test_clip_refusals():
+    far = tensor(0x500000, 0x500000)
+    for tensors, status in (([tensor(count=-1)], DIM), ([tensor(type=3)], ARG), ([tensor(data=None)], NULL), ([tensor(out=None)], NULL), ([tensor(data=0x100002)], ALIGN),
+                            ([tensor(out=0x100001, type=1)], ALIGN), ([tensor(), tensor()], ARG), ([tensor(), far, tensor(0x100000 + 396, 0x600000)], ARG),
+                            ([tensor(out=0x100000 + 200)], ARG), ([tensor(out=0x500000), far], ARG)):
+        assert clip(tensors) == status, status
+    assert clip([tensor()], count=-1) == DIM
+    assert B.load().regot_grad_clip(1, None, 1.0, P, Q, WS, BIG, None) == NULL
+    for changed, status in ((dict(max_norm=0.0), ARG), (dict(max_norm=-1.0), ARG), (dict(max_norm=float("nan")), ARG), (dict(norm=None), NULL), (dict(factor=None), NULL),
+                            (dict(norm=HALF), ALIGN), (dict(ws=None), NULL), (dict(ws_bytes=0), WORKSPACE), (dict(ws=ctypes.c_void_p(0x800010)), ALIGN)):
+        assert clip([tensor(), far], **changed) == status, changed
+    out = ctypes.c_size_t()
+    assert B.load().regot_grad_norm_workspace_bytes(1, listed(tensor()), None) == NULL
+    assert B.load().regot_grad_norm_workspace_bytes(1, listed(tensor(count=-2)), ctypes.byref(out)) == DIM
+    assert B.load().regot_grad_norm_workspace_bytes(2, listed(tensor(), tensor(count=1 << 40)), ctypes.byref(out)) == 0 and 256 <= out.value < 1 << 19
+    assert B.load().regot_grad_norm(1, listed(tensor()), None, WS, BIG, None) == NULL
+
+
+def test_the_binding_checks_weights():
+    assert B._weights(fake(3, 4, 5))[:6] == (3, 4, 5, 0, 5, 20)
+    assert B._weights(fake(3, 5, 4).transpose(1, 2))[:6] == (3, 4, 5, 1, 4, 20)
+    assert B._weights(fake(3, 4, 9)[:, :, :5])[:6] == (3, 4, 5, 0, 9, 36)
+    assert B._weights(fake(1, 4, 5).expand(3, 4, 5))[:6] == (3, 4, 5, 0, 5, 0)
+    assert B._weights(fake(3, 1, 5))[:5] == (3, 1, 5, 0, 5)
+    for bad in (fake(3, 4), fake(3, 4, 5, dtype=torch.float64), fake(3, 4, 10)[:, :, ::2], fake(3, 1, 5).expand(3, 4, 5), torch.zeros(3, 4, 5), None):
+        with pytest.raises(TypeError):
+            B._weights(bad)
+
+
+def test_buffers_are_not_replaced_and_shapes():
+    order, product, combine = (ExpertOrder(4, 2, 3, device="cpu"), ExpertProduct(8, 16, 24, 3, gated=True, keep=True, device="cpu"),
+                               ExpertCombine(4, 2, 16, device="cpu"))
+    for op, names in ((order, ["start", "order", "place", "workspace"]), (product, ["Y", "saved"]), (combine, ["out", "g_weight"])):
+        for name in names:
+            with pytest.raises(AttributeError):
+                setattr(op, name, torch.empty(4, 9))
+            assert isinstance(getattr(op, name), torch.Tensor)
+    assert order.start.shape == (4,) and order.start.dtype == torch.int64 and order.place.shape == (4, 2)
+    assert product.Y.shape == (8, 16) and product.saved.shape == (8, 32)
+    assert ExpertProduct(8, 16, 24, 3, device="cpu").saved is None
+    for bad in (dict(dtype=torch.float64), dict(grad_dtype=torch.float16)):
+        with pytest.raises(TypeError):
+            ExpertProduct(8, 16, 24, 3, device="cpu", **bad)
