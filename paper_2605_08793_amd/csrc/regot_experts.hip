@@ -151,19 +151,25 @@ void launch(const GroupArgs &A, const TilePlan &P, int type, hipStream_t s)
     else expert_tiles_f16(A, P, s);
 }
 
+// Tiles of 256 x 256 (one to a compute unit, 128 x 128 for each wave) do more of the products for what they read than those of 128 x 128 (two to a unit), and leave
+// more of the chip empty in the last round.  us, 256 / 128: 131072 rows of 64 experts, 1024 x 2048: product 577 / 715 (4400 tiles of 256), weight gradient 648 /
+// 778 (2048 tiles); 32768 rows of 60, 2048 by 2 x 1024 with the gate 353 / 390 (1264); 8192 rows of 8, 2048 x 1408: 87 / 83 (216), weight gradient 80 / 69 (384).
+bool big_tiles(int type, int64_t tiles) { return type != REGOT_F32 && tiles >= 2 * kCUs; }
+
 // A weight gradient of few tiles is summed in parts, which a second launch adds up.
 struct GradPlan {
     int64_t tiles_m = 0, tiles_d = 0;
     int splits = 1;
     size_t total = 0;
+    int64_t tiles(int64_t experts) const { return tiles_m * tiles_d * experts * splits; }
 };
 
-GradPlan plan_weight_grad(int64_t rows, int64_t m, int64_t d, int64_t experts)
+GradPlan plan_weight_grad(int64_t rows, int64_t m, int64_t d, int64_t experts, int tile)
 {
     GradPlan P;
-    const TileShape T = tile_shape(kTileDirect);
-    P.tiles_m = (m + T.rows - 1) / T.rows;
-    P.tiles_d = (d + T.cols - 1) / T.cols;
+    const int64_t size = tile_size(tile);
+    P.tiles_m = (m + size - 1) / size;
+    P.tiles_d = (d + size - 1) / size;
     const int64_t tiles = P.tiles_m * P.tiles_d * experts;
     if (tiles > 0 && tiles < kCUs) P.splits = (int)std::max<int64_t>(std::min<int64_t>(2 * kCUs / tiles, rows / experts / 512), 1);
     P.total = padded(P.splits > 1 ? (size_t)P.splits * experts * m * d * sizeof(float) : 0);
@@ -381,10 +387,12 @@ int regot_expert_product(int64_t rows, int64_t m, int64_t d, int64_t experts, co
     // (results are stored 8 neighbours at a time)
     const bool direct = d > 0 && m % 8 == 0 && whole_chunks(X, d, ldX, b) && whole_chunks(W, w_cols, ldW, b) && strideW % (16 / b) == 0 &&
                         whole_chunks(Y, m, ldY, b) && (!saved || whole_chunks(saved, m, ldSaved, b));
-    P.tile = direct ? kTileDirect : kTileStaged;
-    const TileShape T = tile_shape(P.tile);
-    A.single = rows < rows / T.rows + experts;
-    const int64_t row_tiles = A.single ? rows : rows / T.rows + experts, col_tiles = (wide + T.cols - 1) / T.cols;
+    // (tiles of a call, where each expert's last one is half empty)
+    const auto tiles_of = [&](int64_t size) { return (rows / size + experts / 2) * ((wide + size - 1) / size); };
+    P.tile = !direct ? kTileStaged : big_tiles(type, tiles_of(256)) ? kTileBig : kTileDirect;
+    const int64_t size = tile_size(P.tile);
+    A.single = rows < rows / size + experts;
+    const int64_t row_tiles = A.single ? rows : rows / size + experts, col_tiles = (wide + size - 1) / size;
     if (row_tiles * col_tiles > kMaxDim) return REGOT_ERR_DIM;
     A.row_tiles = (uint32_t)row_tiles;
     A.col_tiles = (uint32_t)col_tiles;
@@ -397,7 +405,7 @@ int regot_expert_weight_grad_workspace_bytes(int64_t rows, int64_t m, int64_t d,
 {
     if (!bytes) return REGOT_ERR_NULL;
     if (bad_dim(rows) || bad_dim(m) || bad_dim(d) || experts < 0 || experts > REGOT_ROW_MAX_EXPERTS) return REGOT_ERR_DIM;
-    *bytes = plan_weight_grad(rows, m, d, experts).total;
+    *bytes = plan_weight_grad(rows, m, d, experts, kTileDirect).total;  // (large tiles are many, and not in parts)
     return REGOT_OK;
 }
 
@@ -414,7 +422,7 @@ int regot_expert_weight_grad(int64_t rows, int64_t m, int64_t d, int64_t experts
     if (ldY < m || ldW < d || (experts > 1 && m > 0 && strideW < (m - 1) * ldW + d)) return REGOT_ERR_LD;
     const int b = element_bytes(type), ob = element_bytes(out_type);
     if (misaligned(dY, b) || misaligned(dW, ob)) return REGOT_ERR_ALIGN;
-    const GradPlan G = plan_weight_grad(rows, m, d, experts);
+    GradPlan G = plan_weight_grad(rows, m, d, experts, kTileDirect);
     if (!workspace) return REGOT_ERR_NULL;
     if (misaligned(workspace, kAlign)) return REGOT_ERR_ALIGN;
     if (workspace_bytes < G.total) return REGOT_ERR_WORKSPACE;
@@ -437,7 +445,11 @@ int regot_expert_weight_grad(int64_t rows, int64_t m, int64_t d, int64_t experts
     const int pb = element_bytes(P.out_type);
     const bool direct = whole_chunks(X, d, ldX, b) && whole_chunks(dY, m, ldY, b) && whole_chunks(A.Y, d, A.ldY, pb) && A.strideY % (16 / pb) == 0;
     P.tile = direct ? kTileDirect : kTileStaged;
-    const int64_t tiles = G.tiles_m * G.tiles_d * experts * G.splits;
+    if (direct && big_tiles(type, plan_weight_grad(rows, m, d, experts, kTileBig).tiles(experts))) {
+        P.tile = kTileBig;
+        G = plan_weight_grad(rows, m, d, experts, kTileBig);
+    }
+    const int64_t tiles = G.tiles(experts);
     if (tiles > kMaxDim) return REGOT_ERR_DIM;
     A.row_tiles = (uint32_t)G.tiles_m;
     A.col_tiles = (uint32_t)G.tiles_d;

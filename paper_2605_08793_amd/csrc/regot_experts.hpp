@@ -51,12 +51,11 @@ struct GroupArgs {
 };
 
 // The row of X that row r of the product takes.  (An entry that is none of X's rows is not followed beyond X.)
-__device__ __forceinline__ int64_t source_row(const GroupArgs &A, int64_t r)
+__device__ __forceinline__ int64_t row_of_slot(const GroupArgs &A, uint32_t slot)
 {
-    if (!A.order) return r;
-    const uint32_t slot = (uint32_t)A.order[r];
     return min((int64_t)((uint64_t)slot * A.by_k.magic >> A.by_k.shift), A.x_rows - 1);
 }
+__device__ __forceinline__ int64_t source_row(const GroupArgs &A, int64_t r) { return A.order ? row_of_slot(A, A.order[r]) : r; }
 
 // start[e], kept within the rows there are
 __device__ __forceinline__ int64_t run_start(const GroupArgs &A, int e) { return min(max(A.start[e], (int64_t)0), A.rows); }

@@ -5,25 +5,24 @@
 
 namespace regot {
 
-enum { kTileStaged = 0, kTileDirect = 1 };
+enum { kTileStaged = 0, kTileDirect = 1, kTileBig = 2 };
 
 struct TilePlan {
     int kind, across, tile, out_type, gather;
 };
 
-struct TileShape {
-    int rows, cols;
-};
-inline TileShape tile_shape(int) { return TileShape{128, 128}; }
+inline int64_t tile_size(int tile) { return tile == kTileBig ? 256 : 128; }
 
 template <int TYPE, bool ACROSS, int KIND, int OUT, bool GATHER>
 void launch_tile(const GroupArgs &A, int tile, hipStream_t s)
 {
-    const dim3 grid(A.tiles);
-    if (tile == kTileDirect) {
-        hipLaunchKernelGGL((expert_tile_kernel<TYPE, 128, 128, 2, 2, ACROSS, KIND, true, OUT, GATHER>), grid, dim3(256), 0, s, A);
+    const dim3 grid(A.tiles), threads(256);
+    if (tile == kTileBig) {
+        if constexpr (TYPE != REGOT_F32) hipLaunchKernelGGL((expert_tile_kernel<TYPE, 256, 256, 2, 2, ACROSS, KIND, true, OUT, GATHER>), grid, threads, 0, s, A);
+    } else if (tile == kTileDirect) {
+        hipLaunchKernelGGL((expert_tile_kernel<TYPE, 128, 128, 2, 2, ACROSS, KIND, true, OUT, GATHER>), grid, threads, 0, s, A);
     } else {
-        hipLaunchKernelGGL((expert_tile_kernel<TYPE, 128, 128, 2, 2, ACROSS, KIND, false, OUT, GATHER>), grid, dim3(256), 0, s, A);
+        hipLaunchKernelGGL((expert_tile_kernel<TYPE, 128, 128, 2, 2, ACROSS, KIND, false, OUT, GATHER>), grid, threads, 0, s, A);
     }
 }
 

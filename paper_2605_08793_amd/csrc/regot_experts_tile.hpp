@@ -10,8 +10,17 @@ enum { kPlain = 0, kGate = 1, kGateGrad = 2, kWeightGrad = 3 };
 
 __device__ const uint32_t kNoNumbers[8] = {};  // what is loaded in the place of numbers that are not there: 0
 
-typedef __attribute__((address_space(3))) uint32_t LdsWord;
-typedef const __attribute__((address_space(1))) uint32_t GlobalWord;
+// 64 lanes' 16 bytes each from memory to LDS, one lane's behind the other's from `lds` on (the same in all lanes), without registers between.  Nothing waits
+// for it but s_waitcnt vmcnt.  (As the compiler's builtin it would make every read of LDS behind it wait, whatever it reads.)
+__device__ __forceinline__ void load_to_lds(const char *p, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(p) : "memory");  // (M0 is used by nothing else here)
+}
+
+__device__ __forceinline__ uint32_t lds_address(const void *p)
+{
+    return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p;
+}
 
 // One side of a tile: EXT rows (or columns) of a matrix, 128 bytes of each along the sum at a time.  LDS holds them
 //   TRANS = false (numbers along the sum are neighbours in memory): row after row, 8 chunks of 16 bytes each
@@ -71,15 +80,17 @@ struct Side {
 };
 
 // Loads of one side, kSum places of the sum at a time.  DIRECT: whole chunks that are 16 bytes aligned, from memory straight into LDS;
-// otherwise through registers, at any alignment, numbers beyond the matrix as 0.
+// the first `rest` places of a sum, which need not be kSum, come first, the others in whole stretches behind them.  Otherwise through registers, at any
+// alignment, numbers beyond the matrix as 0, the last stretch as short as it is.
 template <int TYPE, int EXT, bool TRANS, int THREADS, bool DIRECT, bool GATHER, bool HALVES>
 struct Loader {
     using S = Side<TYPE, EXT, TRANS, THREADS>;
     using Raw = typename S::Raw;
-    const char *at[S::kLoads];  // of the next chunks
+    const char *at[S::kLoads];  // of the next chunks (GATHER: of their columns)
     int64_t step;               // to those after them
     u32x4 kept[DIRECT ? 1 : S::kLoads];
-    int next_row[GATHER ? S::kLoads : 1];
+    int32_t next_slot[GATHER ? S::kLoads : 1];
+    const GroupArgs *args;
     int64_t ld;
 
     // TRANS = false: row(i) is the address of the i-th row, from the sum's first place on
@@ -105,47 +116,64 @@ struct Loader {
             at[ii] = p + c * S::kElem + (GATHER ? 0 : S::lds_row(ii) * ld);
         }
     }
-    // which rows of the matrix the places done .. done + kSum - 1 of a gathered sum are
+    // which slots the next kSum places of a gathered sum are, the first of them row `row`, all before `end`: asked for while the stretch before is on its
+    // way, and there (`gathered`) when the waves have met, so that nothing waits for them
     __device__ __forceinline__ void gather(const GroupArgs &A, int64_t row, int64_t end)
     {
+        args = &A;
 #pragma unroll
-        for (int ii = 0; ii < S::kLoads; ++ii) next_row[ii] = (int)source_row(A, min(row + S::lds_row(ii), end - 1));
+        for (int ii = 0; ii < S::kLoads; ++ii) next_slot[ii] = A.order[min(row + S::lds_row(ii), end - 1)];
     }
-    // the chunks of places done .. of a sum of `sum` places; first, extent: as for across
-    __device__ __forceinline__ void load(char *lds, int64_t done, int64_t sum, int64_t first, int64_t extent)
+    __device__ __forceinline__ void gathered()
     {
-        const bool last = done + S::kSum > sum;
+#pragma unroll
+        for (int ii = 0; ii < S::kLoads; ++ii) asm volatile("" : "+v"(next_slot[ii]));
+    }
+    __device__ __forceinline__ const char *chunk_at(int ii) const { return GATHER ? at[ii] + row_of_slot(*args, next_slot[ii]) * ld : at[ii]; }
+
+    // DIRECT: the first `rest` places; then whole stretches, load ii of one, and the way to the next (none where there is no next)
+    __device__ __forceinline__ void first(uint32_t lds, int rest)
+    {
+        const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
 #pragma unroll
         for (int ii = 0; ii < S::kLoads; ++ii) {
-            const char *p = at[ii];
-            if constexpr (GATHER) p += (int64_t)next_row[ii] * ld;
-            else at[ii] += step;
-            const int64_t k = done + (TRANS ? S::lds_row(ii) : S::chunk(ii) * S::kChunk);
-            if constexpr (DIRECT) {
-                if (last && k >= sum) p = reinterpret_cast<const char *>(kNoNumbers);
-                const int wave = threadIdx.x / kLanes;
-                __builtin_amdgcn_global_load_lds((GlobalWord *)p, (LdsWord *)(lds + (wave * S::kLoads + ii) * 1024), 16, 0, 0);
-            } else {
-                const int64_t left = TRANS ? (k < sum ? extent - first - column(ii) : 0) : sum - k;
-                u32x4 v = {0, 0, 0, 0};
-                if (left >= S::kChunk) {
-                    __builtin_memcpy(&v, p, 16);
-                } else {
-                    Raw part[S::kChunk];
+            const int k = TRANS ? S::lds_row(ii) : S::chunk(ii) * S::kChunk;
+            load_to_lds(k < rest ? chunk_at(ii) : reinterpret_cast<const char *>(kNoNumbers), lds + (wave * S::kLoads + ii) * 1024);
+            if constexpr (!GATHER) at[ii] += TRANS ? rest * ld : rest * S::kElem;
+        }
+    }
+    __device__ __forceinline__ void load(int ii, uint32_t lds, int64_t by)
+    {
+        const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
+        load_to_lds(chunk_at(ii), lds + (wave * S::kLoads + ii) * 1024);
+        if constexpr (!GATHER) at[ii] += by;
+    }
+
+    // through registers: the chunks of places done .. of a sum of `sum` places; first, extent: as for across
+    __device__ __forceinline__ void fetch(int64_t done, int64_t sum, int64_t first, int64_t extent)
+    {
 #pragma unroll
-                    for (int c = 0; c < S::kChunk; ++c) part[c] = c < left ? reinterpret_cast<const Raw *>(p)[c] : Raw(0.f);
-                    __builtin_memcpy(&v, part, 16);
-                }
-                kept[ii] = v;
+        for (int ii = 0; ii < S::kLoads; ++ii) {
+            const char *p = chunk_at(ii);
+            if constexpr (!GATHER) at[ii] += step;
+            const int64_t k = done + (TRANS ? S::lds_row(ii) : S::chunk(ii) * S::kChunk);
+            const int64_t left = TRANS ? (k < sum ? extent - first - column(ii) : 0) : sum - k;
+            u32x4 v = {0, 0, 0, 0};
+            if (left >= S::kChunk) {
+                __builtin_memcpy(&v, p, 16);
+            } else {
+                Raw part[S::kChunk];
+#pragma unroll
+                for (int c = 0; c < S::kChunk; ++c) part[c] = c < left ? reinterpret_cast<const Raw *>(p)[c] : Raw(0.f);
+                __builtin_memcpy(&v, part, 16);
             }
+            kept[ii] = v;
         }
     }
     __device__ __forceinline__ void put(char *lds)
     {
-        if constexpr (!DIRECT) {
 #pragma unroll
-            for (int ii = 0; ii < S::kLoads; ++ii) *reinterpret_cast<u32x4 *>(lds + S::place(ii) * 16) = kept[ii];
-        }
+        for (int ii = 0; ii < S::kLoads; ++ii) *reinterpret_cast<u32x4 *>(lds + S::place(ii) * 16) = kept[ii];
     }
 };
 
@@ -163,20 +191,108 @@ __device__ __forceinline__ f32x4 multiply(u32x4 a, u32x4 b, f32x4 c)
     }
 }
 
-// COUNT neighbouring results to a row of `left` (or more) numbers, the first of them at p
-template <int TYPE, int COUNT, bool WHOLE>
-__device__ __forceinline__ void store_run(void *p, const float *v, int64_t left)
+// The same for 16 bits, where it stands and with the sum in the accumulation registers: as a builtin the compiler keeps sums of 256 registers a lane in
+// the others, moves and spills them, and gathers the reads of LDS in front of the products.  What the compiler does not know to keep apart here: a
+// number that an instruction other than a load writes may be multiplied two cycles later (s_nop 1, in the shadow of the product before), and sums are read
+// behind `multiplied`.
+template <int TYPE>
+__device__ __forceinline__ void multiply_here(u32x4 a, u32x4 b, f32x4 &c)
+{
+    if constexpr (TYPE == REGOT_BF16) asm volatile("s_nop 1\n\tv_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+    else asm volatile("s_nop 1\n\tv_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+}
+
+// 0, as a product's result
+__device__ __forceinline__ void clear_here(f32x4 &c)
+{
+    const u32x4 none = {0, 0, 0, 0};
+    asm volatile("s_nop 1\n\tv_mfma_f32_16x16x32_f16 %0, %1, %1, 0" : "=a"(c) : "v"(none));
+}
+
+// Products' results before other instructions read them, which takes 18 cycles at most behind the last product: behind the wait for that, each goes
+// through an empty instruction, or its reads could come before the wait.
+template <int COUNT>
+__device__ __forceinline__ void multiplied(f32x4 (&c)[COUNT])
+{
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) asm volatile("" : "+a"(c[i]));
+}
+
+// A wave's results, ROWS x COLS fragments, through its own part of LDS, so that they go to memory as whole rows and not as the pieces of 8 or
+// 16 bytes that a lane has (131072 x 1024 by 64 x 2048 x 1024, bf16: 693 us without, see the table at the kernel).  value(x, y, e): result e of run y (of 8
+// neighbours, or 4 where ACROSS) in fragment row x; take(x, i, c, v): 16 bytes of numbers of type TYPE, row i of fragment row x, from column c on.
+// Chunks of 16 bytes lie in an order that depends on their row, as in Side.
+template <int TYPE, int ROWS, int COLS, bool ACROSS, int BYTES, typename Value, typename Take>
+__device__ __forceinline__ void through_lds(char *mine, Value value, Take take)
 {
     using Raw = typename Score<TYPE>::Raw;
-    Raw part[COUNT];
+    constexpr int kElem = sizeof(Raw), kRun = ACROSS ? 4 : 8, kRow = COLS * 16 * kElem, kChunks = kRow / 16, kPiece = kRun * kElem < 16 ? kRun * kElem : 16;
+    constexpr int kFit = BYTES / (16 * kRow), kPass = kFit < ROWS ? kFit : ROWS;
+    static_assert(kPass >= 1, "a row of fragments fits");
+    const int lane = threadIdx.x % kLanes, g = lane / 16, i = lane % 16;
 #pragma unroll
-    for (int c = 0; c < COUNT; ++c) part[c] = Score<TYPE>::put(v[c]);
+    for (int x0 = 0; x0 < ROWS; x0 += kPass) {
+#pragma unroll
+        for (int x = x0; x < min(x0 + kPass, ROWS); ++x)
+#pragma unroll
+            for (int y = 0; y < COLS * 4 / kRun; ++y) {
+                Raw v[kRun];
+#pragma unroll
+                for (int e = 0; e < kRun; ++e) v[e] = Score<TYPE>::put(value(x, y, e));
+#pragma unroll
+                for (int p = 0; p < kRun * kElem; p += kPiece) {
+                    const int at = (y * 4 * kRun + kRun * g) * kElem + p;
+                    char *to = mine + ((x - x0) * 16 + i) * kRow + ((at / 16) ^ (i & (kChunks - 1))) * 16 + at % 16;
+                    __builtin_memcpy(__builtin_assume_aligned(to, kPiece), reinterpret_cast<const char *>(v) + p, kPiece);
+                }
+            }
+        wave_lds();
+        constexpr int kRowsAtOnce = kLanes / kChunks;
+        const int row = lane / kChunks, chunk = lane % kChunks;
+#pragma unroll
+        for (int it = 0; it < min(kPass, ROWS - x0) * 16 / kRowsAtOnce; ++it) {
+            const int at = it * kRowsAtOnce + row, of = at % 16;
+            take(x0 + at / 16, of, chunk * 16 / kElem, *reinterpret_cast<const u32x4 *>(mine + at * kRow + (chunk ^ (of & (kChunks - 1))) * 16));
+        }
+        wave_lds();
+    }
+}
+
+// The same without LDS, where a lane's 8 neighbours are 16 bytes (of 64 that follow each other): 131072 x 1024 by 64 x 2048 x 1024, bf16 634 us, through LDS 653.
+template <int TYPE, int ROWS, int COLS, bool ACROSS, int BYTES, typename Value, typename Take>
+__device__ __forceinline__ void results(char *mine, Value value, Take take)
+{
+    using Raw = typename Score<TYPE>::Raw;
+    if constexpr (ACROSS) {
+        through_lds<TYPE, ROWS, COLS, ACROSS, BYTES>(mine, value, take);
+    } else {
+        constexpr int kChunk = 16 / sizeof(Raw);
+        const int lane = threadIdx.x % kLanes, g = lane / 16, i = lane % 16;
+#pragma unroll
+        for (int x = 0; x < ROWS; ++x)
+#pragma unroll
+            for (int y = 0; y < COLS / 2; ++y)
+#pragma unroll
+                for (int p = 0; p < 8; p += kChunk) {
+                    Raw v[kChunk];
+#pragma unroll
+                    for (int e = 0; e < kChunk; ++e) v[e] = Score<TYPE>::put(value(x, y, p + e));
+                    take(x, i, y * 32 + 8 * g + p, WideChunk::pack(v));
+                }
+    }
+}
+
+// The first numbers of a chunk, or as many as a row of `left` more has (WHOLE: all or none)
+template <int TYPE, int COUNT, bool WHOLE>
+__device__ __forceinline__ void store_run(void *p, const typename Score<TYPE>::Raw *v, int64_t left)
+{
+    using Raw = typename Score<TYPE>::Raw;
     if constexpr (WHOLE) {
-        if (left > 0) __builtin_memcpy(__builtin_assume_aligned(p, sizeof(part) < 16 ? sizeof(part) : 16), part, sizeof(part));
+        if (left > 0) __builtin_memcpy(__builtin_assume_aligned(p, COUNT * sizeof(Raw)), v, COUNT * sizeof(Raw));
     } else {
 #pragma unroll
         for (int c = 0; c < COUNT; ++c)
-            if (c < left) static_cast<Raw *>(p)[c] = part[c];
+            if (c < left) static_cast<Raw *>(p)[c] = v[c];
     }
 }
 
@@ -186,7 +302,7 @@ __device__ __forceinline__ void load_run(float *v, const void *p, int64_t left)
     using Raw = typename Score<TYPE>::Raw;
     Raw part[COUNT];
     if constexpr (WHOLE) {
-        __builtin_memcpy(part, __builtin_assume_aligned(p, sizeof(part) < 16 ? sizeof(part) : 16), sizeof(part));
+        __builtin_memcpy(part, __builtin_assume_aligned(p, COUNT * sizeof(Raw)), COUNT * sizeof(Raw));
     } else {
 #pragma unroll
         for (int c = 0; c < COUNT; ++c) part[c] = c < left ? static_cast<const Raw *>(p)[c] : Raw(0.f);
@@ -199,7 +315,7 @@ __device__ __forceinline__ void load_run(float *v, const void *p, int64_t left)
 // in a row.  Rows: of X (product), or columns of dY (weight gradient, summed over rows).  Columns: rows of W (of its columns where ACROSS;
 // with the gate half of them are g's and half u's), or columns of X.
 template <int TYPE, int BM, int BN, int WM, int WN, bool ACROSS, int KIND, bool DIRECT, int OUT, bool GATHER>
-__global__ void __launch_bounds__(WM *WN *kLanes) expert_tile_kernel(const GroupArgs A)
+__device__ __forceinline__ void expert_tile(const GroupArgs &A, const Run &run, uint32_t b, char *lds)
 {
     constexpr int kThreadsHere = WM * WN * kLanes;
     constexpr bool kAcrossRows = KIND == kWeightGrad;
@@ -209,9 +325,8 @@ __global__ void __launch_bounds__(WM *WN *kLanes) expert_tile_kernel(const Group
     constexpr int kElem = sizeof(Raw), kSum = Rows::kSum;
     constexpr int kFragRows = BM / WM / 16, kFragCols = BN / WN / 16;
     static_assert(kFragCols % 2 == 0 && (kAcrossRows || kFragRows % 2 == 0), "fragments come in pairs");
-    __shared__ __attribute__((aligned(1024))) char rows0[Rows::kBytes], cols0[Cols::kBytes], rows1[Rows::kBytes], cols1[Cols::kBytes];
-
-    const uint32_t b = die_order(blockIdx.x, A.tiles);
+    // two stretches of the sum: the rows' numbers, and the columns' behind them
+    constexpr int kStretch = Rows::kBytes + Cols::kBytes;
     Loader<TYPE, BM, kAcrossRows, kThreadsHere, DIRECT, false, false> rows;
     Loader<TYPE, BN, ACROSS, kThreadsHere, DIRECT, KIND == kWeightGrad && GATHER, KIND == kGate> cols;
     int64_t first_row, row_end, first_col, col_end, sum, from = 0;
@@ -233,8 +348,6 @@ __global__ void __launch_bounds__(WM *WN *kLanes) expert_tile_kernel(const Group
         if constexpr (GATHER)
             if (sum > 0) cols.gather(A, from, from + sum);
     } else {
-        const Run run = find_run<BM>(A, b / A.col_tiles);
-        if (run.first >= run.end) return;
         expert = run.expert;
         first_row = run.first;
         row_end = run.end;
@@ -264,117 +377,207 @@ __global__ void __launch_bounds__(WM *WN *kLanes) expert_tile_kernel(const Group
             return Cols::fragment(lds, wn * kFragCols, f, step);
         }
     };
-    f32x4 acc[kFragRows][kFragCols] = {};
-    const auto compute = [&](const char *r, const char *c) {
+    constexpr bool kHere = DIRECT && TYPE != REGOT_F32;
+    f32x4 acc[kFragRows][kFragCols];
 #pragma unroll
-        for (int step = 0; step < 2; ++step) {
-            u32x4 fr[kFragRows], fc[kFragCols];
+    for (int xy = 0; xy < kFragRows * kFragCols; ++xy) {
+        if constexpr (kHere) clear_here(acc[xy / kFragCols][xy % kFragCols]);
+        else acc[xy / kFragCols][xy % kFragCols] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    struct Fragments {
+        u32x4 rows[kFragRows], cols[kFragCols];
+    };
+    constexpr int kFragments = kFragRows + kFragCols, kAtOnce = kFragRows * kFragCols / kFragments;
+    const auto read_one = [&](Fragments &F, const char *from, int step, int f) {
+        if (f < kFragCols) F.cols[f] = col_fragment(from + Rows::kBytes, f, step);
+        else F.rows[f - kFragCols] = Rows::fragment(from, wm * kFragRows, f - kFragCols, step);
+    };
+    const auto read = [&](Fragments &F, const char *from, int step) {
 #pragma unroll
-            for (int f = 0; f < kFragCols; ++f) fc[f] = col_fragment(c, f, step);
+        for (int f = 0; f < kFragments; ++f) read_one(F, from, step, f);
+    };
+    const auto add_some = [&](const Fragments &F, int first, int last) {
 #pragma unroll
-            for (int f = 0; f < kFragRows; ++f) fr[f] = Rows::fragment(r, wm * kFragRows, f, step);
-#pragma unroll
-            for (int x = 0; x < kFragRows; ++x)
-#pragma unroll
-                for (int y = 0; y < kFragCols; ++y) acc[x][y] = multiply<TYPE>(fc[y], fr[x], acc[x][y]);
+        for (int xy = first; xy < last; ++xy) {
+            const int x = xy / kFragCols, y = xy % kFragCols;
+            if constexpr (kHere) multiply_here<TYPE>(F.cols[y], F.rows[x], acc[x][y]);
+            else acc[x][y] = multiply<TYPE>(F.cols[y], F.rows[x], acc[x][y]);
         }
     };
-    int64_t done = 0;
-    const auto load = [&](char *r, char *c) {
-        rows.load(r, done, sum, first_row, row_end);
-        cols.load(c, done, sum, first_col, col_end);
-        done += kSum;
-        if constexpr (KIND == kWeightGrad && GATHER)
-            if (done < sum) cols.gather(A, from + done, from + sum);
-    };
-    const auto put = [&](char *r, char *c) {
-        rows.put(r);
-        cols.put(c);
-    };
-    const auto all_there = [&] {
-        if constexpr (DIRECT) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (this wave's loads into LDS; the barrier: everybody's)
-        __syncthreads();
-    };
-    if (sum > 0) {
-        load(rows0, cols0);
-        put(rows0, cols0);
-        for (int64_t t = 0;; t += 2 * kSum) {
+    const auto add = [&](const Fragments &F) { add_some(F, 0, kFragRows * kFragCols); };
+    if constexpr (DIRECT) {
+        // Two stretches of the sum are in LDS or on their way.  While a step's fragments are multiplied, the next step's are read; when the last of a stretch have
+        // been read (by all waves: the barrier), its place is filled with the stretch after the next.
+        constexpr int kLoads = decltype(rows)::S::kLoads + decltype(cols)::S::kLoads, kRowLoads = decltype(rows)::S::kLoads;
+        const int stretches = (int)((sum + kSum - 1) / kSum);
+        const uint32_t lds_at = lds_address(lds);
+        const auto load_one = [&](int ii, uint32_t to, bool more) {
+            if (ii < kRowLoads) rows.load(ii, to, more ? rows.step : 0);
+            else cols.load(ii - kRowLoads, to + Rows::kBytes, more ? cols.step : 0);
+        };
+        const auto all_there = [&] {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (this wave's loads into LDS)
+            __syncthreads();
+            if constexpr (KIND == kWeightGrad && GATHER) cols.gathered();
+        };
+        if (stretches > 0) {
+            int64_t done = sum - (int64_t)(stretches - 1) * kSum;
+            const auto next_rows = [&] {
+                if constexpr (KIND == kWeightGrad && GATHER) cols.gather(A, from + done, from + sum);
+            };
+            Fragments even, odd;
+            rows.first(lds_at, (int)done);
+            cols.first(lds_at + Rows::kBytes, (int)done);
+            next_rows();
             all_there();
-            if (t + kSum < sum) load(rows1, cols1);
-            compute(rows0, cols0);
-            if (t + kSum >= sum) break;
-            put(rows1, cols1);
-            all_there();
-            if (t + 2 * kSum < sum) load(rows0, cols0);
-            compute(rows1, cols1);
-            if (t + 2 * kSum >= sum) break;
-            put(rows0, cols0);
+            if (stretches > 1) {
+#pragma unroll
+                for (int ii = 0; ii < kLoads; ++ii) load_one(ii, lds_at + kStretch, stretches > 2);
+                done += stretches > 2 ? kSum : 0;
+                next_rows();
+            }
+            read(even, lds, 0);
+            uint32_t here = 0;
+            // kAtOnce products for each fragment that is read, so that neither waits for the other
+            const auto first_half = [&] {
+#pragma unroll
+                for (int f = 0; f < kFragments; ++f) {
+                    read_one(odd, lds + here, 1, f);
+                    add_some(even, f * kAtOnce, f + 1 < kFragments ? (f + 1) * kAtOnce : kFragRows * kFragCols);
+                }
+            };
+            for (int t = 1; t < stretches; ++t) {
+                first_half();
+                all_there();
+                const bool more = t + 2 < stretches;  // (where there is no stretch after the next, the next one is loaded once more, for nobody)
+                constexpr int kEach = (kLoads + kFragments - 1) / kFragments;
+#pragma unroll
+                for (int f = 0; f < kFragments; ++f) {
+#pragma unroll
+                    for (int ii = f * kEach; ii < min((f + 1) * kEach, kLoads); ++ii) load_one(ii, lds_at + here, more);
+                    read_one(even, lds + (here ^ kStretch), 0, f);
+                    add_some(odd, f * kAtOnce, f + 1 < kFragments ? (f + 1) * kAtOnce : kFragRows * kFragCols);
+                }
+                done += more ? kSum : 0;
+                next_rows();
+                here ^= kStretch;
+            }
+            first_half();
+            add(odd);
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (nothing is on its way into LDS when the workgroup ends)
+        }
+        if constexpr (kHere) {
+            asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+#pragma unroll
+            for (int x = 0; x < kFragRows; ++x) multiplied(acc[x]);
+        }
+    } else if (sum > 0) {
+        int64_t done = 0;  // of the sum: what has been asked for
+        const auto load = [&] {
+            rows.fetch(done, sum, first_row, row_end);
+            cols.fetch(done, sum, first_col, col_end);
+            done += kSum;
+            if constexpr (KIND == kWeightGrad && GATHER)
+                if (done < sum) cols.gather(A, from + done, from + sum);
+        };
+        const auto put = [&](char *to) {
+            rows.put(to);
+            cols.put(to + Rows::kBytes);
+        };
+        load();
+        put(lds);
+        for (uint32_t here = 0;; here ^= kStretch) {
+            __syncthreads();
+            const bool more = done < sum;
+            if (more) load();
+            Fragments F;
+            read(F, lds + here, 0);
+            add(F);
+            read(F, lds + here, 1);
+            add(F);
+            if (!more) break;
+            put(lds + (here ^ kStretch));
         }
     }
 
-    // results: fragments y and y + 1 of a pair are 8 neighbours of a row, or two runs of 4
-    constexpr int kOutElem = sizeof(typename Score<OUT>::Raw);
-    const auto row_of = [&](int x) {
+    // results: a run y of 8 neighbours is that of fragments 2 y and 2 y + 1, one of 4 (ACROSS) that of fragment y
+    __syncthreads();
+    constexpr int kOutElem = sizeof(typename Score<OUT>::Raw), kMine = 2 * kStretch / (WM * WN);
+    char *const mine = lds + wave * kMine;
+    const auto row_of = [&](int x, int i) {
         return first_row + (wm * kFragRows + (kAcrossRows ? x : x / 2 * 2)) * 16 + (kAcrossRows ? i : 8 * (i / 4) + 4 * (x % 2) + i % 4);
     };
-    constexpr int kRun = ACROSS ? 4 : 8;
+    const auto result = [&](int x, int y, int e) { return acc[x][ACROSS ? y : 2 * y + e / 4][e % 4]; };
     if constexpr (KIND == kGate) {
         constexpr int kHalf = kFragCols / 2;
         static_assert(KIND != kGate || kHalf % 2 == 0, "halves are pairs of fragments");
-#pragma unroll
-        for (int x = 0; x < kFragRows; ++x) {
-            const int64_t r = row_of(x);
-            if (r >= row_end) continue;
-#pragma unroll
-            for (int y = 0; y < kHalf; y += kRun / 4) {
-                const int64_t c = first_col + (wn * kHalf + y) * 16 + kRun * g;
-                float gate[kRun], up[kRun], h[kRun];
-#pragma unroll
-                for (int e = 0; e < kRun; ++e) {
-                    gate[e] = acc[x][y + e / 4][e % 4];
-                    up[e] = acc[x][kHalf + y + e / 4][e % 4];
-                    h[e] = gate[e] * sigmoid(gate[e]) * up[e];
-                }
-                store_run<TYPE, kRun, DIRECT>(static_cast<char *>(A.Y) + (r * A.ldY + c) * kElem, h, col_end - c);
-                if (A.saved) {
-                    char *s = static_cast<char *>(A.saved) + (r * A.ldSaved + c) * kElem;
-                    store_run<TYPE, kRun, DIRECT>(s, gate, col_end - c);
-                    store_run<TYPE, kRun, DIRECT>(s + col_end * kElem, up, col_end - c);
-                }
-            }
+        constexpr int kUp = ACROSS ? kHalf : kHalf / 2;  // runs of g
+        const auto store = [&](char *to, int64_t ld) {
+            return [=](int x, int i, int c, u32x4 v) {
+                const int64_t r = row_of(x, i), col = first_col + wn * kHalf * 16 + c;
+                Raw part[16 / kElem];
+                __builtin_memcpy(part, &v, 16);
+                if (r < row_end) store_run<TYPE, 16 / kElem, DIRECT>(to + (r * ld + col) * kElem, part, col_end - col);
+            };
+        };
+        results<TYPE, kFragRows, kHalf, ACROSS, kMine>(mine, [&](int x, int y, int e) {
+            const float gate = result(x, y, e);
+            return gate * sigmoid(gate) * result(x, kUp + y, e);
+        }, store(static_cast<char *>(A.Y), A.ldY));
+        if (A.saved) {
+            results<TYPE, kFragRows, kHalf, ACROSS, kMine>(mine, result, store(static_cast<char *>(A.saved), A.ldSaved));
+            results<TYPE, kFragRows, kHalf, ACROSS, kMine>(mine, [&](int x, int y, int e) { return result(x, kUp + y, e); },
+                                                               store(static_cast<char *>(A.saved) + col_end * kElem, A.ldSaved));
         }
+    } else if constexpr (KIND == kGateGrad) {
+        through_lds<REGOT_F32, kFragRows, kFragCols, ACROSS, kMine>(mine, result, [&](int x, int i, int c, u32x4 v) {
+            const int64_t r = row_of(x, i), col = first_col + wn * kFragCols * 16 + c, left = col_end - col;
+            if (r >= row_end || left <= 0) return;
+            const char *s = static_cast<const char *>(A.saved) + (r * A.ldSaved + col) * kElem;
+            float gate[4], up[4];
+            load_run<TYPE, 4, DIRECT>(gate, s, left);
+            load_run<TYPE, 4, DIRECT>(up, s + col_end * kElem, left);
+            Raw dg[4], du[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float p = sigmoid(gate[e]), D = __uint_as_float(v[e]);
+                dg[e] = Score<TYPE>::put(D * up[e] * (p * (1.0f + gate[e] * (1.0f - p))));
+                du[e] = Score<TYPE>::put(D * (gate[e] * p));
+            }
+            char *to = static_cast<char *>(A.Y) + (r * A.ldY + col) * kElem;
+            store_run<TYPE, 4, DIRECT>(to, dg, left);
+            store_run<TYPE, 4, DIRECT>(to + col_end * kElem, du, left);
+        });
     } else {
         char *Y = static_cast<char *>(A.Y);
         if constexpr (KIND == kWeightGrad) Y += ((int64_t)part * A.experts + expert) * A.strideY * kOutElem;
-#pragma unroll
-        for (int x = 0; x < kFragRows; ++x) {
-            const int64_t r = row_of(x);
-            if (r >= row_end) continue;
-#pragma unroll
-            for (int y = 0; y < kFragCols; y += kRun / 4) {
-                const int64_t c = first_col + (wn * kFragCols + y) * 16 + kRun * g;
-                float v[kRun];
-#pragma unroll
-                for (int e = 0; e < kRun; ++e) v[e] = acc[x][y + e / 4][e % 4];
-                if constexpr (KIND == kGateGrad) {
-                    if (c >= col_end) continue;
-                    const char *s = static_cast<const char *>(A.saved) + (r * A.ldSaved + c) * kElem;
-                    float gate[kRun], up[kRun];
-                    load_run<TYPE, kRun, DIRECT>(gate, s, col_end - c);
-                    load_run<TYPE, kRun, DIRECT>(up, s + col_end * kElem, col_end - c);
-#pragma unroll
-                    for (int e = 0; e < kRun; ++e) {
-                        const float p = sigmoid(gate[e]), D = v[e];
-                        v[e] = D * up[e] * (p * (1.0f + gate[e] * (1.0f - p)));
-                        up[e] = D * (gate[e] * p);
-                    }
-                    store_run<TYPE, kRun, DIRECT>(Y + (r * A.ldY + c) * kElem, v, col_end - c);
-                    store_run<TYPE, kRun, DIRECT>(Y + (r * A.ldY + col_end + c) * kElem, up, col_end - c);
-                } else {
-                    store_run<OUT, kRun, DIRECT>(Y + (r * A.ldY + c) * kOutElem, v, col_end - c);
-                }
+        results<OUT, kFragRows, kFragCols, ACROSS, kMine>(mine, result, [&](int x, int i, int c, u32x4 v) {
+            const int64_t r = row_of(x, i), col = first_col + wn * kFragCols * 16 + c;
+            typename Score<OUT>::Raw of[16 / kOutElem];
+            __builtin_memcpy(of, &v, 16);
+            if (r < row_end) store_run<OUT, 16 / kOutElem, DIRECT>(Y + (r * A.ldY + col) * kOutElem, of, col_end - col);
+        });
+    }
+}
+
+// A workgroup: one tile.  A run's last tile that has half of its rows or less is one of half the height.
+template <int TYPE, int BM, int BN, int WM, int WN, bool ACROSS, int KIND, bool DIRECT, int OUT, bool GATHER>
+__global__ void __launch_bounds__(WM *WN *kLanes, BM + BN <= 320 ? 2 : 1) expert_tile_kernel(const GroupArgs A)
+{
+    __shared__ __attribute__((aligned(1024))) char lds[2 * 128 * (BM + BN)];
+    const uint32_t b = die_order(blockIdx.x, A.tiles);
+    if constexpr (KIND == kWeightGrad) {
+        expert_tile<TYPE, BM, BN, WM, WN, ACROSS, KIND, DIRECT, OUT, GATHER>(A, Run{}, b, lds);
+    } else {
+        const Run run = find_run<BM>(A, b / A.col_tiles);
+        if (run.first >= run.end) return;
+        if constexpr (BM / WM % 64 == 0) {
+            if (run.end - run.first <= BM / 2) {
+                expert_tile<TYPE, BM / 2, BN, WM, WN, ACROSS, KIND, DIRECT, OUT, GATHER>(A, run, b, lds);
+                return;
             }
         }
+        expert_tile<TYPE, BM, BN, WM, WN, ACROSS, KIND, DIRECT, OUT, GATHER>(A, run, b, lds);
     }
 }
 
