@@ -40,7 +40,7 @@ unsigned grid_of(int64_t blocks) { return (unsigned)std::min(blocks, kMaxGrid); 
 
 // ---- the order of choices ----
 
-constexpr int kOneGroup = 16384;  // choices that one workgroup puts in order, in one launch
+constexpr int64_t kOneGroup = 8192;  // choices that one workgroup puts in order, in one launch
 constexpr int kMostGroups = 128;
 
 struct OrderPlan {
@@ -155,6 +155,14 @@ void launch(const GroupArgs &A, const TilePlan &P, int type, hipStream_t s)
 // more of the chip empty in the last round.  us, 256 / 128: 131072 rows of 64 experts, 1024 x 2048: product 577 / 715 (4400 tiles of 256), weight gradient 648 /
 // 778 (2048 tiles); 32768 rows of 60, 2048 by 2 x 1024 with the gate 353 / 390 (1264); 8192 rows of 8, 2048 x 1408: 87 / 83 (216), weight gradient 80 / 69 (384).
 bool big_tiles(int type, int64_t tiles) { return type != REGOT_F32 && tiles >= 2 * kCUs; }
+
+// (us, tiles of 128 x 128 / few rows, 1400 x 2048 fp16: 256 rows of 60 experts 74 / 70, 512 rows 99 / 83)
+constexpr int64_t kFewRows = 16;  // rows of an expert, on average
+
+// How many stretches of 32 rows of W a workgroup of the kernel for few rows has, of `all` that each of `runs` experts' weights have: four rounds of workgroups, one to a
+// compute unit, so that the last one does not weigh much.  us, 1 / 2 / 4 / 8 / 16 stretches: 256 rows of 60 experts, 1400 x 2048 fp16 104 / 81 / 70 / 81 / 98; 8 rows of 256
+// experts, 2048 x 2 x 1024 bf16 with the gate 13.7 / 14.1 / 14.9 / 20 / 34.
+int64_t few_groups(int64_t runs, int64_t all) { return std::min(all, (runs * all + 4 * kCUs - 1) / (4 * kCUs)); }
 
 // A weight gradient of few tiles is summed in parts, which a second launch adds up.
 struct GradPlan {
@@ -389,10 +397,14 @@ int regot_expert_product(int64_t rows, int64_t m, int64_t d, int64_t experts, co
                         whole_chunks(Y, m, ldY, b) && (!saved || whole_chunks(saved, m, ldSaved, b));
     // (tiles of a call, where each expert's last one is half empty)
     const auto tiles_of = [&](int64_t size) { return (rows / size + experts / 2) * ((wide + size - 1) / size); };
-    P.tile = !direct ? kTileStaged : big_tiles(type, tiles_of(256)) ? kTileBig : kTileDirect;
-    const int64_t size = tile_size(P.tile);
+    P.units = (d * b + 128 * kFewWaves - 1) / (128 * kFewWaves);
+    const bool few = direct && !P.across && P.kind != kGateGrad && rows <= kFewRows * experts && P.units <= kFewUnits;
+    P.tile = few ? kTileFew : !direct ? kTileStaged : big_tiles(type, tiles_of(256)) ? kTileBig : kTileDirect;
+    const int64_t size = few ? 16 : tile_size(P.tile);
+    if (few) A.groups = (int)few_groups(std::min(rows, experts), (wide + 31) / 32);
+    const int64_t cols = few ? 32 * A.groups : size;
     A.single = rows < rows / size + experts;
-    const int64_t row_tiles = A.single ? rows : rows / size + experts, col_tiles = (wide + size - 1) / size;
+    const int64_t row_tiles = A.single ? rows : rows / size + experts, col_tiles = (wide + cols - 1) / cols;
     if (row_tiles * col_tiles > kMaxDim) return REGOT_ERR_DIM;
     A.row_tiles = (uint32_t)row_tiles;
     A.col_tiles = (uint32_t)col_tiles;

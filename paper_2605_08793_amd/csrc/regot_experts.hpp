@@ -47,6 +47,7 @@ struct GroupArgs {
     int64_t ldSaved;
     uint32_t row_tiles, col_tiles, tiles;
     int splits;
+    int groups;             // few rows: stretches of 32 rows of W that a workgroup has
     int single;             // tiles are numbered by their first row (fewer rows than experts)
 };
 
@@ -71,18 +72,32 @@ struct Run {
 template <int BM>
 __device__ __forceinline__ Run find_run(const GroupArgs &A, int64_t t)
 {
+    constexpr int kAtOnce = 4;
     const int lane = threadIdx.x % kLanes;
-    int e = 0;
-    for (int i = lane; i < (A.experts + kLanes - 1) / kLanes * kLanes; i += kLanes) {
-        bool before = false;
-        if (i < A.experts) {
-            const int64_t end = run_start(A, i + 1);
-            before = A.single ? end <= t : end / BM + i + 1 <= t;
+    const int first_start = (int)run_start(A, 0);
+    int e = 0, s = 0, end = 0x7fffffff;  // experts before the tile; the largest end of one of those, the smallest of another
+    for (int i0 = lane; i0 - lane < A.experts; i0 += kAtOnce * kLanes) {
+        int ends[kAtOnce];
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) ends[j] = (int)run_start(A, min(i0 + j * kLanes + 1, A.experts));
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) {
+            const int i = i0 + j * kLanes;
+            const bool is = i < A.experts, before = is && (A.single ? ends[j] <= t : ends[j] / BM + i + 1 <= t);
+            e += __popcll(__ballot(before));
+            s = before ? max(s, ends[j]) : s;
+            end = is && !before ? min(end, ends[j]) : end;
         }
-        e += __popcll(__ballot(before));
     }
     if (e >= A.experts) return {0, 0, 0};
-    const int64_t s = run_start(A, e), end = run_start(A, e + 1);
+#pragma unroll
+    for (int d = 1; d < kLanes; d *= 2) {
+        s = max(s, __shfl_xor(s, d));
+        end = min(end, __shfl_xor(end, d));
+    }
+    s = __builtin_amdgcn_readfirstlane(e == 0 ? first_start : s);
+    end = __builtin_amdgcn_readfirstlane(end);
+    e = __builtin_amdgcn_readfirstlane(e);
     if (A.single) return {e, t, t < s || (t - s) % BM != 0 ? t : end};
     return {e, s + (t - s / BM - e) * BM, end};
 }

@@ -1,14 +1,16 @@
 // Products grouped by expert: which kernel a call runs.  One source for each type of numbers includes this.
 #pragma once
 
+#include "regot_experts_few.hpp"
 #include "regot_experts_tile.hpp"
 
 namespace regot {
 
-enum { kTileStaged = 0, kTileDirect = 1, kTileBig = 2 };
+enum { kTileStaged = 0, kTileDirect = 1, kTileBig = 2, kTileFew = 3 };
 
 struct TilePlan {
     int kind, across, tile, out_type, gather;
+    int64_t units;  // few rows: what a wave has of a sum
 };
 
 inline int64_t tile_size(int tile) { return tile == kTileBig ? 256 : 128; }
@@ -29,7 +31,16 @@ void launch_tile(const GroupArgs &A, int tile, hipStream_t s)
 template <int TYPE>
 void launch_tiles(const GroupArgs &A, const TilePlan &P, hipStream_t s)
 {
-    if (P.kind == kWeightGrad) {
+    if (P.tile == kTileFew) {
+        const dim3 grid(A.tiles), threads(kFewWaves * kLanes);
+        if (P.units <= 4) {
+            if (P.kind == kGate) hipLaunchKernelGGL((expert_few_kernel<TYPE, true, 4>), grid, threads, 0, s, A);
+            else hipLaunchKernelGGL((expert_few_kernel<TYPE, false, 4>), grid, threads, 0, s, A);
+        } else {
+            if (P.kind == kGate) hipLaunchKernelGGL((expert_few_kernel<TYPE, true, kFewUnits>), grid, threads, 0, s, A);
+            else hipLaunchKernelGGL((expert_few_kernel<TYPE, false, kFewUnits>), grid, threads, 0, s, A);
+        }
+    } else if (P.kind == kWeightGrad) {
         if (P.out_type == REGOT_F32) P.gather ? launch_tile<TYPE, true, kWeightGrad, REGOT_F32, true>(A, P.tile, s) : launch_tile<TYPE, true, kWeightGrad, REGOT_F32, false>(A, P.tile, s);
         else P.gather ? launch_tile<TYPE, true, kWeightGrad, TYPE, true>(A, P.tile, s) : launch_tile<TYPE, true, kWeightGrad, TYPE, false>(A, P.tile, s);
     } else if (P.across) {

@@ -59,22 +59,35 @@ __global__ void __launch_bounds__(kOrderThreads) expert_order_kernel(const Order
     uint32_t *const my_next = next + wave * E;
     count_choices(A, mine, end, my_next);
     __syncthreads();
-    // thread t: experts 2 t and 2 t + 1 (1025 of them at most, with none), a thread's and then the experts' sums
-    uint32_t all[2] = {0, 0}, before[2] = {0, 0};
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int e = 2 * threadIdx.x + j;
-        if (e >= E) continue;
-        if (A.groups > 1) {
-            for (int b = 0; b < A.groups; ++b) {
+    // what all workgroups have of each expert, and those before this one: every thread takes a share of the workgroups
+    __shared__ uint32_t of_all[REGOT_ROW_MAX_EXPERTS + 1], of_before[REGOT_ROW_MAX_EXPERTS + 1];
+    if (A.groups > 1) {
+        for (int e = threadIdx.x; e < E; e += kOrderThreads) of_all[e] = of_before[e] = 0;
+        __syncthreads();
+        const int shares = max(kOrderThreads / E, 1), share = threadIdx.x / E;
+        for (int e = threadIdx.x % E; e < E && share < shares; e += kOrderThreads) {
+            uint32_t all = 0, before = 0;
+#pragma unroll 8
+            for (int b = share; b < A.groups; b += shares) {
                 const uint32_t v = A.counts[(int64_t)b * E + e];
-                all[j] += v;
-                if (b < (int)blockIdx.x) before[j] += v;
+                all += v;
+                before += b < (int)blockIdx.x ? v : 0;
             }
-        } else {
-            for (int w = 0; w < kOrderWaves; ++w) all[j] += next[w * E + e];
+            atomicAdd(&of_all[e], all);
+            atomicAdd(&of_before[e], before);
+        }
+    } else {
+        for (int e = threadIdx.x; e < E; e += kOrderThreads) {
+            uint32_t v = 0;
+            for (int w = 0; w < kOrderWaves; ++w) v += next[w * E + e];
+            of_all[e] = v;
+            of_before[e] = 0;
         }
     }
+    __syncthreads();
+    // thread t: experts 2 t and 2 t + 1 (1025 of them at most, with none), a thread's and then the experts' sums
+    const auto of = [&](const uint32_t *counts, int e) { return e < E ? counts[e] : 0; };
+    const uint32_t all[2] = {of(of_all, 2 * threadIdx.x), of(of_all, 2 * threadIdx.x + 1)};
     uint32_t sum = all[0] + all[1];
 #pragma unroll
     for (int d = 1; d < kLanes; d *= 2) {
@@ -91,7 +104,7 @@ __global__ void __launch_bounds__(kOrderThreads) expert_order_kernel(const Order
         if (e >= E) continue;
         const uint32_t begin = first + (j ? all[0] : 0);
         if (blockIdx.x == 0) A.start[e] = begin;
-        uint32_t at = begin + before[j];
+        uint32_t at = begin + of_before[e];
         for (int w = 0; w < kOrderWaves; ++w) {
             const uint32_t here = next[w * E + e];
             next[w * E + e] = at;
