@@ -151,10 +151,17 @@ void launch(const GroupArgs &A, const TilePlan &P, int type, hipStream_t s)
     else expert_tiles_f16(A, P, s);
 }
 
-// Tiles of 256 x 256 (one to a compute unit, 128 x 128 for each wave) do more of the products for what they read than those of 128 x 128 (two to a unit), and leave
-// more of the chip empty in the last round.  us, 256 / 128: 131072 rows of 64 experts, 1024 x 2048: product 577 / 715 (4400 tiles of 256), weight gradient 648 /
-// 778 (2048 tiles); 32768 rows of 60, 2048 by 2 x 1024 with the gate 353 / 390 (1264); 8192 rows of 8, 2048 x 1408: 87 / 83 (216), weight gradient 80 / 69 (384).
-bool big_tiles(int type, int64_t tiles) { return type != REGOT_F32 && tiles >= 2 * kCUs; }
+// Tiles of 256 x 256 (one to a compute unit, 128 x 128 for each wave) do more of the products for what they read than those of 128 x 128 (two to a unit) or 64 x 128
+// (three), and leave more of the chip empty in the last round.  us, 256 / 128: 131072 rows of 64 experts, 1024 x 2048: product 577 / 715 (4400 tiles of 256),
+// weight gradient 648 / 778 (2048 tiles); 32768 rows of 60, 2048 by 2 x 1024 with the gate 353 / 390 (1264); 8192 rows of 8, 2048 x 1408: 87 / 83 (216), weight gradient
+// 80 / 69 (384).  128 / 64 rows: gradients of 2997 rows of 12 experts, 555 x 777: fp32 285 / 161, bf16 50 / 46 (250 and 420 tiles of 128).
+template <typename Tiles>
+int choose_tile(int type, bool direct, Tiles tiles)
+{
+    if (direct && type != REGOT_F32 && tiles(tile_shape(kTileBig)) >= 2 * kCUs) return kTileBig;
+    const bool small = tiles(tile_shape(kTileDirect)) < 2 * kCUs;
+    return direct ? small ? kTileDirectSmall : kTileDirect : small ? kTileStagedSmall : kTileStaged;
+}
 
 // (us, tiles of 128 x 128 / few rows, 1400 x 2048 fp16: 256 rows of 60 experts 74 / 70, 512 rows 99 / 83)
 constexpr int64_t kFewRows = 16;  // rows of an expert, on average
@@ -175,9 +182,9 @@ struct GradPlan {
 GradPlan plan_weight_grad(int64_t rows, int64_t m, int64_t d, int64_t experts, int tile)
 {
     GradPlan P;
-    const int64_t size = tile_size(tile);
-    P.tiles_m = (m + size - 1) / size;
-    P.tiles_d = (d + size - 1) / size;
+    const TileShape T = tile_shape(tile);
+    P.tiles_m = (m + T.rows - 1) / T.rows;
+    P.tiles_d = (d + T.cols - 1) / T.cols;
     const int64_t tiles = P.tiles_m * P.tiles_d * experts;
     if (tiles > 0 && tiles < kCUs) P.splits = (int)std::max<int64_t>(std::min<int64_t>(2 * kCUs / tiles, rows / experts / 512), 1);
     P.total = padded(P.splits > 1 ? (size_t)P.splits * experts * m * d * sizeof(float) : 0);
@@ -395,16 +402,18 @@ int regot_expert_product(int64_t rows, int64_t m, int64_t d, int64_t experts, co
     // (results are stored 8 neighbours at a time)
     const bool direct = d > 0 && m % 8 == 0 && whole_chunks(X, d, ldX, b) && whole_chunks(W, w_cols, ldW, b) && strideW % (16 / b) == 0 &&
                         whole_chunks(Y, m, ldY, b) && (!saved || whole_chunks(saved, m, ldSaved, b));
-    // (tiles of a call, where each expert's last one is half empty)
-    const auto tiles_of = [&](int64_t size) { return (rows / size + experts / 2) * ((wide + size - 1) / size); };
     P.units = (d * b + 128 * kFewWaves - 1) / (128 * kFewWaves);
-    const bool few = direct && !P.across && P.kind != kGateGrad && rows <= kFewRows * experts && P.units <= kFewUnits;
-    P.tile = few ? kTileFew : !direct ? kTileStaged : big_tiles(type, tiles_of(256)) ? kTileBig : kTileDirect;
-    const int64_t size = few ? 16 : tile_size(P.tile);
-    if (few) A.groups = (int)few_groups(std::min(rows, experts), (wide + 31) / 32);
-    const int64_t cols = few ? 32 * A.groups : size;
-    A.single = rows < rows / size + experts;
-    const int64_t row_tiles = A.single ? rows : rows / size + experts, col_tiles = (wide + cols - 1) / cols;
+    if (direct && !P.across && P.kind != kGateGrad && rows <= kFewRows * experts && P.units <= kFewUnits) {
+        P.tile = kTileFew;
+        A.groups = (int)few_groups(std::min(rows, experts), (wide + 31) / 32);
+    } else {
+        // (tiles of a call, where each expert's last one is half empty)
+        P.tile = choose_tile(type, direct, [&](TileShape T) { return (rows / T.rows + experts / 2) * ((wide + T.cols - 1) / T.cols); });
+    }
+    const TileShape T = tile_shape(P.tile);
+    const int64_t cols = P.tile == kTileFew ? T.cols * A.groups : T.cols;
+    A.single = rows < rows / T.rows + experts;
+    const int64_t row_tiles = A.single ? rows : rows / T.rows + experts, col_tiles = (wide + cols - 1) / cols;
     if (row_tiles * col_tiles > kMaxDim) return REGOT_ERR_DIM;
     A.row_tiles = (uint32_t)row_tiles;
     A.col_tiles = (uint32_t)col_tiles;
@@ -417,7 +426,7 @@ int regot_expert_weight_grad_workspace_bytes(int64_t rows, int64_t m, int64_t d,
 {
     if (!bytes) return REGOT_ERR_NULL;
     if (bad_dim(rows) || bad_dim(m) || bad_dim(d) || experts < 0 || experts > REGOT_ROW_MAX_EXPERTS) return REGOT_ERR_DIM;
-    *bytes = plan_weight_grad(rows, m, d, experts, kTileDirect).total;  // (large tiles are many, and not in parts)
+    *bytes = plan_weight_grad(rows, m, d, experts, kTileDirectSmall).total;  // (larger tiles are many, and not in parts)
     return REGOT_OK;
 }
 
@@ -434,7 +443,7 @@ int regot_expert_weight_grad(int64_t rows, int64_t m, int64_t d, int64_t experts
     if (ldY < m || ldW < d || (experts > 1 && m > 0 && strideW < (m - 1) * ldW + d)) return REGOT_ERR_LD;
     const int b = element_bytes(type), ob = element_bytes(out_type);
     if (misaligned(dY, b) || misaligned(dW, ob)) return REGOT_ERR_ALIGN;
-    GradPlan G = plan_weight_grad(rows, m, d, experts, kTileDirect);
+    GradPlan G = plan_weight_grad(rows, m, d, experts, kTileDirectSmall);
     if (!workspace) return REGOT_ERR_NULL;
     if (misaligned(workspace, kAlign)) return REGOT_ERR_ALIGN;
     if (workspace_bytes < G.total) return REGOT_ERR_WORKSPACE;
@@ -456,10 +465,12 @@ int regot_expert_weight_grad(int64_t rows, int64_t m, int64_t d, int64_t experts
     A.strideY = parts ? m * d : strideW;
     const int pb = element_bytes(P.out_type);
     const bool direct = whole_chunks(X, d, ldX, b) && whole_chunks(dY, m, ldY, b) && whole_chunks(A.Y, d, A.ldY, pb) && A.strideY % (16 / pb) == 0;
-    P.tile = direct ? kTileDirect : kTileStaged;
-    if (direct && big_tiles(type, plan_weight_grad(rows, m, d, experts, kTileBig).tiles(experts))) {
-        P.tile = kTileBig;
-        G = plan_weight_grad(rows, m, d, experts, kTileBig);
+    P.tile = kTileDirectSmall;
+    if (!parts) P.tile = choose_tile(type, direct, [&](TileShape T) { return (m + T.rows - 1) / T.rows * ((d + T.cols - 1) / T.cols) * experts; });
+    else if (!direct) P.tile = kTileStagedSmall;
+    if (!parts) {
+        G = plan_weight_grad(rows, m, d, experts, P.tile);
+        G.splits = 1;
     }
     const int64_t tiles = G.tiles(experts);
     if (tiles > kMaxDim) return REGOT_ERR_DIM;

@@ -6,14 +6,23 @@
 
 namespace regot {
 
-enum { kTileStaged = 0, kTileDirect = 1, kTileBig = 2, kTileFew = 3 };
+enum { kTileStaged, kTileDirect, kTileStagedSmall, kTileDirectSmall, kTileBig, kTileFew };
 
 struct TilePlan {
     int kind, across, tile, out_type, gather;
     int64_t units;  // few rows: what a wave has of a sum
 };
 
-inline int64_t tile_size(int tile) { return tile == kTileBig ? 256 : 128; }
+struct TileShape {
+    int64_t rows, cols;
+};
+inline TileShape tile_shape(int tile)
+{
+    if (tile == kTileBig) return {256, 256};
+    if (tile == kTileStagedSmall || tile == kTileDirectSmall) return {64, 128};
+    if (tile == kTileFew) return {16, 32};
+    return {128, 128};
+}
 
 template <int TYPE, bool ACROSS, int KIND, int OUT, bool GATHER>
 void launch_tile(const GroupArgs &A, int tile, hipStream_t s)
@@ -23,8 +32,12 @@ void launch_tile(const GroupArgs &A, int tile, hipStream_t s)
         if constexpr (TYPE != REGOT_F32) hipLaunchKernelGGL((expert_tile_kernel<TYPE, 256, 256, 2, 2, ACROSS, KIND, true, OUT, GATHER>), grid, threads, 0, s, A);
     } else if (tile == kTileDirect) {
         hipLaunchKernelGGL((expert_tile_kernel<TYPE, 128, 128, 2, 2, ACROSS, KIND, true, OUT, GATHER>), grid, threads, 0, s, A);
-    } else {
+    } else if (tile == kTileDirectSmall) {
+        hipLaunchKernelGGL((expert_tile_kernel<TYPE, 64, 128, 2, 2, ACROSS, KIND, true, OUT, GATHER>), grid, threads, 0, s, A);
+    } else if (tile == kTileStaged) {
         hipLaunchKernelGGL((expert_tile_kernel<TYPE, 128, 128, 2, 2, ACROSS, KIND, false, OUT, GATHER>), grid, threads, 0, s, A);
+    } else {
+        hipLaunchKernelGGL((expert_tile_kernel<TYPE, 64, 128, 2, 2, ACROSS, KIND, false, OUT, GATHER>), grid, threads, 0, s, A);
     }
 }
 

@@ -191,7 +191,48 @@ __device__ __forceinline__ f32x4 multiply(u32x4 a, u32x4 b, f32x4 c)
     }
 }
 
-// The same for 16 bits, where it stands and with the sum in the accumulation registers: as a builtin the compiler keeps sums of 256 registers a lane in
+// 8 numbers of 32 bits as three of 8 significant bits each, which add up to them exactly (numbers that are not finite, or round to infinity, give a NaN)
+struct Pieces {
+    u32x4 high, mid, low;
+    static __device__ __forceinline__ uint32_t rounded(float x, float y)
+    {
+        typedef float f32x2 __attribute__((ext_vector_type(2)));
+        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x, y}, bf16x2));
+    }
+    __device__ __forceinline__ Pieces(u32x4 a, u32x4 b)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float x = __uint_as_float(i < 2 ? a[2 * i] : b[2 * i - 4]), y = __uint_as_float(i < 2 ? a[2 * i + 1] : b[2 * i - 3]);
+            high[i] = rounded(x, y);
+            x -= __uint_as_float(high[i] << 16);
+            y -= __uint_as_float(high[i] & 0xffff0000u);
+            mid[i] = rounded(x, y);
+            x -= __uint_as_float(mid[i] << 16);
+            y -= __uint_as_float(mid[i] & 0xffff0000u);
+            low[i] = rounded(x, y);
+        }
+    }
+};
+
+// The products of pieces that are not below 2^-24 of the whole, the smallest first: 6 of 16 cycles in the place of 8 of 32 for the same numbers as they are
+template <int COUNT>
+__device__ __forceinline__ void multiply_pieces(const Pieces (&a)[COUNT], const Pieces &b, f32x4 (&c)[COUNT])
+{
+    const auto add = [&](u32x4 Pieces::*p, u32x4 Pieces::*q) {
+#pragma unroll
+        for (int y = 0; y < COUNT; ++y) c[y] = multiply<REGOT_BF16>(a[y].*p, b.*q, c[y]);
+    };
+    add(&Pieces::low, &Pieces::high);
+    add(&Pieces::high, &Pieces::low);
+    add(&Pieces::mid, &Pieces::mid);
+    add(&Pieces::mid, &Pieces::high);
+    add(&Pieces::high, &Pieces::mid);
+    add(&Pieces::high, &Pieces::high);
+}
+
+// A product of 16 bits where it stands and with the sum in the accumulation registers: as a builtin the compiler keeps sums of 256 registers a lane in
 // the others, moves and spills them, and gathers the reads of LDS in front of the products.  What the compiler does not know to keep apart here: a
 // number that an instruction other than a load writes may be multiplied two cycles later (s_nop 1, in the shadow of the product before), and sums are read
 // behind `multiplied`.
@@ -343,10 +384,6 @@ __device__ __forceinline__ void expert_tile(const GroupArgs &A, const Run &run, 
         const int64_t each = ((count + kSum - 1) / kSum + A.splits - 1) / A.splits * kSum;
         from = s + min(part * each, count);
         sum = min(each, count - min(part * each, count));
-        rows.across(static_cast<const char *>(A.W) + from * A.ldW * kElem, A.ldW, first_row, row_end);
-        cols.across(static_cast<const char *>(A.X) + (GATHER ? 0 : from * A.ldX * kElem), A.ldX, first_col, col_end);
-        if constexpr (GATHER)
-            if (sum > 0) cols.gather(A, from, from + sum);
     } else {
         expert = run.expert;
         first_row = run.first;
@@ -354,17 +391,26 @@ __device__ __forceinline__ void expert_tile(const GroupArgs &A, const Run &run, 
         first_col = (int64_t)(b % A.col_tiles) * (KIND == kGate ? BN / 2 : BN);
         col_end = A.m;
         sum = A.d;
-        const char *W = static_cast<const char *>(A.W) + expert * A.strideW * kElem;
-        rows.rows([&](int i) { return static_cast<const char *>(A.X) + source_row(A, min(first_row + i, row_end - 1)) * A.ldX * kElem; });
-        if constexpr (ACROSS) {
-            cols.across(W, A.ldW, first_col, col_end);
-        } else {
-            cols.rows([&](int i) {
-                const int64_t c = KIND == kGate ? min(first_col + i % (BN / 2), col_end - 1) + (i >= BN / 2 ? col_end : 0) : min(first_col + i, col_end - 1);
-                return W + c * A.ldW * kElem;
-            });
-        }
     }
+    const auto begin = [&] {
+        if constexpr (KIND == kWeightGrad) {
+            rows.across(static_cast<const char *>(A.W) + from * A.ldW * kElem, A.ldW, first_row, row_end);
+            cols.across(static_cast<const char *>(A.X) + (GATHER ? 0 : from * A.ldX * kElem), A.ldX, first_col, col_end);
+            if constexpr (GATHER)
+                if (sum > 0) cols.gather(A, from, from + sum);
+        } else {
+            const char *W = static_cast<const char *>(A.W) + expert * A.strideW * kElem;
+            rows.rows([&](int i) { return static_cast<const char *>(A.X) + source_row(A, min(first_row + i, row_end - 1)) * A.ldX * kElem; });
+            if constexpr (ACROSS) {
+                cols.across(W, A.ldW, first_col, col_end);
+            } else {
+                cols.rows([&](int i) {
+                    const int64_t c = KIND == kGate ? min(first_col + i % (BN / 2), col_end - 1) + (i >= BN / 2 ? col_end : 0) : min(first_col + i, col_end - 1);
+                    return W + c * A.ldW * kElem;
+                });
+            }
+        }
+    };
 
     const int wave = threadIdx.x / kLanes, lane = threadIdx.x % kLanes, g = lane / 16, i = lane % 16;
     const int wm = wave / WN, wn = wave % WN;
@@ -379,11 +425,13 @@ __device__ __forceinline__ void expert_tile(const GroupArgs &A, const Run &run, 
     };
     constexpr bool kHere = DIRECT && TYPE != REGOT_F32;
     f32x4 acc[kFragRows][kFragCols];
+    const auto clear = [&] {
 #pragma unroll
-    for (int xy = 0; xy < kFragRows * kFragCols; ++xy) {
-        if constexpr (kHere) clear_here(acc[xy / kFragCols][xy % kFragCols]);
-        else acc[xy / kFragCols][xy % kFragCols] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
+        for (int xy = 0; xy < kFragRows * kFragCols; ++xy) {
+            if constexpr (kHere) clear_here(acc[xy / kFragCols][xy % kFragCols]);
+            else acc[xy / kFragCols][xy % kFragCols] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+    };
     struct Fragments {
         u32x4 rows[kFragRows], cols[kFragCols];
     };
@@ -405,7 +453,9 @@ __device__ __forceinline__ void expert_tile(const GroupArgs &A, const Run &run, 
         }
     };
     const auto add = [&](const Fragments &F) { add_some(F, 0, kFragRows * kFragCols); };
-    if constexpr (DIRECT) {
+    if constexpr (kHere) {
+        begin();
+        clear();
         // Two stretches of the sum are in LDS or on their way.  While a step's fragments are multiplied, the next step's are read; when the last of a stretch have
         // been read (by all waves: the barrier), its place is filled with the stretch after the next.
         constexpr int kLoads = decltype(rows)::S::kLoads + decltype(cols)::S::kLoads, kRowLoads = decltype(rows)::S::kLoads;
@@ -466,37 +516,105 @@ __device__ __forceinline__ void expert_tile(const GroupArgs &A, const Run &run, 
             add(odd);
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (nothing is on its way into LDS when the workgroup ends)
         }
-        if constexpr (kHere) {
-            asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+        asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
 #pragma unroll
-            for (int x = 0; x < kFragRows; ++x) multiplied(acc[x]);
-        }
-    } else if (sum > 0) {
-        int64_t done = 0;  // of the sum: what has been asked for
-        const auto load = [&] {
-            rows.fetch(done, sum, first_row, row_end);
-            cols.fetch(done, sum, first_col, col_end);
-            done += kSum;
-            if constexpr (KIND == kWeightGrad && GATHER)
-                if (done < sum) cols.gather(A, from + done, from + sum);
-        };
-        const auto put = [&](char *to) {
-            rows.put(to);
-            cols.put(to + Rows::kBytes);
-        };
-        load();
-        put(lds);
-        for (uint32_t here = 0;; here ^= kStretch) {
-            __syncthreads();
-            const bool more = done < sum;
-            if (more) load();
+        for (int x = 0; x < kFragRows; ++x) multiplied(acc[x]);
+    } else {
+        // Numbers of 32 bits are multiplied in pieces.  A tile whose sums are not all finite is summed once more as the numbers are, and gives its results in the place of
+        // those that are not, so that infinities and NaNs are those of the numbers.  us, pieces / numbers as they are: 8192 rows of 60 experts, 2048 by 2 x 1024 with the gate
+        // 600 / 829, gradients of 2048 x 1024 611 / 833, of 777 x 555 with 2997 rows of 12 107 / 137.  The splitting (361 vector instructions for 96 products) bounds it.
+        const auto stretch = [&](const char *at, bool pieces) {
+            if constexpr (TYPE == REGOT_F32) {
+                if (pieces) {
+                    const auto of_col = [&](int f) { return Pieces(col_fragment(at + Rows::kBytes, f, 0), col_fragment(at + Rows::kBytes, f, 1)); };
+                    const auto of_row = [&](int f) { return Pieces(Rows::fragment(at, wm * kFragRows, f, 0), Rows::fragment(at, wm * kFragRows, f, 1)); };
+                    if constexpr (kFragCols == 4) {
+                        const Pieces c[4] = {of_col(0), of_col(1), of_col(2), of_col(3)};
+#pragma unroll
+                        for (int x = 0; x < kFragRows; ++x) multiply_pieces(c, of_row(x), acc[x]);
+                    }
+                    return;
+                }
+            }
             Fragments F;
-            read(F, lds + here, 0);
+            read(F, at, 0);
             add(F);
-            read(F, lds + here, 1);
+            read(F, at, 1);
             add(F);
-            if (!more) break;
-            put(lds + (here ^ kStretch));
+        };
+        const auto pass = [&](bool pieces) {
+            begin();
+            clear();
+            if constexpr (DIRECT) {
+                const int stretches = (int)((sum + kSum - 1) / kSum);
+                const uint32_t lds_at = lds_address(lds);
+                if (stretches > 0) {
+                    int64_t done = sum - (int64_t)(stretches - 1) * kSum;
+                    const auto next_rows = [&] {
+                        if constexpr (KIND == kWeightGrad && GATHER) cols.gather(A, from + done, from + sum);
+                    };
+                    rows.first(lds_at, (int)done);
+                    cols.first(lds_at + Rows::kBytes, (int)done);
+                    next_rows();
+                    uint32_t here = 0;
+                    for (int t = 1; t <= stretches; ++t) {
+                        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (this wave's loads into LDS)
+                        __syncthreads();
+                        if (t < stretches) {
+                            if constexpr (KIND == kWeightGrad && GATHER) cols.gathered();
+                            const uint32_t to = lds_at + (here ^ kStretch);
+#pragma unroll
+                            for (int ii = 0; ii < decltype(rows)::S::kLoads; ++ii) rows.load(ii, to, rows.step);
+#pragma unroll
+                            for (int ii = 0; ii < decltype(cols)::S::kLoads; ++ii) cols.load(ii, to + Rows::kBytes, cols.step);
+                            done += kSum;
+                            next_rows();
+                        }
+                        stretch(lds + here, pieces);
+                        here ^= kStretch;
+                    }
+                }
+            } else if (sum > 0) {
+                int64_t done = 0;  // of the sum: what has been asked for
+                const auto load = [&] {
+                    rows.fetch(done, sum, first_row, row_end);
+                    cols.fetch(done, sum, first_col, col_end);
+                    done += kSum;
+                    if constexpr (KIND == kWeightGrad && GATHER)
+                        if (done < sum) cols.gather(A, from + done, from + sum);
+                };
+                const auto put = [&](char *to) {
+                    rows.put(to);
+                    cols.put(to + Rows::kBytes);
+                };
+                load();
+                put(lds);
+                for (uint32_t here = 0;; here ^= kStretch) {
+                    __syncthreads();
+                    const bool more = done < sum;
+                    if (more) load();
+                    stretch(lds + here, pieces);
+                    if (!more) break;
+                    put(lds + (here ^ kStretch));
+                }
+            }
+        };
+        pass(TYPE == REGOT_F32);
+        if constexpr (TYPE == REGOT_F32) {
+            const auto finite = [](const f32x4 &v) { return fabsf(v[0]) < kInf && fabsf(v[1]) < kInf && fabsf(v[2]) < kInf && fabsf(v[3]) < kInf; };
+            bool all_finite = true;
+#pragma unroll
+            for (int xy = 0; xy < kFragRows * kFragCols; ++xy) all_finite &= finite(acc[xy / kFragCols][xy % kFragCols]);
+            if (__builtin_expect(!__syncthreads_and(all_finite), 0)) {
+                f32x4 first[kFragRows][kFragCols];
+                __builtin_memcpy(first, acc, sizeof(acc));
+                pass(false);
+#pragma unroll
+                for (int xy = 0; xy < kFragRows * kFragCols; ++xy)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (fabsf(first[xy / kFragCols][xy % kFragCols][e]) < kInf) acc[xy / kFragCols][xy % kFragCols][e] = first[xy / kFragCols][xy % kFragCols][e];
+            }
         }
     }
 
