@@ -167,9 +167,13 @@ int choose_tile(int type, bool direct, Tiles tiles)
 constexpr int64_t kFewRows = 16;  // rows of an expert, on average
 
 // How many stretches of 32 rows of W a workgroup of the kernel for few rows has, of `all` that each of `runs` experts' weights have: four rounds of workgroups, one to a
-// compute unit, so that the last one does not weigh much.  us, 1 / 2 / 4 / 8 / 16 stretches: 256 rows of 60 experts, 1400 x 2048 fp16 104 / 81 / 70 / 81 / 98; 8 rows of 256
-// experts, 2048 x 2 x 1024 bf16 with the gate 13.7 / 14.1 / 14.9 / 20 / 34.
-int64_t few_groups(int64_t runs, int64_t all) { return std::min(all, (runs * all + 4 * kCUs - 1) / (4 * kCUs)); }
+// compute unit, so that the last one does not weigh much, or one where two stretches are enough for that.  us, 1 / 2 / 4 / 8 / 16 stretches: 256 rows of 60 experts, 1400 x
+// 2048 fp16 104 / 81 / 70 / 81 / 98; 8 rows of 256 experts, 2048 x 2 x 1024 bf16 with the gate 13.7 to 18 / 14.3 / 15 / 20 / 34.
+int64_t few_groups(int64_t runs, int64_t all)
+{
+    const auto rounds = [&](int64_t n) { return (runs * all + n * kCUs - 1) / (n * kCUs); };
+    return std::min(all, std::max(rounds(4), std::min<int64_t>(rounds(1), 2)));
+}
 
 // A weight gradient of few tiles is summed in parts, which a second launch adds up.
 struct GradPlan {
@@ -216,8 +220,8 @@ __global__ void __launch_bounds__(kThreads) expert_join_kernel(const JoinArgs A)
 // ---- the norm ----
 
 constexpr uint32_t kLeastEach = 8 * kThreads;  // numbers of a workgroup
-constexpr int64_t kMostParts = 16384;
-constexpr uint32_t kFewParts = 1024;           // partial sums that each workgroup of the scaling adds up itself
+constexpr int64_t kMostParts = 16384;  // (4096: 1.2 GB in 300 tensors 759 us in the place of 692, the ends of the launches are longer)
+constexpr uint32_t kFewParts = 2048;           // partial sums that each workgroup of the scaling adds up itself
 
 int check_tensors(int64_t count, const regot_tensor *list, bool clip)
 {

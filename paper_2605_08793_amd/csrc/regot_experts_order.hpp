@@ -29,6 +29,7 @@ __device__ __forceinline__ int choice(const OrderArgs &A, int64_t s)
 __device__ __forceinline__ void count_choices(const OrderArgs &A, int64_t from, int64_t to, uint32_t *mine)
 {
     const int lane = threadIdx.x % kLanes;
+#pragma unroll 4
     for (int64_t s = from + lane; s < to; s += kLanes) atomicAdd(&mine[choice(A, s)], 1u);
 }
 
@@ -112,25 +113,33 @@ __global__ void __launch_bounds__(kOrderThreads) expert_order_kernel(const Order
         }
     }
     __syncthreads();
-    for (int64_t s0 = mine; s0 < end; s0 += kLanes) {
-        const int64_t s = s0 + lane;
-        const bool live = s < end;
-        const int e = live ? choice(A, s) : 0;
-        uint64_t same = __ballot(live);
-        for (int bit = 0; bit < A.key_bits; ++bit) {
-            const bool set = e >> bit & 1;
-            const uint64_t b = __ballot(set);
-            same &= set ? b : ~b;
-        }
-        if (live) {
-            const uint32_t rank = __popcll(same & ((1ull << lane) - 1));
-            const uint32_t r = my_next[e] + rank;
+    constexpr int kHeld = 8;  // choices that a lane asks for at a time
+    for (int64_t s0 = mine; s0 < end; s0 += kHeld * kLanes) {
+        int held[kHeld];
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j) held[j] = s0 + j * kLanes + lane < end ? choice(A, s0 + j * kLanes + lane) : 0;
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j) {
+            if (s0 + j * kLanes >= end) break;
+            const int64_t s = s0 + j * kLanes + lane;
+            const bool live = s < end;
+            const int e = held[j];
+            uint64_t same = __ballot(live);
+            for (int bit = 0; bit < A.key_bits; ++bit) {
+                const bool set = e >> bit & 1;
+                const uint64_t b = __ballot(set);
+                same &= set ? b : ~b;
+            }
+            if (live) {
+                const uint32_t rank = __popcll(same & ((1ull << lane) - 1));
+                const uint32_t r = my_next[e] + rank;
+                wave_lds();
+                if (rank == 0) my_next[e] = r + __popcll(same);
+                A.order[r] = e < A.experts ? (int32_t)s : -1;
+                A.place[s] = e < A.experts ? (int32_t)r : -1;
+            }
             wave_lds();
-            if (rank == 0) my_next[e] = r + __popcll(same);
-            A.order[r] = e < A.experts ? (int32_t)s : -1;
-            A.place[s] = e < A.experts ? (int32_t)r : -1;
         }
-        wave_lds();
     }
 }
 

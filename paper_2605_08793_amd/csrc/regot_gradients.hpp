@@ -101,6 +101,7 @@ __global__ void __launch_bounds__(kThreads) grad_norm_kernel(const ClipArgs A)
 __device__ __forceinline__ float clip_factor(const ClipArgs &A, bool tell)
 {
     double v = 0.0;
+#pragma unroll 8
     for (uint32_t i = threadIdx.x; i < A.parts; i += kThreads) v += A.sums[i];
     const double norm = sqrt(block_total(v));
     const float factor = norm > A.max_norm && norm < __builtin_inf() ? (float)(A.max_norm / norm) : 1.f;
