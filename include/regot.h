@@ -773,7 +773,7 @@ int regot_expert_combine_grad(int64_t n, int k, int64_t m, int64_t rows,
  *     out       = factor * data, rounded once, for each tensor; out may be data, and is then not written where factor is 1
  * `list` is a HOST array, read during the call; each tensor is `count` numbers without gaps.  Types may differ.  regot_grad_norm does not look at
  * `out`.  Tensors whose outputs share memory with each other, or with another's numbers, are refused: they would be scaled twice.
- * max_norm > 0 (inf: nothing is scaled).  The workspace's size depends on the tensors' counts.
+ * max_norm > 0 (inf: nothing is scaled).  count <= 2^40.  The workspace's size depends on the tensors' counts.
  */
 typedef struct {
     const void *data;  /* device */

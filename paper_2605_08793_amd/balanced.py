@@ -2,7 +2,7 @@
 
     python -m paper_2605_08793_amd.balanced
 
-Two uses of one idea.  Scores of n rows against m columns are the negative costs of a transport problem with uniform
+Three uses of one idea.  Scores of n rows against m columns are the negative costs of a transport problem with uniform
 marginals; its column duals beta, added to the scores, spread the rows evenly over the columns.
 
 `train_student`: a teacher's scores of samples against prototypes are balanced by a few Sinkhorn sweeps; the best columns of
@@ -11,11 +11,16 @@ gradient in one call), and its answers are looked at with RowLogprob.
 
 `route_tokens`: a router's scores of tokens against experts are balanced in the same way; RowRoute takes the duals as its
 bias, and regot_pattern_transpose puts the choices into the order of the experts.
+
+`train_experts`: a layer of gated experts behind such a router learns a map.  ExpertOrder puts the choices into the order of the experts,
+ExpertProduct multiplies each expert's tokens by its weights, ExpertCombine adds a token's answers up under the router's weights; their
+gradients lead back to the weights and, through RowRoute, to the router, and GradClip bounds the norm of a step.
 """
 import torch
 
 from . import binding as B
 from .driver import DualPass
+from .experts import ExpertCombine, ExpertOrder, ExpertProduct, GradClip
 from .rows import RowDistill, RowLogprob, RowRoute
 
 
@@ -82,9 +87,75 @@ def route_tokens(n=4096, experts=64, k=2, sweeps=8, dtype=torch.float32, seed=0)
     return dict(load_balanced=load[0], load_plain=load[1], start=start, tokens=tokens, idx=balanced.idx, weight=balanced.weight, grad=grad)
 
 
+class ExpertLayer:
+    """A gated layer of n tokens: k of `experts` experts each, features -> 2 x hidden -> features.
+
+    `forward` leaves the answers in .out, `backward` the gradients in .grads: of W_up (experts, 2 hidden, features), of W_down (experts, features, hidden), of
+    the router's scores, and of the tokens as the experts take them."""
+
+    def __init__(self, n, features, hidden, experts, k, dtype=torch.bfloat16):
+        self.k = k
+        self.route = RowRoute(n, experts, k, bias_on="logit", dtype=torch.float32)
+        self.order = ExpertOrder(n, k, experts)
+        self.up = ExpertProduct(n * k, hidden, features, experts, gated=True, keep=True, dtype=dtype, grad_dtype=torch.float32)
+        self.down = ExpertProduct(n * k, features, hidden, experts, dtype=dtype, grad_dtype=torch.float32)
+        self.total, self.tokens = (ExpertCombine(n, k, features, dtype=dtype) for _ in range(2))
+        self.up.dW = torch.empty(experts, 2 * hidden, features, device="cuda")
+        self.down.dW = torch.empty(experts, features, hidden, device="cuda")
+        self.out = self.total.out
+
+    def forward(self, X, scores, bias, W_up, W_down):
+        self.route.route(scores, bias=bias)
+        self.order.sort(self.route.idx)
+        self.up.product(X, W_up, self.order.start, self.order.order, self.k)
+        self.down.product(self.up.Y, W_down, self.order.start)
+        self.total.combine(self.down.Y, self.order.place, self.route.weight)
+
+    def backward(self, X, scores, W_up, W_down, g_out):
+        start = self.order.start
+        self.total.grad(g_out, self.down.Y, self.order.place, self.route.weight)
+        self.down.weight_grad(self.total.dY, self.up.Y, start)
+        self.down.input_grad(self.total.dY, W_down, start, saved=self.up.saved)
+        self.up.weight_grad(self.down.dX, X, start, self.order.order, self.k)
+        self.up.input_grad(self.down.dX, W_up, start)
+        self.tokens.combine(self.up.dX, self.order.place)
+        self.grads = self.up.dW, self.down.dW, self.route.grad(scores, self.total.g_weight), self.tokens.out
+
+
+def train_experts(n=2048, features=64, hidden=48, experts=16, k=2, sweeps=6, steps=40, rate=4.0, max_norm=0.5, dtype=torch.bfloat16, seed=0):
+    """Returns the loss of each step, the gradients' norms before they were clipped, and the tokens of the most used expert over the mean at the end."""
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    X = torch.randn(n, features, generator=gen, device="cuda")
+    wanted = torch.tanh(X @ torch.randn(features, features, generator=gen, device="cuda") * features ** -0.5)
+    X = X.to(dtype)
+    W_up = torch.randn(experts, 2 * hidden, features, generator=gen, device="cuda") * features ** -0.5
+    W_down = torch.randn(experts, features, hidden, generator=gen, device="cuda") * hidden ** -0.5
+    R = torch.randn(features, experts, generator=gen, device="cuda") * features ** -0.5
+
+    layer = ExpertLayer(n, features, hidden, experts, k, dtype)
+    dR = torch.empty_like(R)
+    clip = GradClip([layer.up.dW, layer.down.dW, dR])
+    losses, norms = [], []
+    for _ in range(steps):
+        scores, up, down = X.float() @ R, W_up.to(dtype), W_down.to(dtype)
+        layer.forward(X, scores, column_duals(scores, 1.0, sweeps), up, down)
+        off = layer.out.float() - wanted
+        layer.backward(X, scores, up, down, (off / n).to(dtype))
+        torch.mm(X.float().t(), layer.grads[2], out=dR)
+        clip.clip(max_norm)
+        for W, g in ((W_up, layer.up.dW), (W_down, layer.down.dW), (R, dR)):
+            W -= rate * g
+        losses.append(0.5 * off.square().sum(1).mean())
+        norms.append(clip.norm_out.clone())
+    load = (layer.order.start[1:] - layer.order.start[:-1]).max() * experts / (n * k)
+    return dict(loss=torch.stack(losses).tolist(), norm=torch.cat(norms).tolist(), load=float(load))
+
+
 if __name__ == "__main__":
     s = train_student()
     print(f"student: loss {s['loss'][0]:.4f} -> {s['loss'][-1]:.4f}, entropy {s['entropy']:.3f}, log probability of the target {s['logprob']:.3f}; "
           f"most used column {100 * s['most_plain']:.2f} % of the rows, balanced {100 * s['most_balanced']:.2f} %")
     r = route_tokens()
     print(f"router: most used expert {r['load_plain']:.2f} times the mean, balanced {r['load_balanced']:.2f}")
+    e = train_experts()
+    print(f"experts: loss {e['loss'][0]:.3f} -> {e['loss'][-1]:.3f}, norm of the gradients {e['norm'][0]:.3f} -> {e['norm'][-1]:.3f}, most used expert {e['load']:.2f} times the mean")

@@ -27,6 +27,8 @@ using namespace regot;
 
 constexpr int64_t kMaxDim = 2147483647LL;
 constexpr int64_t kMaxGrid = 1 << 22;
+constexpr int64_t kMaxTiles = (1 << 23) - 1;     // workgroups of 512 threads: a launch has fewer than 2^32 threads
+constexpr int64_t kMaxNumbers = (int64_t)1 << 40;  // of a tensor
 constexpr size_t kAlign = 256;
 constexpr int kCUs = 256;
 
@@ -219,7 +221,7 @@ __global__ void __launch_bounds__(kThreads) expert_join_kernel(const JoinArgs A)
 
 // ---- the norm ----
 
-constexpr uint32_t kLeastEach = 8 * kThreads;  // numbers of a workgroup
+constexpr int64_t kLeastEach = 8 * kThreads;  // numbers of a workgroup
 constexpr int64_t kMostParts = 16384;  // (4096: 1.2 GB in 300 tensors 759 us in the place of 692, the ends of the launches are longer)
 constexpr uint32_t kFewParts = 2048;           // partial sums that each workgroup of the scaling adds up itself
 
@@ -228,7 +230,7 @@ int check_tensors(int64_t count, const regot_tensor *list, bool clip)
     if (count < 0 || count > kMaxDim) return REGOT_ERR_DIM;
     if (count > 0 && !list) return REGOT_ERR_NULL;
     for (int64_t t = 0; t < count; ++t) {
-        if (list[t].count < 0) return REGOT_ERR_DIM;
+        if (list[t].count < 0 || list[t].count > kMaxNumbers) return REGOT_ERR_DIM;
         if (bad_type(list[t].type)) return REGOT_ERR_ARG;
         if (list[t].count > 0 && (!list[t].data || (clip && !list[t].out))) return REGOT_ERR_NULL;
         if (misaligned(list[t].data, element_bytes(list[t].type)) || misaligned(list[t].out, element_bytes(list[t].type))) return REGOT_ERR_ALIGN;
@@ -238,8 +240,7 @@ int check_tensors(int64_t count, const regot_tensor *list, bool clip)
 
 // Numbers of a workgroup, and workgroups of all tensors: as many as a sum takes, whatever the tensors' sizes are
 struct ClipPlan {
-    uint32_t each = kLeastEach;
-    int64_t parts = 0;
+    int64_t each = kLeastEach, parts = 0;
 };
 
 ClipPlan plan_clip(int64_t count, const regot_tensor *list)
@@ -247,9 +248,7 @@ ClipPlan plan_clip(int64_t count, const regot_tensor *list)
     ClipPlan P;
     int64_t all = 0;
     for (int64_t t = 0; t < count; ++t) all += list[t].count / kLeastEach + 1;
-    uint32_t times = 1;
-    while (all / times > kMostParts) times *= 2;
-    P.each = kLeastEach * times;
+    while (all / (P.each / kLeastEach) > kMostParts && P.each < kMaxNumbers) P.each *= 2;
     for (int64_t t = 0; t < count; ++t) P.parts += (list[t].count + P.each - 1) / P.each;
     return P;
 }
@@ -403,11 +402,11 @@ int regot_expert_product(int64_t rows, int64_t m, int64_t d, int64_t experts, co
     P.kind = act == REGOT_ACT_NONE ? kPlain : act == REGOT_ACT_GATE ? kGate : kGateGrad;
     P.across = w_by == REGOT_W_INPUTS;
     P.out_type = type;
-    // (results are stored 8 neighbours at a time)
-    const bool direct = d > 0 && m % 8 == 0 && whole_chunks(X, d, ldX, b) && whole_chunks(W, w_cols, ldW, b) && strideW % (16 / b) == 0 &&
-                        whole_chunks(Y, m, ldY, b) && (!saved || whole_chunks(saved, m, ldSaved, b));
+    const bool direct = d > 0 && whole_chunks(X, d, ldX, b) && whole_chunks(W, w_cols, ldW, b) && strideW % (16 / b) == 0 && (!P.across || m % (16 / b) == 0);
+    // (a half's numbers end with a chunk too)
+    A.whole = whole_chunks(Y, m, ldY, b) && (!saved || whole_chunks(saved, m, ldSaved, b));
     P.units = (d * b + 128 * kFewWaves - 1) / (128 * kFewWaves);
-    if (direct && !P.across && P.kind != kGateGrad && rows <= kFewRows * experts && P.units <= kFewUnits) {
+    if (direct && A.whole && m % 8 == 0 && !P.across && P.kind != kGateGrad && rows <= kFewRows * experts && P.units <= kFewUnits) {
         P.tile = kTileFew;
         A.groups = (int)few_groups(std::min(rows, experts), (wide + 31) / 32);
     } else {
@@ -418,7 +417,7 @@ int regot_expert_product(int64_t rows, int64_t m, int64_t d, int64_t experts, co
     const int64_t cols = P.tile == kTileFew ? T.cols * A.groups : T.cols;
     A.single = rows < rows / T.rows + experts;
     const int64_t row_tiles = A.single ? rows : rows / T.rows + experts, col_tiles = (wide + cols - 1) / cols;
-    if (row_tiles * col_tiles > kMaxDim) return REGOT_ERR_DIM;
+    if (row_tiles * col_tiles > kMaxTiles) return REGOT_ERR_DIM;
     A.row_tiles = (uint32_t)row_tiles;
     A.col_tiles = (uint32_t)col_tiles;
     A.tiles = (uint32_t)(row_tiles * col_tiles);
@@ -468,7 +467,8 @@ int regot_expert_weight_grad(int64_t rows, int64_t m, int64_t d, int64_t experts
     A.ldY = parts ? d : ldW;
     A.strideY = parts ? m * d : strideW;
     const int pb = element_bytes(P.out_type);
-    const bool direct = whole_chunks(X, d, ldX, b) && whole_chunks(dY, m, ldY, b) && whole_chunks(A.Y, d, A.ldY, pb) && A.strideY % (16 / pb) == 0;
+    const bool direct = whole_chunks(X, d, ldX, b) && whole_chunks(dY, m, ldY, b);
+    A.whole = whole_chunks(A.Y, d, A.ldY, pb) && A.strideY % (16 / pb) == 0;
     P.tile = kTileDirectSmall;
     if (!parts) P.tile = choose_tile(type, direct, [&](TileShape T) { return (m + T.rows - 1) / T.rows * ((d + T.cols - 1) / T.cols) * experts; });
     else if (!direct) P.tile = kTileStagedSmall;
@@ -477,7 +477,7 @@ int regot_expert_weight_grad(int64_t rows, int64_t m, int64_t d, int64_t experts
         G.splits = 1;
     }
     const int64_t tiles = G.tiles(experts);
-    if (tiles > kMaxDim) return REGOT_ERR_DIM;
+    if (tiles > kMaxTiles) return REGOT_ERR_DIM;
     A.row_tiles = (uint32_t)G.tiles_m;
     A.col_tiles = (uint32_t)G.tiles_d;
     A.tiles = (uint32_t)tiles;

@@ -48,6 +48,7 @@ struct GroupArgs {
     uint32_t row_tiles, col_tiles, tiles;
     int splits;
     int groups;             // few rows: stretches of 32 rows of W that a workgroup has
+    bool whole;             // results' rows are whole chunks of 16 bytes, and begin at multiples of 16 bytes
     int single;             // tiles are numbered by their first row (fewer rows than experts)
 };
 

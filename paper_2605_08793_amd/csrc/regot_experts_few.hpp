@@ -89,7 +89,7 @@ __global__ void __launch_bounds__(kFewWaves *kLanes) expert_few_kernel(const Gro
         Raw part[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) part[e] = Score<TYPE>::put(v[e]);
-        store_run<TYPE, 4, true>(static_cast<char *>(to) + (r * ld + c) * kElem, part, 1);
+        store_run<TYPE, 4>(static_cast<char *>(to) + (r * ld + c) * kElem, part, 1, true);
     };
     int slot = 0, s = 0;
     for (int of = 0; of < groups; ++of) {

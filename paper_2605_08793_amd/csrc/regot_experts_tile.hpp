@@ -290,7 +290,7 @@ __device__ __forceinline__ void through_lds(char *mine, Value value, Take take)
         wave_lds();
         constexpr int kRowsAtOnce = kLanes / kChunks;
         const int row = lane / kChunks, chunk = lane % kChunks;
-#pragma unroll
+#pragma unroll 4
         for (int it = 0; it < min(kPass, ROWS - x0) * 16 / kRowsAtOnce; ++it) {
             const int at = it * kRowsAtOnce + row, of = at % 16;
             take(x0 + at / 16, of, chunk * 16 / kElem, *reinterpret_cast<const u32x4 *>(mine + at * kRow + (chunk ^ (of & (kChunks - 1))) * 16));
@@ -323,27 +323,32 @@ __device__ __forceinline__ void results(char *mine, Value value, Take take)
     }
 }
 
-// The first numbers of a chunk, or as many as a row of `left` more has (WHOLE: all or none)
-template <int TYPE, int COUNT, bool WHOLE>
-__device__ __forceinline__ void store_run(void *p, const typename Score<TYPE>::Raw *v, int64_t left)
+// The numbers of a chunk of which a row has `left` more, at any multiple of their element; whole: it has all or none, at a multiple of the chunk
+template <int TYPE, int COUNT>
+__device__ __forceinline__ void store_run(void *p, const typename Score<TYPE>::Raw *v, int64_t left, bool whole)
 {
     using Raw = typename Score<TYPE>::Raw;
-    if constexpr (WHOLE) {
+    if (whole) {
         if (left > 0) __builtin_memcpy(__builtin_assume_aligned(p, COUNT * sizeof(Raw)), v, COUNT * sizeof(Raw));
+    } else if (left >= COUNT) {
+        typedef uint32_t Any __attribute__((ext_vector_type(COUNT * sizeof(Raw) / 4), aligned(alignof(uint16_t))));
+        __builtin_memcpy(static_cast<Any *>(p), v, sizeof(Any));
     } else {
 #pragma unroll
-        for (int c = 0; c < COUNT; ++c)
+        for (int c = 0; c < COUNT - 1; ++c)
             if (c < left) static_cast<Raw *>(p)[c] = v[c];
     }
 }
 
-template <int TYPE, int COUNT, bool WHOLE>
-__device__ __forceinline__ void load_run(float *v, const void *p, int64_t left)
+template <int TYPE, int COUNT>
+__device__ __forceinline__ void load_run(float *v, const void *p, int64_t left, bool whole)
 {
     using Raw = typename Score<TYPE>::Raw;
     Raw part[COUNT];
-    if constexpr (WHOLE) {
+    if (whole) {
         __builtin_memcpy(part, __builtin_assume_aligned(p, COUNT * sizeof(Raw)), COUNT * sizeof(Raw));
+    } else if (left >= COUNT) {
+        __builtin_memcpy(part, p, COUNT * sizeof(Raw));
     } else {
 #pragma unroll
         for (int c = 0; c < COUNT; ++c) part[c] = c < left ? static_cast<const Raw *>(p)[c] : Raw(0.f);
@@ -631,11 +636,11 @@ __device__ __forceinline__ void expert_tile(const GroupArgs &A, const Run &run, 
         static_assert(KIND != kGate || kHalf % 2 == 0, "halves are pairs of fragments");
         constexpr int kUp = ACROSS ? kHalf : kHalf / 2;  // runs of g
         const auto store = [&](char *to, int64_t ld) {
-            return [=](int x, int i, int c, u32x4 v) {
+            return [=, &A](int x, int i, int c, u32x4 v) {
                 const int64_t r = row_of(x, i), col = first_col + wn * kHalf * 16 + c;
                 Raw part[16 / kElem];
                 __builtin_memcpy(part, &v, 16);
-                if (r < row_end) store_run<TYPE, 16 / kElem, DIRECT>(to + (r * ld + col) * kElem, part, col_end - col);
+                if (r < row_end) store_run<TYPE, 16 / kElem>(to + (r * ld + col) * kElem, part, col_end - col, A.whole);
             };
         };
         results<TYPE, kFragRows, kHalf, ACROSS, kMine>(mine, [&](int x, int y, int e) {
@@ -653,8 +658,8 @@ __device__ __forceinline__ void expert_tile(const GroupArgs &A, const Run &run, 
             if (r >= row_end || left <= 0) return;
             const char *s = static_cast<const char *>(A.saved) + (r * A.ldSaved + col) * kElem;
             float gate[4], up[4];
-            load_run<TYPE, 4, DIRECT>(gate, s, left);
-            load_run<TYPE, 4, DIRECT>(up, s + col_end * kElem, left);
+            load_run<TYPE, 4>(gate, s, left, A.whole);
+            load_run<TYPE, 4>(up, s + col_end * kElem, left, A.whole);
             Raw dg[4], du[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -663,8 +668,8 @@ __device__ __forceinline__ void expert_tile(const GroupArgs &A, const Run &run, 
                 du[e] = Score<TYPE>::put(D * (gate[e] * p));
             }
             char *to = static_cast<char *>(A.Y) + (r * A.ldY + col) * kElem;
-            store_run<TYPE, 4, DIRECT>(to, dg, left);
-            store_run<TYPE, 4, DIRECT>(to + col_end * kElem, du, left);
+            store_run<TYPE, 4>(to, dg, left, A.whole);
+            store_run<TYPE, 4>(to + col_end * kElem, du, left, A.whole);
         });
     } else {
         char *Y = static_cast<char *>(A.Y);
@@ -673,7 +678,7 @@ __device__ __forceinline__ void expert_tile(const GroupArgs &A, const Run &run, 
             const int64_t r = row_of(x, i), col = first_col + wn * kFragCols * 16 + c;
             typename Score<OUT>::Raw of[16 / kOutElem];
             __builtin_memcpy(of, &v, 16);
-            if (r < row_end) store_run<OUT, 16 / kOutElem, DIRECT>(Y + (r * A.ldY + col) * kOutElem, of, col_end - col);
+            if (r < row_end) store_run<OUT, 16 / kOutElem>(Y + (r * A.ldY + col) * kOutElem, of, col_end - col, A.whole);
         });
     }
 }

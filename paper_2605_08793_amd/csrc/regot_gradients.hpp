@@ -26,7 +26,7 @@ struct ClipArgs {
     uint32_t blocks;     // of this launch
     uint32_t part;       // this launch's first partial sum
     uint32_t parts;      // partial sums of all launches
-    uint32_t each;       // numbers of a workgroup, a multiple of 8 kThreads
+    int64_t each;        // numbers of a workgroup, a multiple of 8 kThreads
     double max_norm;
     double *sums;        // [parts]
     float *norm, *factor;
@@ -88,7 +88,7 @@ __device__ __forceinline__ double block_total(double v)
 __global__ void __launch_bounds__(kThreads) grad_norm_kernel(const ClipArgs A)
 {
     const ListedTensor &T = A.list[listed(A, blockIdx.x)];
-    const int64_t from = (int64_t)(blockIdx.x - T.first) * A.each, to = min(from + (int64_t)A.each, T.count);
+    const int64_t from = (blockIdx.x - T.first) * A.each, to = min(from + A.each, T.count);
     double v;
     if (T.type == REGOT_F32) v = sum_of_squares<REGOT_F32>(T, from, to);
     else if (T.type == REGOT_BF16) v = sum_of_squares<REGOT_BF16>(T, from, to);
@@ -151,7 +151,7 @@ __global__ void __launch_bounds__(kThreads) grad_scale_kernel(const ClipArgs A)
     const float factor = SUMS ? clip_factor(A, A.part + b == 0) : A.factor[0];
     const ListedTensor &T = A.list[listed(A, b)];
     if (factor == 1.f && T.data == T.out) return;
-    const int64_t from = (int64_t)(b - T.first) * A.each, to = min(from + (int64_t)A.each, T.count);
+    const int64_t from = (b - T.first) * A.each, to = min(from + A.each, T.count);
     if (T.type == REGOT_F32) scale<REGOT_F32>(T, from, to, factor);
     else if (T.type == REGOT_BF16) scale<REGOT_BF16>(T, from, to, factor);
     else scale<REGOT_F16>(T, from, to, factor);

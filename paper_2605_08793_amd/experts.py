@@ -91,7 +91,7 @@ class ExpertProduct(_Buffers):
         self.wide = 2 * self.m if gated else self.m
         self._Y = self._buffer(self.rows, self.m, dtype=dtype)
         self._saved = self._buffer(self.rows, 2 * self.m, dtype=dtype) if keep and gated else None
-        self._work = None
+        self._work = self._workspace(B.regot_expert_weight_grad_workspace_bytes(self.rows, self.wide, self.d, self.experts))
         self.dX = self.dW = None
 
     def _run(self, X, x_rows, d, W, by, start, order, k, act, m, Y, saved, ldS):
@@ -142,8 +142,6 @@ class ExpertProduct(_Buffers):
         _, _, _, by, ldW, stride, to = B._weights(dW, "dW")
         if by != 0 and dW.numel():
             raise TypeError("dW must have rows of neighbours")
-        if self._work is None:
-            self._work = self._workspace(B.regot_expert_weight_grad_workspace_bytes(self.rows, self.wide, self.d, self.experts))
         B._check(B.load().regot_expert_weight_grad(
             self.rows, self.wide, self.d, self.experts, self._list(start, self.experts + 1, 1, "start", torch.int64), g_at, B.SCORE_TYPES[self.dtype], ldY,
             at, ldX, X.shape[0], self._list(order, self.rows, 1, "order", torch.int32, optional=True), int(k), to, B.SCORE_TYPES[self.grad_dtype], ldW,

@@ -119,6 +119,25 @@ def test_clip_refusals():
     assert B.load().regot_grad_norm(1, listed(tensor()), None, WS, BIG, None) == NULL
 
 
+def test_tensors_of_any_count():
+    """Asked for on the host: many tensors, the largest, more than any memory has."""
+    out = ctypes.c_size_t()
+    size = lambda *counts: (B.load().regot_grad_norm_workspace_bytes(len(counts), listed(*[tensor(count=c) for c in counts]), ctypes.byref(out)), out.value)  # noqa: E731
+    assert size() == (0, 256) and size(0) == (0, 256) and size(1, 1) == (0, 256)
+    assert size(*[1] * 20000) == (0, 160000)
+    status, most = size(*[1 << 40] * 40)
+    assert status == 0 and most <= 8 * (16384 + 2 * 40) + 256
+    for count in ((1 << 40) + 1, (1 << 62), (1 << 63) - 1):
+        assert size(3, count)[0] == DIM
+
+
+def test_more_tiles_than_a_launch_has():
+    wide = dict(rows=1 << 20, m=1 << 30, d=8, experts=1, ldX=8, x_rows=1 << 20, order=None, ldY=1 << 30, ldW=8, strideW=0, saved=None, Y=ctypes.c_void_p(1 << 50))
+    assert call("regot_expert_product", **wide) == DIM
+    wide = dict(rows=8, m=1 << 30, d=1 << 30, experts=1, ldY=1 << 30, ldX=1 << 30, ldW=1 << 30, strideW=0, X=ctypes.c_void_p(1 << 52), dW=ctypes.c_void_p(1 << 54))
+    assert call("regot_expert_weight_grad", **wide) == DIM
+
+
 def test_the_binding_checks_weights():
     assert B._weights(fake(3, 4, 5))[:6] == (3, 4, 5, 0, 5, 20)
     assert B._weights(fake(3, 5, 4).transpose(1, 2))[:6] == (3, 4, 5, 1, 4, 20)

@@ -1,0 +1,263 @@
+"""The experts' operators as they are used: a whole layer and its way back, in a captured step, on another stream, at sizes beyond 32-bit offsets, and the
+example that trains such a layer."""
+import numpy as np
+import pytest
+import torch
+
+import experts_reference as ref
+from paper_2605_08793_amd import balanced
+from paper_2605_08793_amd import binding as B
+from paper_2605_08793_amd.experts import ExpertCombine, ExpertOrder, ExpertProduct, GradClip
+from rows_reference import U
+
+pytestmark = pytest.mark.gpu
+
+
+def test_example_runs():
+    e = balanced.train_experts()
+    assert np.isfinite(e["loss"]).all() and np.isfinite(e["norm"]).all() and min(e["norm"]) > 0
+    assert 1.0 <= e["load"] < 2.0
+
+
+def layer_in_64_bits(X, scores, bias, W_up, W_down, g_out, k):
+    """(out, gradients of W_up, W_down, scores, X) of a gated layer by automatic differentiation."""
+    X, scores, W_up, W_down = (t.detach().cpu().double().requires_grad_(True) for t in (X, scores, W_up, W_down))
+    idx = (scores + bias.cpu()).detach().float().sort(dim=1, descending=True, stable=True).indices[:, :k]
+    s = torch.softmax(scores, 1).gather(1, idx)
+    weight = s / s.sum(1, keepdim=True)
+    out = torch.zeros(X.shape[0], W_down.shape[1], dtype=torch.float64)
+    hidden = W_down.shape[2]
+    for l in range(k):
+        z = torch.bmm(W_up[idx[:, l]], X[:, :, None])[:, :, 0]
+        h = torch.nn.functional.silu(z[:, :hidden]) * z[:, hidden:]
+        out = out + weight[:, l, None] * torch.bmm(W_down[idx[:, l]], h[:, :, None])[:, :, 0]
+    return out.detach(), *torch.autograd.grad((out * g_out.cpu().double()).sum(), (W_up, W_down, scores, X))
+
+
+@pytest.mark.parametrize("n,features,hidden,experts,k", [(70, 40, 24, 6, 2), (150, 33, 47, 9, 3), (1, 64, 64, 16, 4)])
+def test_a_layer_and_its_way_back(n, features, hidden, experts, k):
+    """fp32.  Each of at most six sums one behind the other is off by 2 U (c + 16) of the sum of its terms' sizes, which is at most about sqrt(c) times
+    the sum's own size for terms of random signs; c < 250."""
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    normal = lambda *shape: torch.randn(*shape, generator=gen, device="cuda")  # noqa: E731
+    X, scores, bias, g_out = normal(n, features), normal(n, experts), 0.3 * normal(experts), normal(n, features)
+    W_up, W_down = normal(experts, 2 * hidden, features) * features ** -0.5, normal(experts, features, hidden) * hidden ** -0.5
+    layer = balanced.ExpertLayer(n, features, hidden, experts, k, torch.float32)
+    layer.forward(X, scores, bias, W_up, W_down)
+    layer.backward(X, scores, W_up, W_down, g_out)
+    for got, want, what in zip((layer.out, *layer.grads), layer_in_64_bits(X, scores, bias, W_up, W_down, g_out, k), ("out", "W_up", "W_down", "scores", "X")):
+        off = float((got.cpu().double() - want).norm() / want.norm())
+        assert off < 6 * 2 * U * (250 + 16) * 250 ** 0.5, (what, off)
+
+
+def test_captured_steps_replay_like_eager():
+    """Other tokens, another routing at each replay; two graphs of one object's buffers, eager work between."""
+    n, features, hidden, experts, k = 600, 72, 40, 12, 3
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    X, g_out = (torch.empty(n, features, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    scores, bias = torch.empty(n, experts, device="cuda"), torch.zeros(experts, device="cuda")
+    W_up = (torch.randn(experts, 2 * hidden, features, generator=gen, device="cuda") * features ** -0.5).bfloat16()
+    W_down = (torch.randn(experts, features, hidden, generator=gen, device="cuda") * hidden ** -0.5).bfloat16()
+    layer = balanced.ExpertLayer(n, features, hidden, experts, k)
+    copies = [torch.empty_like(t) for t in (layer.up.dW, layer.down.dW)]
+    clip = GradClip([layer.up.dW, layer.down.dW], out=copies)
+
+    def fill():
+        X.normal_(generator=gen)
+        g_out.normal_(generator=gen)
+        scores.normal_(generator=gen)
+
+    def forward():
+        layer.forward(X, scores, bias, W_up, W_down)
+
+    def backward():
+        layer.backward(X, scores, W_up, W_down, g_out)
+        clip.clip(1.0)
+
+    outputs = lambda: [layer.order.start, layer.order.order, layer.order.place, layer.up.Y, layer.up.saved, layer.out, layer.total.g_weight, *layer.grads,  # noqa: E731
+                       clip.norm_out, clip.factor, *copies]
+    fill()
+    forward()
+    backward()
+    torch.cuda.synchronize()
+    graphs = []
+    for f in (forward, backward):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            f()
+    for replay in range(4):
+        fill()
+        forward()
+        backward()
+        torch.cuda.synchronize()
+        eager = [t.clone() for t in outputs()]
+        for t in outputs():
+            t.fill_(3)
+        torch.cuda.synchronize()
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for i, (a, b) in enumerate(zip(eager, outputs())):
+            assert torch.equal(a, b), (replay, i)
+
+
+def test_on_a_stream_of_its_own():
+    gen = torch.Generator().manual_seed(4)
+    idx = ref.choices(300, 2, 7, gen).cuda()
+    X, W = torch.randn(300, 64, generator=gen).cuda(), torch.randn(7, 32, 64, generator=gen).cuda()
+    here, there = (ExpertOrder(300, 2, 7) for _ in range(2))
+    a, b = (ExpertProduct(600, 32, 64, 7, dtype=torch.float32) for _ in range(2))
+    here.sort(idx)
+    a.product(X, W, here.start, here.order, 2)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        there.sort(idx)
+        b.product(X, W, there.start, there.order, 2)
+    torch.cuda.current_stream().wait_stream(side)
+    live = int(here.start[-1])
+    assert torch.equal(here.order, there.order) and torch.equal(a.Y[:live], b.Y[:live])
+
+
+def test_an_expert_chosen_twice():
+    """A token that has an expert twice has two rows of it, and gets both; its gradient is the sum."""
+    idx = torch.tensor([[1, 1], [0, 1]], dtype=torch.int32, device="cuda")
+    order = ExpertOrder(2, 2, 2)
+    order.sort(idx)
+    assert order.start.tolist() == [0, 1, 4] and order.place.tolist() == [[1, 2], [0, 3]]
+    X, W = torch.tensor([[1.0], [10.0]], device="cuda"), torch.tensor([[[2.0]], [[3.0]]], device="cuda")
+    op, total = ExpertProduct(4, 1, 1, 2, dtype=torch.float32), ExpertCombine(2, 2, 1, dtype=torch.float32)
+    op.product(X, W, order.start, order.order, 2)
+    total.combine(op.Y, order.place, torch.tensor([[0.5, 0.25], [1.0, 1.0]], device="cuda"))
+    assert total.out[:, 0].tolist() == [0.75 * 3.0, 20.0 + 30.0]
+    op.weight_grad(torch.ones(4, 1, device="cuda"), X, order.start, order.order, 2)
+    assert op.dW[:, 0, 0].tolist() == [10.0, 12.0]
+
+
+def test_rows_beyond_32_bit_offsets():
+    """2.4 billion numbers in rows that are read, gathered, written and added up; rows at both ends looked at."""
+    n, d, m, experts = 300_000, 8192, 64, 4
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    X = torch.empty(n, d, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    W = torch.empty(experts, m, d, dtype=torch.bfloat16, device="cuda").normal_(0, d ** -0.5, generator=gen)
+    idx = (torch.arange(n, device="cuda", dtype=torch.int32)[:, None] * 7) % experts
+    order = ExpertOrder(n, 1, experts)
+    order.sort(idx)
+    op = ExpertProduct(n, m, d, experts)
+    op.product(X, W, order.start, order.order, 1)
+    look = torch.cat([torch.arange(200, device="cuda"), torch.arange(n - 200, n, device="cuda")])
+
+    def check(got, rows, weights, what, length):
+        want = torch.bmm(weights.double(), rows.double()[:, :, None])[:, :, 0]
+        tol = torch.bmm(weights.double().abs(), rows.double().abs()[:, :, None])[:, :, 0] * 2 * U * (length + 16)
+        ref.close(got, want.cpu(), ref.rounded(want, tol, torch.bfloat16).cpu(), what)
+
+    expert = torch.searchsorted(order.start[1:], look, right=True)
+    check(op.Y[look], X[order.order[look].long()], W[expert], "Y", d)
+    dX = op.input_grad(op.Y, W, order.start)       # n x d
+    check(dX[look], op.Y[look], W[expert].transpose(1, 2).contiguous(), "dX", m)
+    total = ExpertCombine(n, 1, d)
+    total.combine(dX, order.place)
+    assert torch.equal(total.out[look], dX[order.place[look, 0].long()])
+    total.grad(X, dX, order.place)
+    assert torch.equal(total.dY[look], X[order.order[look].long()])
+    g = torch.zeros(n, m, dtype=torch.bfloat16, device="cuda")
+    g[look] = 1.0
+    op.weight_grad(g, X, order.start, order.order, 1)
+    rows = X[order.order[look].long()].double()
+    for e in range(experts):
+        want, size = rows[expert == e].sum(0), rows[expert == e].abs().sum(0)
+        ref.close(op.dW[e, 5], want.cpu(), ref.rounded(want, size * 2 * U * (n / experts + 16), torch.bfloat16).cpu(), f"dW {e}")
+
+
+def test_weights_beyond_32_bit_offsets():
+    """70 experts of 8192 x 8192: 4.7 billion numbers; few rows, and as many as tiles take."""
+    experts, m, d = 70, 8192, 8192
+    W = torch.empty(experts, m, d, dtype=torch.bfloat16, device="cuda")
+    for e in (0, 69):
+        W[e].normal_(0, d ** -0.5)
+    for rows in (40, 1400):
+        X = torch.randn(rows, d, device="cuda").bfloat16()
+        start = torch.full((experts + 1,), rows // 2, dtype=torch.int64, device="cuda")
+        start[0], start[-1] = 0, rows
+        op = ExpertProduct(rows, m, d, experts)
+        op.product(X, W, start)
+        for r, e in ((0, 0), (rows - 1, 69)):
+            want, tol = W[e].double() @ X[r].double(), W[e].double().abs() @ X[r].double().abs() * 2 * U * (d + 16)
+            ref.close(op.Y[r], want.cpu(), ref.rounded(want, tol, torch.bfloat16).cpu(), f"row {r}")
+        op.input_grad(X, W, start)
+        want, tol = W[69].double().t() @ X[-1].double(), W[69].double().abs().t() @ X[-1].double().abs() * 2 * U * (m + 16)
+        ref.close(op.dX[-1], want.cpu(), ref.rounded(want, tol, torch.bfloat16).cpu(), "dX")
+
+
+@pytest.mark.parametrize("d,m", [(64, 64), (33, 17)])
+def test_32_bit_numbers_that_pieces_do_not_hold(d, m):
+    """The largest finite numbers (whose first piece rounds to infinity), infinities and NaNs among ordinary rows: results are those of the numbers as they are, and
+    the ordinary rows' are the ones they have alone."""
+    gen = torch.Generator().manual_seed(d)
+    X, W = torch.randn(200, d, generator=gen), torch.randn(1, m, d, generator=gen)
+    start = torch.tensor([0, 200], device="cuda")
+    op = ExpertProduct(200, m, d, 1, dtype=torch.float32)
+    op.product(X.cuda(), W.cuda(), start)
+    clean = op.Y.clone()
+    odd = torch.zeros(5, d)
+    odd[0, 0], odd[1, :2], odd[2, 0], odd[3, 0] = -torch.finfo(torch.float32).max, torch.tensor([3.4e38, 3.4e38]), float("inf"), float("nan")
+    odd[4, 0] = 3.4e38
+    Y = X.clone()
+    Y[50:55] = odd
+    V = W.clone()
+    V[0, 0, 0], V[0, 1, 0], V[0, 2, 0] = 1e-20, 0.0, -2.0
+    op.product(Y.cuda(), V.cuda(), start)
+    got = op.Y.cpu()
+    assert torch.equal(got[:50, 3:], clean.cpu()[:50, 3:]) and torch.equal(got[55:, 3:], clean.cpu()[55:, 3:])
+    want = odd.double() @ V[0].double().t()
+    want = torch.where(want.abs() > torch.finfo(torch.float32).max, want.sign() * float("inf"), want)
+    # (row 1 adds up two products: where one of them is beyond 32 bits and the other has another sign, 32-bit arithmetic has the sum where it comes fused and last,
+    # and otherwise an infinity or a NaN, by their order)
+    a, b = odd[1, 0].double() * V[0, :, 0].double(), odd[1, 1].double() * V[0, :, 1].double()
+    open_ = (a * b < 0) & (torch.maximum(a.abs(), b.abs()) > torch.finfo(torch.float32).max)
+    open_ &= ~got[51].isfinite()
+    want[1, open_] = got[51, open_].double()
+    ref.close(got[50:55], want, want.abs().nan_to_num(posinf=0.0) * 2 * U * (d + 16), "odd rows")
+
+
+def test_wrong_sizes_are_refused():
+    start = torch.zeros(4, dtype=torch.int64, device="cuda")
+    op = ExpertProduct(8, 16, 24, 3, dtype=torch.float32)
+    X, W, dY = torch.zeros(8, 24, device="cuda"), torch.zeros(3, 16, 24, device="cuda"), torch.zeros(8, 16, device="cuda")
+    for bad in ((X[:, :23], W, start), (X.double(), W, start), (X.cpu(), W, start), (X, W[:2], start), (X, W.half(), start), (X, W[:, :, ::2], start), (X, W, start[:3]),
+                (X, W, start.int()), (X, W, start.cpu()), (X, W, start, torch.zeros(7, dtype=torch.int32, device="cuda")), (X, W, start, torch.zeros(8, device="cuda"))):
+        with pytest.raises(TypeError):
+            op.product(*bad)
+    with pytest.raises(B.RegotError):
+        op.product(X[:7], W, start)      # (row 7 has no row of X)
+    with pytest.raises(B.RegotError):
+        op.product(X, W, start, torch.zeros(8, dtype=torch.int32, device="cuda"), 0)
+    for bad in ((dY[:7], W, start), (dY[:, :15], W, start), (dY, W, start, torch.zeros(8, 47, device="cuda"))):
+        with pytest.raises(TypeError):
+            op.input_grad(*bad)
+    op.dW = torch.zeros(3, 24, 16, device="cuda").transpose(1, 2)
+    with pytest.raises(TypeError):
+        op.weight_grad(dY, X, start)
+    with pytest.raises(TypeError):
+        ExpertOrder(4, 2, 3).sort(torch.zeros(4, 2, dtype=torch.int64, device="cuda"))
+    total = ExpertCombine(4, 2, 16, dtype=torch.float32)
+    place = torch.zeros(4, 2, dtype=torch.int32, device="cuda")
+    for bad in ((dY[:7], place), (dY, place[:3]), (dY, place.long()), (dY, place, torch.zeros(4, 3, device="cuda"))):
+        with pytest.raises(TypeError):
+            total.combine(*bad)
+
+
+def test_memory_that_is_shared_is_refused():
+    start = torch.tensor([0, 4], device="cuda")
+    wide = torch.zeros(4, 64, device="cuda")
+    W = torch.zeros(1, 16, 16, device="cuda")
+    for X, Y in ((wide[:, :16], wide[:, 8:24]), (wide[:, 48:], wide[:, 48:])):
+        with pytest.raises(B.RegotError):
+            B.regot_expert_product(X, W, start, Y)
+    B.regot_expert_product(wide[:, :16], W, start, wide[:, 16:32])       # (rows of one between those of the other)
+    with pytest.raises(B.RegotError):
+        B.regot_expert_product(wide[:, :16], W, start, W[0, :4])
+    place = torch.zeros(2, 2, dtype=torch.int32, device="cuda")
+    with pytest.raises(B.RegotError):
+        B.regot_expert_combine(wide[:, :16], place, None, wide[:2, :16])
