@@ -261,10 +261,11 @@ __device__ __forceinline__ void multiplied(f32x4 (&c)[COUNT])
 
 // A wave's results, ROWS x COLS fragments, through its own part of LDS, so that they go to memory as whole rows and not as the pieces of 8 or
 // 16 bytes that a lane has (131072 x 1024 by 64 x 2048 x 1024, bf16: 693 us without, see the table at the kernel).  value(x, y, e): result e of run y (of 8
-// neighbours, or 4 where ACROSS) in fragment row x; take(x, i, c, v): 16 bytes of numbers of type TYPE, row i of fragment row x, from column c on.
+// neighbours, or 4 where ACROSS) in fragment row x; take(x, i, c, v, asked): 16 bytes of numbers of type TYPE, row i of fragment row x, from column c on, with
+// what ask(x, i, c) gave, which is asked for eight times before the first is taken.
 // Chunks of 16 bytes lie in an order that depends on their row, as in Side.
-template <int TYPE, int ROWS, int COLS, bool ACROSS, int BYTES, typename Value, typename Take>
-__device__ __forceinline__ void through_lds(char *mine, Value value, Take take)
+template <int TYPE, int ROWS, int COLS, bool ACROSS, int BYTES, typename Value, typename Ask, typename Take>
+__device__ __forceinline__ void through_lds(char *mine, Value value, Ask ask, Take take)
 {
     using Raw = typename Score<TYPE>::Raw;
     constexpr int kElem = sizeof(Raw), kRun = ACROSS ? 4 : 8, kRow = COLS * 16 * kElem, kChunks = kRow / 16, kPiece = kRun * kElem < 16 ? kRun * kElem : 16;
@@ -288,12 +289,23 @@ __device__ __forceinline__ void through_lds(char *mine, Value value, Take take)
                 }
             }
         wave_lds();
-        constexpr int kRowsAtOnce = kLanes / kChunks;
+        constexpr int kRowsAtOnce = kLanes / kChunks, kAsked = 8;
         const int row = lane / kChunks, chunk = lane % kChunks;
-#pragma unroll 4
-        for (int it = 0; it < min(kPass, ROWS - x0) * 16 / kRowsAtOnce; ++it) {
-            const int at = it * kRowsAtOnce + row, of = at % 16;
-            take(x0 + at / 16, of, chunk * 16 / kElem, *reinterpret_cast<const u32x4 *>(mine + at * kRow + (chunk ^ (of & (kChunks - 1))) * 16));
+        const int all = min(kPass, ROWS - x0) * 16 / kRowsAtOnce;
+#pragma unroll 1
+        for (int it0 = 0; it0 < all; it0 += kAsked) {
+            decltype(ask(0, 0, 0)) asked[kAsked];
+#pragma unroll
+            for (int j = 0; j < kAsked; ++j) {
+                const int at = min(it0 + j, all - 1) * kRowsAtOnce + row;
+                asked[j] = ask(x0 + at / 16, at % 16, chunk * 16 / kElem);
+            }
+#pragma unroll
+            for (int j = 0; j < kAsked; ++j) {
+                const int at = (it0 + j) * kRowsAtOnce + row, of = at % 16;
+                if (it0 + j >= all) break;
+                take(x0 + at / 16, of, chunk * 16 / kElem, *reinterpret_cast<const u32x4 *>(mine + at * kRow + (chunk ^ (of & (kChunks - 1))) * 16), asked[j]);
+            }
         }
         wave_lds();
     }
@@ -305,7 +317,7 @@ __device__ __forceinline__ void results(char *mine, Value value, Take take)
 {
     using Raw = typename Score<TYPE>::Raw;
     if constexpr (ACROSS) {
-        through_lds<TYPE, ROWS, COLS, ACROSS, BYTES>(mine, value, take);
+        through_lds<TYPE, ROWS, COLS, ACROSS, BYTES>(mine, value, [](int, int, int) { return 0; }, [&](int x, int i, int c, u32x4 v, int) { take(x, i, c, v); });
     } else {
         constexpr int kChunk = 16 / sizeof(Raw);
         const int lane = threadIdx.x % kLanes, g = lane / 16, i = lane % 16;
@@ -653,24 +665,43 @@ __device__ __forceinline__ void expert_tile(const GroupArgs &A, const Run &run, 
                                                                store(static_cast<char *>(A.saved) + col_end * kElem, A.ldSaved));
         }
     } else if constexpr (KIND == kGateGrad) {
-        through_lds<REGOT_F32, kFragRows, kFragCols, ACROSS, kMine>(mine, result, [&](int x, int i, int c, u32x4 v) {
-            const int64_t r = row_of(x, i), col = first_col + wn * kFragCols * 16 + c, left = col_end - col;
+        struct Gate {
+            float g[4], u[4];
+        };
+        const auto saved_at = [&](int64_t r, int64_t col) { return static_cast<const char *>(A.saved) + (r * A.ldSaved + col) * kElem; };
+        const auto column = [&](int c) { return first_col + wn * kFragCols * 16 + c; };
+        const auto take = [&](int x, int i, int c, u32x4 v, const Gate &of) {
+            const int64_t r = row_of(x, i), col = column(c), left = col_end - col;
             if (r >= row_end || left <= 0) return;
-            const char *s = static_cast<const char *>(A.saved) + (r * A.ldSaved + col) * kElem;
-            float gate[4], up[4];
-            load_run<TYPE, 4>(gate, s, left, A.whole);
-            load_run<TYPE, 4>(up, s + col_end * kElem, left, A.whole);
             Raw dg[4], du[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float p = sigmoid(gate[e]), D = __uint_as_float(v[e]);
-                dg[e] = Score<TYPE>::put(D * up[e] * (p * (1.0f + gate[e] * (1.0f - p))));
-                du[e] = Score<TYPE>::put(D * (gate[e] * p));
+                const float p = sigmoid(of.g[e]), D = __uint_as_float(v[e]);
+                dg[e] = Score<TYPE>::put(D * of.u[e] * (p * (1.0f + of.g[e] * (1.0f - p))));
+                du[e] = Score<TYPE>::put(D * (of.g[e] * p));
             }
             char *to = static_cast<char *>(A.Y) + (r * A.ldY + col) * kElem;
             store_run<TYPE, 4>(to, dg, left, A.whole);
             store_run<TYPE, 4>(to + col_end * kElem, du, left, A.whole);
-        });
+        };
+        if (A.whole) {  // (the place of what is beyond the matrix is one inside, so that nothing stands between the loads)
+            through_lds<REGOT_F32, kFragRows, kFragCols, ACROSS, kMine>(mine, result, [&](int x, int i, int c) {
+                const char *s = saved_at(min(row_of(x, i), row_end - 1), min(column(c), col_end - 4));
+                Gate of;
+                load_run<TYPE, 4>(of.g, s, 4, true);
+                load_run<TYPE, 4>(of.u, s + col_end * kElem, 4, true);
+                return of;
+            }, take);
+        } else {
+            through_lds<REGOT_F32, kFragRows, kFragCols, ACROSS, kMine>(mine, result, [](int, int, int) { return 0; }, [&](int x, int i, int c, u32x4 v, int) {
+                const int64_t r = row_of(x, i), col = column(c), left = col_end - col;
+                if (r >= row_end || left <= 0) return;
+                Gate of;
+                load_run<TYPE, 4>(of.g, saved_at(r, col), left, false);
+                load_run<TYPE, 4>(of.u, saved_at(r, col + col_end), left, false);
+                take(x, i, c, v, of);
+            });
+        }
     } else {
         char *Y = static_cast<char *>(A.Y);
         if constexpr (KIND == kWeightGrad) Y += ((int64_t)part * A.experts + expert) * A.strideY * kOutElem;
