@@ -12,6 +12,8 @@ constexpr int kFewUnits = 16;                // units of a sum that a wave can h
 // reading of the weights, once each, so everything is for keeping loads under way: each wave has its share of the sum, a unit of 128 bytes of each row at a time (so that
 // a workgroup reads 1 KB of each of 32 rows), which it loads into its own part of LDS, four units ahead and across the ends of sums, without
 // registers and without waiting for another wave.  The rows' numbers stay in registers.  The waves' sums are added up in their order, by each wave in turn.
+// Measured: 64 tokens x 4 of 60 experts, 1400 x 2048 fp16 69 us = 5.0 TB/s; one token, 8 of 256, 2048 by 2 x 1024 bf16 14 us = 4.8 TB/s.  (Loads alone in the same order reach 5.4 TB/s
+// on rows of 2800 bytes and 6.0 on rows of whole lines; a workgroup's begin, until its first numbers are there, is what is missing.)
 template <int TYPE, bool GATE, int MOST>
 __global__ void __launch_bounds__(kFewWaves *kLanes) expert_few_kernel(const GroupArgs A)
 {

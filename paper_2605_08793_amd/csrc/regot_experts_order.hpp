@@ -46,7 +46,8 @@ __global__ void __launch_bounds__(kOrderThreads) expert_count_kernel(const Order
 
 // Each workgroup puts its choices where they belong: behind those of the experts before, of the same expert in the workgroups before, and in the waves
 // before; within a wave, 64 choices at a time, behind the equal ones in lower lanes (a ballot for each bit of the expert's number).  The counts
-// are sums of integers: nothing depends on the order of the additions.
+// are sums of integers: nothing depends on the order of the additions.  A chain of short steps is what bounds it: 524288 choices of 256 experts 13 us behind the counting's 3,
+// 32768 of 60 6.6 behind 2.4.
 __global__ void __launch_bounds__(kOrderThreads) expert_order_kernel(const OrderArgs A)
 {
     __shared__ uint32_t next[kOrderWaves * (REGOT_ROW_MAX_EXPERTS + 1)];  // [kOrderWaves][experts + 1]: where the next choice of an expert goes
@@ -189,7 +190,7 @@ struct Stretch {
     }
 };
 
-// A wave: 64 x 16 bytes of one token's sum.  The rows are asked for four at a time.
+// A wave: 64 x 16 bytes of one token's sum.  The rows are asked for four at a time.  Memory bounds it: 65536 tokens x 8 rows of 2048 bf16 423 us = 5.7 TB/s.
 template <int TYPE>
 __global__ void __launch_bounds__(kThreads) expert_combine_kernel(const CombineArgs A)
 {
@@ -223,7 +224,8 @@ __global__ void __launch_bounds__(kThreads) expert_combine_kernel(const CombineA
     }
 }
 
-// A wave: one choice.  dY = weight times the token's gradient, and the weight's gradient, the product of the two rows.
+// A wave: one choice.  dY = weight times the token's gradient, and the weight's gradient, the product of the two rows.  The token's row comes from the caches but for
+// once: 65536 tokens x 8 rows of 2048 bf16 845 us = 5.4 TB/s of reads and writes.
 template <int TYPE>
 __global__ void __launch_bounds__(kThreads) expert_combine_grad_kernel(const CombineArgs A)
 {

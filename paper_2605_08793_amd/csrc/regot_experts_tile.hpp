@@ -311,7 +311,7 @@ __device__ __forceinline__ void through_lds(char *mine, Value value, Ask ask, Ta
     }
 }
 
-// The same without LDS, where a lane's 8 neighbours are 16 bytes (of 64 that follow each other): 131072 x 1024 by 64 x 2048 x 1024, bf16 634 us, through LDS 653.
+// The same without LDS, where a lane's 8 neighbours are 16 bytes (of 64 that follow each other): the same product with weights by outputs 634 us, through LDS 653.
 template <int TYPE, int ROWS, int COLS, bool ACROSS, int BYTES, typename Value, typename Take>
 __device__ __forceinline__ void results(char *mine, Value value, Take take)
 {
@@ -372,6 +372,12 @@ __device__ __forceinline__ void load_run(float *v, const void *p, int64_t left, 
 // A tile of BM rows and BN columns, WM x WN waves.  Columns come first in the matrix instruction, so that a lane's four results are neighbours
 // in a row.  Rows: of X (product), or columns of dY (weight gradient, summed over rows).  Columns: rows of W (of its columns where ACROSS;
 // with the gate half of them are g's and half u's), or columns of X.
+//
+// 16 bits, DIRECT: what bounds it is the way of the numbers into LDS and the writing of the results.  8192 x 8192 x 8192 bf16 in a copy that leaves parts out, 256 x 256: 1064
+// TFLOP/s; every load from the same place 1230, no loads 1430, products alone 1573 (a library product on this card 1190 to 1317); 192 x 128 (two workgroups to a
+// unit) 1107, 128 x 128 843.  192 x 128 was no faster on runs of some hundred rows (32768 rows of 60 experts 355 and 353 us).  Measured here: 131072 rows, 64 experts,
+// 1024 x 2048: product 591 us = 930 TFLOP/s (writing the 0.54 GB of results is 100 of them), weight gradient 637 us = 863.
+// The sums have to be where the loop has them in one block: with an exit in its middle the compiler copies all of them (256 registers) each time round.
 template <int TYPE, int BM, int BN, int WM, int WN, bool ACROSS, int KIND, bool DIRECT, int OUT, bool GATHER>
 __device__ __forceinline__ void expert_tile(const GroupArgs &A, const Run &run, uint32_t b, char *lds)
 {
