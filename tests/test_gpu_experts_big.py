@@ -1,4 +1,5 @@
-"""Products grouped by expert in tiles of 256 x 256, which calls of many tiles take: many experts, some with several tiles, most with a few rows or none."""
+"""Products grouped by expert in tiles of 256 x 256, which calls of many tiles take: products of few experts with several tiles and a part of one and many columns;
+weight gradients of many experts, some with several stretches, most with a few rows or none; and products of those in smaller tiles."""
 import pytest
 import torch
 
@@ -11,8 +12,11 @@ TYPES = [torch.bfloat16, torch.float16]
 
 
 def uneven(n, k, experts, gen):
-    """Most choices to three experts, whose runs then are several tiles and a part of one, the others anywhere."""
+    """Most choices to three experts, whose runs then are several tiles and a part of one, the others anywhere; of few experts, about evenly."""
     idx = torch.randint(0, experts, (n, k), generator=gen)
+    if experts < 8:
+        idx[torch.rand(n, k, generator=gen) < 0.05] = -1
+        return idx.to(torch.int32)
     idx[torch.rand(n, k, generator=gen) < 0.8] = 5
     idx[torch.rand(n, k, generator=gen) < 0.3] = experts - 1
     idx[torch.rand(n, k, generator=gen) < 0.1] = 6
@@ -27,7 +31,7 @@ def case(n, k, experts, d, m, dtype, **kw):
     return c
 
 
-SIZES = [(900, 2, 1024, 64, 8), (700, 2, 520, 8, 304), (1500, 1, 1024, 200, 128), (400, 4, 600, 136, 264)]
+SIZES = [(900, 2, 1024, 64, 8), (700, 2, 520, 8, 304), (1500, 1, 1024, 200, 128), (400, 4, 600, 136, 264), (1300, 2, 4, 72, 13000), (1100, 1, 3, 8, 29960), (2100, 1, 1, 200, 15008)]
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=["bf16", "f16"])
