@@ -158,10 +158,11 @@ void launch(const GroupArgs &A, const TilePlan &P, int type, hipStream_t s)
 // (three), and leave more of the chip empty in the last round.  us, 256 / 128: 131072 rows of 64 experts, 1024 x 2048: product 577 / 715 (4400 tiles of 256),
 // weight gradient 648 / 778 (2048 tiles); 32768 rows of 60, 2048 by 2 x 1024 with the gate 353 / 390 (1264); 8192 rows of 8, 2048 x 1408: 87 / 83 (216), weight gradient
 // 80 / 69 (384).  128 / 64 rows: gradients of 2997 rows of 12 experts, 555 x 777: fp32 285 / 161, bf16 50 / 46 (250 and 420 tiles of 128).
+// Products of fewer than 192 rows an expert leave most of a tall tile empty: 600 rows of 128, 1024 x 2048 133 / 109, 16384 rows 160 / 156.
 template <typename Tiles>
-int choose_tile(int type, bool direct, Tiles tiles)
+int choose_tile(int type, bool direct, bool tall, Tiles tiles)
 {
-    if (direct && type != REGOT_F32 && tiles(tile_shape(kTileBig)) >= 2 * kCUs) return kTileBig;
+    if (direct && tall && type != REGOT_F32 && tiles(tile_shape(kTileBig)) >= 2 * kCUs) return kTileBig;
     const bool small = tiles(tile_shape(kTileDirect)) < 2 * kCUs;
     return direct ? small ? kTileDirectSmall : kTileDirect : small ? kTileStagedSmall : kTileStaged;
 }
@@ -412,7 +413,7 @@ int regot_expert_product(int64_t rows, int64_t m, int64_t d, int64_t experts, co
         A.groups = (int)few_groups(std::min(rows, experts), (wide + 31) / 32);
     } else {
         // (tiles of a call, where each expert's last one is half empty)
-        P.tile = choose_tile(type, direct, [&](TileShape T) { return (rows / T.rows + experts / 2) * ((wide + T.cols - 1) / T.cols); });
+        P.tile = choose_tile(type, direct, rows >= 192 * experts, [&](TileShape T) { return (rows / T.rows + experts / 2) * ((wide + T.cols - 1) / T.cols); });
     }
     const TileShape T = tile_shape(P.tile);
     const int64_t cols = P.tile == kTileFew ? T.cols * A.groups : T.cols;
@@ -471,7 +472,7 @@ int regot_expert_weight_grad(int64_t rows, int64_t m, int64_t d, int64_t experts
     const bool direct = whole_chunks(X, d, ldX, b) && whole_chunks(dY, m, ldY, b);
     A.whole = whole_chunks(A.Y, d, A.ldY, pb) && A.strideY % (16 / pb) == 0;
     P.tile = kTileDirectSmall;
-    if (!parts) P.tile = choose_tile(type, direct, [&](TileShape T) { return (m + T.rows - 1) / T.rows * ((d + T.cols - 1) / T.cols) * experts; });
+    if (!parts) P.tile = choose_tile(type, direct, true, [&](TileShape T) { return (m + T.rows - 1) / T.rows * ((d + T.cols - 1) / T.cols) * experts; });
     else if (!direct) P.tile = kTileStagedSmall;
     if (!parts) {
         G = plan_weight_grad(rows, m, d, experts, P.tile);

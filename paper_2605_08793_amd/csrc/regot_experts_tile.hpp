@@ -435,7 +435,7 @@ __device__ __forceinline__ void expert_tile(const GroupArgs &A, const Run &run, 
         }
     };
 
-    const int wave = threadIdx.x / kLanes, lane = threadIdx.x % kLanes, g = lane / 16, i = lane % 16;
+    const int wave = threadIdx.x / kLanes;
     const int wm = wave / WN, wn = wave % WN;
     // with the gate a wave's columns are kFragCols / 2 fragments of g and as many of u
     const auto col_fragment = [&](const char *lds, int f, int step) {
