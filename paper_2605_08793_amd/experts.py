@@ -93,6 +93,7 @@ class ExpertProduct(_Buffers):
         self._saved = self._buffer(self.rows, 2 * self.m, dtype=dtype) if keep and gated else None
         self._work = self._workspace(B.regot_expert_weight_grad_workspace_bytes(self.rows, self.wide, self.d, self.experts))
         self.dX = self.dW = None
+        self._other_dX = None  # that of the other width: a captured call may still write it
 
     def _run(self, X, x_rows, d, W, by, start, order, k, act, m, Y, saved, ldS):
         _, _, _, w_by, ldW, stride, w_at = W
@@ -111,7 +112,10 @@ class ExpertProduct(_Buffers):
 
     def _out(self, name, shape, dtype):
         t = getattr(self, name)
-        if t is None or (t.shape != shape and name == "dX"):
+        if name == "dX" and t is not None and t.shape != shape:
+            t, self._other_dX = self._other_dX, t
+            self.dX = t
+        if t is None:
             t = self._buffer(*shape, dtype=dtype)
             setattr(self, name, t)
         if t.shape != shape or t.dtype != dtype or t.device != self.device:

@@ -101,6 +101,36 @@ def test_captured_steps_replay_like_eager():
             assert torch.equal(a, b), (replay, i)
 
 
+def test_a_captured_gradient_keeps_its_buffer():
+    """The same object's gradients with and without the gate: what one wrote when it was captured stays its own when the other has been called."""
+    gen = torch.Generator().manual_seed(5)
+    rows, d, m, experts = 300, 64, 32, 7
+    start = torch.tensor([0, 40, 40, 90, 150, 151, 260, 300], device="cuda")
+    dY, W = torch.randn(rows, m, generator=gen).cuda(), torch.randn(experts, m, d, generator=gen).cuda()
+    saved = torch.randn(rows, 2 * d, generator=gen).cuda()
+    op = ExpertProduct(rows, m, d, experts, dtype=torch.float32)
+    op.input_grad(dY, W, start, saved=saved)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        behind_gate = op.input_grad(dY, W, start, saved=saved)
+    plain = op.input_grad(dY, W, start)
+    assert plain is op.dX and plain.shape == (rows, d) and behind_gate.shape == (rows, 2 * d)
+    other = torch.full((rows, 2 * d), 7.0, device="cuda")  # (would have the memory of a buffer that was let go)
+    kept = plain.clone()
+    for replay in range(3):
+        dY.copy_(torch.randn(rows, m, generator=gen))
+        behind_gate.fill_(3.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(plain, kept) and bool((other == 7.0).all()), replay
+        got = behind_gate.clone()
+        assert torch.equal(op.input_grad(dY, W, start, saved=saved), got) and op.dX is behind_gate, replay
+        op.dX.zero_()
+        assert op.input_grad(dY, W, start) is plain, replay
+        kept = plain.clone()
+
+
 def test_on_a_stream_of_its_own():
     gen = torch.Generator().manual_seed(4)
     idx = ref.choices(300, 2, 7, gen).cuda()
