@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <initializer_list>
 #include <memory>
 #include <new>
 
@@ -92,6 +93,14 @@ bool meet(const Memory &a, const Memory &b)
     const wide off = ((b0 - a0) % sa + sa) % sa;  // where b's rows begin in a's
     return off < ra || off + rb > sa;
 }
+
+// (for each output, the inputs and the outputs before it)
+bool meets(const Memory &a, std::initializer_list<Memory> others)
+{
+    return std::any_of(others.begin(), others.end(), [&](const Memory &b) { return meet(a, b); });
+}
+
+Memory list_of(const void *p, int64_t count, int bytes) { return {p, 1, count, 0, bytes}; }
 
 // The matrix of a call's weights: experts blocks, as rows one after the other
 Memory blocks_of(const void *p, int64_t experts, int64_t n, int64_t m, int64_t ld, int64_t stride, int bytes)
@@ -280,6 +289,13 @@ int clip(int64_t count, const regot_tensor *list, double max_norm, float *norm, 
     if (!workspace) return REGOT_ERR_NULL;
     if (misaligned(workspace, kAlign)) return REGOT_ERR_ALIGN;
     if (workspace_bytes < padded(P.parts * sizeof(double))) return REGOT_ERR_WORKSPACE;
+    const Memory norms = list_of(norm, 1, 4), factors = list_of(factor, 1, 4);
+    if (meet(norms, factors)) return REGOT_ERR_ARG;
+    for (int64_t t = 0; t < count; ++t) {
+        const int b = element_bytes(list[t].type);
+        const Memory in = list_of(list[t].data, list[t].count, b), out = list_of(scale ? list[t].out : nullptr, list[t].count, b);
+        if (meets(norms, {in, out}) || meets(factors, {in, out})) return REGOT_ERR_ARG;
+    }
     ClipArgs A{};
     A.each = P.each;
     A.parts = (uint32_t)P.parts;
@@ -351,8 +367,8 @@ int regot_expert_order(int64_t n, int k, int64_t experts, const int32_t *idx, in
     if (!workspace) return REGOT_ERR_NULL;
     if (misaligned(workspace, kAlign)) return REGOT_ERR_ALIGN;
     if (workspace_bytes < P.total) return REGOT_ERR_WORKSPACE;
-    const Memory in{idx, 1, n * k, 0, 4}, to{order, 1, n * k, 0, 4}, back{place, 1, n * k, 0, 4}, runs{start, 1, experts + 1, 0, 8};
-    if (meet(in, to) || meet(in, back) || meet(to, back) || meet(runs, in) || meet(runs, to) || meet(runs, back)) return REGOT_ERR_ARG;
+    const Memory in = list_of(idx, n * k, 4), to = list_of(order, n * k, 4), back = list_of(place, n * k, 4), runs = list_of(start, experts + 1, 8);
+    if (meet(to, in) || meets(back, {in, to}) || meets(runs, {in, to, back})) return REGOT_ERR_ARG;
     OrderArgs A{};
     A.idx = idx;
     A.count = n * k;
@@ -391,7 +407,8 @@ int regot_expert_product(int64_t rows, int64_t m, int64_t d, int64_t experts, co
     if (!work) return REGOT_OK;
     const Memory y{Y, rows, out, ldY, b}, x{X, x_rows, d, ldX, b}, kept{saved, rows, 2 * m, ldSaved, b};
     const Memory w = blocks_of(W, experts, w_rows, w_cols, ldW, strideW, b);
-    if (meet(y, x) || meet(y, w) || meet(y, kept) || (act == REGOT_ACT_GATE && (meet(kept, x) || meet(kept, w)))) return REGOT_ERR_ARG;
+    const Memory runs = list_of(start, experts + 1, 8), slots = list_of(order, rows, 4);
+    if (meets(y, {x, w, kept, runs, slots}) || (act == REGOT_ACT_GATE && meets(kept, {x, w, runs, slots}))) return REGOT_ERR_ARG;
     GroupArgs A = group_args(rows, m, d, experts, start, X, ldX, x_rows, order, k);
     A.W = W;
     A.ldW = ldW;
@@ -454,7 +471,7 @@ int regot_expert_weight_grad(int64_t rows, int64_t m, int64_t d, int64_t experts
     if (workspace_bytes < G.total) return REGOT_ERR_WORKSPACE;
     if (!work) return REGOT_OK;
     const Memory w = blocks_of(dW, experts, m, d, ldW, strideW, ob);
-    if (meet(w, {dY, rows, m, ldY, b}) || meet(w, {X, x_rows, d, ldX, b})) return REGOT_ERR_ARG;
+    if (meets(w, {{dY, rows, m, ldY, b}, {X, x_rows, d, ldX, b}, list_of(start, experts + 1, 8), list_of(order, rows, 4)})) return REGOT_ERR_ARG;
     GroupArgs A = group_args(rows, m, d, experts, start, X, ldX, x_rows, order, k);
     A.W = dY;
     A.ldW = ldY;
@@ -530,7 +547,7 @@ int regot_expert_combine(int64_t n, int k, int64_t m, int64_t rows, const void *
     const int b = element_bytes(type);
     if (misaligned(out, b)) return REGOT_ERR_ALIGN;
     if (n == 0 || m == 0) return REGOT_OK;
-    if (meet({out, n, m, ldO, b}, {Y, rows, m, ldY, b})) return REGOT_ERR_ARG;
+    if (meets({out, n, m, ldO, b}, {{Y, rows, m, ldY, b}, list_of(place, n * k, 4), list_of(weight, n * k, 4)})) return REGOT_ERR_ARG;
     CombineArgs A = combine_args(n, k, m, rows, Y, ldY, place, weight);
     A.out = out;
     A.ldO = ldO;
@@ -554,8 +571,9 @@ int regot_expert_combine_grad(int64_t n, int k, int64_t m, int64_t rows, const v
     const int b = element_bytes(type);
     if (misaligned(g_out, b) || misaligned(dY, b) || misaligned(g_weight, 4)) return REGOT_ERR_ALIGN;
     if (n == 0) return REGOT_OK;
-    const Memory d{dY, rows, m, ldD, b};
-    if (meet(d, {g_out, n, m, ldG, b}) || (g_weight && meet(d, {Y, rows, m, ldY, b}))) return REGOT_ERR_ARG;
+    const Memory d{dY, rows, m, ldD, b}, g{g_out, n, m, ldG, b}, y{g_weight ? Y : nullptr, rows, m, ldY, b};
+    const Memory places = list_of(place, n * k, 4), weights = list_of(weight, n * k, 4);
+    if (meets(d, {g, y, places, weights}) || meets(list_of(g_weight, n * k, 4), {d, g, y, places, weights})) return REGOT_ERR_ARG;
     CombineArgs A = combine_args(n, k, m, rows, Y, ldY, place, weight);
     A.g = g_out;
     A.ldG = ldG;

@@ -49,6 +49,14 @@ REFUSED = [("regot_expert_order", a, s) for a, s in [
         (dict(ldD=15), LD), (dict(ldY=15), LD), (dict(g_weight=HALF), ALIGN), (dict(dY=P), ARG), (dict(dY=Q), ARG)]]
 
 
+# outputs in the place of the small inputs, and of each other
+REFUSED += [("regot_expert_product", a, ARG) for a in (dict(Y=PRODUCT["start"]), dict(Y=PRODUCT["order"]), dict(act=1, saved=PRODUCT["start"]),
+                                                       dict(act=1, saved=PRODUCT["order"]))] + [
+    ("regot_expert_weight_grad", a, ARG) for a in (dict(dW=WEIGHT["start"]), dict(dW=WEIGHT["order"]))] + [
+    ("regot_expert_combine", a, ARG) for a in (dict(out=Q), dict(place=R, weight=None, out=R))] + [
+    ("regot_expert_combine_grad", a, ARG) for a in (dict(g_weight=P), dict(g_weight=Q), dict(g_weight=R), dict(place=R, weight=None), dict(weight=R))]
+
+
 def call(name, **changed):
     args = {**CALLS[name], **changed}
     assert set(args) == set(CALLS[name])
@@ -112,6 +120,9 @@ def test_clip_refusals():
     for changed, status in ((dict(max_norm=0.0), ARG), (dict(max_norm=-1.0), ARG), (dict(max_norm=float("nan")), ARG), (dict(norm=None), NULL), (dict(factor=None), NULL),
                             (dict(norm=HALF), ALIGN), (dict(ws=None), NULL), (dict(ws_bytes=0), WORKSPACE), (dict(ws=ctypes.c_void_p(0x800010)), ALIGN)):
         assert clip([tensor(), far], **changed) == status, changed
+    for norm, factor in ((Q, Q), (P, Q), (Q, P), (ctypes.c_void_p(0x100000 + 396), Q), (Q, ctypes.c_void_p(0x500000))):
+        assert clip([tensor(), tensor(0x600000, 0x500000)], norm=norm, factor=factor) == ARG, (norm, factor)
+    assert B.load().regot_grad_norm(1, listed(tensor()), P, WS, BIG, None) == ARG
     out = ctypes.c_size_t()
     assert B.load().regot_grad_norm_workspace_bytes(1, listed(tensor()), None) == NULL
     assert B.load().regot_grad_norm_workspace_bytes(1, listed(tensor(count=-2)), ctypes.byref(out)) == DIM
