@@ -658,6 +658,11 @@ def _weights(W: torch.Tensor, name="W"):
     return experts, outputs, inputs, by, ld, stride, W.data_ptr()
 
 
+def _one_device(*tensors):
+    if len({t.get_device() for t in tensors if isinstance(t, torch.Tensor)}) > 1:
+        raise TypeError("the tensors of a call must be on one device")
+
+
 def regot_expert_order_workspace_bytes(n: int, k: int, experts: int) -> int:
     out = ctypes.c_size_t(0)
     _check(load().regot_expert_order_workspace_bytes(int(n), int(k), int(experts), ctypes.byref(out)), "regot_expert_order_workspace_bytes")
@@ -666,6 +671,7 @@ def regot_expert_order_workspace_bytes(n: int, k: int, experts: int) -> int:
 
 def regot_expert_order(idx, start, order, place, *, workspace, stream=None) -> None:
     """idx, place (n, k), order (n * k): int32; start (experts + 1): int64."""
+    _one_device(idx, start, order, place, workspace)
     if not isinstance(idx, torch.Tensor) or idx.dim() not in (1, 2):
         raise TypeError("idx must be a 1-D or 2-D int32 CUDA tensor")
     n, k = idx.shape[0], _width(idx, idx.shape[0], "idx")
@@ -678,6 +684,7 @@ def regot_expert_order(idx, start, order, place, *, workspace, stream=None) -> N
 
 def regot_expert_product(X, W, start, Y, *, order=None, k=1, act=None, saved=None, stream=None) -> None:
     """X (x_rows, d), W (experts, m or 2 m, d), Y (rows, m or 2 m), saved (rows, 2 m): one type; order (rows): int32, start: int64."""
+    _one_device(X, W, start, Y, order, saved)
     x_rows, d, kind, ldX, at = _scores(X, "X")
     experts, wide, inputs, by, ldW, stride, w_at = _weights(W)
     rows, out, _, ldY, to = _scores(Y, "Y")
@@ -706,6 +713,7 @@ def regot_expert_weight_grad_workspace_bytes(rows: int, m: int, d: int, experts:
 
 def regot_expert_weight_grad(dY, X, start, dW, *, order=None, k=1, workspace, stream=None) -> None:
     """dY (rows, m) and X (x_rows, d) of one type, dW (experts, m, d) of that type or float32, the numbers of its last dimension neighbours."""
+    _one_device(dY, X, start, dW, order, workspace)
     rows, m, kind, ldY, g_at = _scores(dY, "dY")
     x_rows, d, _, ldX, at = _scores(X, "X")
     experts, outputs, inputs, by, ldW, stride, to = _weights(dW, "dW")
@@ -719,6 +727,7 @@ def regot_expert_weight_grad(dY, X, start, dW, *, order=None, k=1, workspace, st
 
 def regot_expert_combine(Y, place, weight, out, *, stream=None) -> None:
     """Y (rows, m), out (n, m); place (n, k) int32, weight (n, k) or None."""
+    _one_device(Y, place, weight, out)
     rows, m, kind, ldY, at = _scores(Y, "Y")
     n, cols, _, ldO, to = _scores(out, "out")
     if cols != m or out.dtype != Y.dtype:
@@ -731,6 +740,7 @@ def regot_expert_combine(Y, place, weight, out, *, stream=None) -> None:
 
 def regot_expert_combine_grad(g_out, Y, place, weight, dY, g_weight=None, *, stream=None) -> None:
     """g_out (n, m), dY (rows, m); Y (rows, m) and g_weight (n, k), or both None."""
+    _one_device(g_out, Y, place, weight, dY, g_weight)
     n, m, kind, ldG, g_at = _scores(g_out, "g_out")
     rows, cols, _, ldD, to = _scores(dY, "dY")
     if cols != m or dY.dtype != g_out.dtype:
@@ -774,11 +784,13 @@ def regot_grad_norm_workspace_bytes(tensors) -> int:
 
 
 def regot_grad_norm(tensors, norm, *, workspace, stream=None) -> None:
+    _one_device(*tensors, norm, workspace)
     _check(load().regot_grad_norm(len(tensors), _tensors(tensors), _list(norm, 1, 1, "norm"), *_ws(workspace), _list_stream(tensors, stream)),
            "regot_grad_norm")
 
 
 def regot_grad_clip(tensors, max_norm, norm, factor, out=None, *, workspace, stream=None) -> None:
+    _one_device(*tensors, norm, factor, workspace)
     _check(load().regot_grad_clip(
         len(tensors), _tensors(tensors, out), float(max_norm), _list(norm, 1, 1, "norm"), _list(factor, 1, 1, "factor"), *_ws(workspace),
         _list_stream(tensors, stream)), "regot_grad_clip")

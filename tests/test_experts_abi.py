@@ -6,7 +6,7 @@ import torch
 
 from paper_2605_08793_amd import binding as B
 from paper_2605_08793_amd.experts import ExpertCombine, ExpertOrder, ExpertProduct
-from test_rows_abi import fake
+from test_rows_abi import FakeCuda, fake
 
 P, Q, R = (ctypes.c_void_p(a) for a in (0x100000, 0x200000, 0x300000))  # never dereferenced
 ODD, HALF, QUAD = ctypes.c_void_p(0x100001), ctypes.c_void_p(0x100002), ctypes.c_void_p(0x100004)
@@ -158,6 +158,31 @@ def test_the_binding_checks_weights():
     for bad in (fake(3, 4), fake(3, 4, 5, dtype=torch.float64), fake(3, 4, 10)[:, :, ::2], fake(3, 1, 5).expand(3, 4, 5), torch.zeros(3, 4, 5), None):
         with pytest.raises(TypeError):
             B._weights(bad)
+
+
+class Elsewhere(FakeCuda):
+    def get_device(self):
+        return 1
+
+
+def test_tensors_of_two_devices_are_refused():
+    """Each tensor of each call in turn."""
+    whole = lambda *shape: fake(*shape, dtype=torch.int32)  # noqa: E731
+    start, ws = fake(4, dtype=torch.int64), fake(1 << 16, dtype=torch.uint8)
+    calls = [(B.regot_expert_order, (whole(4, 2), start, whole(8), whole(4, 2)), dict(workspace=ws)),
+             (B.regot_expert_product, (fake(4, 5), fake(3, 12, 5), start, fake(8, 6)), dict(order=whole(8), k=2, act="gate", saved=fake(8, 12))),
+             (B.regot_expert_weight_grad, (fake(8, 6), fake(4, 5), start, fake(3, 6, 5)), dict(order=whole(8), k=2, workspace=ws)),
+             (B.regot_expert_combine, (fake(8, 6), whole(4, 2), fake(4, 2), fake(4, 6)), {}),
+             (B.regot_expert_combine_grad, (fake(4, 6), fake(8, 6), whole(4, 2), fake(4, 2), fake(8, 6), fake(4, 2)), {}),
+             (B.regot_grad_norm, ([fake(5)], fake(1)), dict(workspace=ws)), (B.regot_grad_clip, ([fake(5)], 1.0, fake(1), fake(1)), dict(workspace=ws))]
+    for call, args, named in calls:
+        both = [*args, *named.values()]
+        for i, t in enumerate(both):
+            if not isinstance(t, torch.Tensor):
+                continue
+            moved = both[:i] + [t.as_subclass(torch.Tensor).as_subclass(Elsewhere)] + both[i + 1:]
+            with pytest.raises(TypeError, match="one device"):
+                call(*moved[:len(args)], **dict(zip(named, moved[len(args):])))
 
 
 def test_buffers_are_not_replaced_and_shapes():
