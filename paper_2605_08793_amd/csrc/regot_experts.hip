@@ -167,17 +167,30 @@ void launch(const GroupArgs &A, const TilePlan &P, int type, hipStream_t s)
 // (three), and leave more of the chip empty in the last round.  us, 256 / 128: 131072 rows of 64 experts, 1024 x 2048: product 577 / 715 (4400 tiles of 256),
 // weight gradient 648 / 778 (2048 tiles); 32768 rows of 60, 2048 by 2 x 1024 with the gate 353 / 390 (1264); 8192 rows of 8, 2048 x 1408: 87 / 83 (216), weight gradient
 // 80 / 69 (384).  128 / 64 rows: gradients of 2997 rows of 12 experts, 555 x 777: fp32 285 / 161, bf16 50 / 46 (250 and 420 tiles of 128).
-// Products of fewer than 192 rows an expert leave most of a tall tile empty: 600 rows of 128, 1024 x 2048 133 / 109, 16384 rows 160 / 156.
-template <typename Tiles>
-int choose_tile(int type, bool direct, bool tall, Tiles tiles)
+// So they are taken from `least` tiles on:
+// weight gradients 2 rounds; products 2.5 (576 tiles: 16384 rows of 16, 1024 x 2048 90 / 80; 720: 2048 x 2560 188 / 206), but none of fewer than 192 rows an expert, which
+// leave most of a tall tile empty (600 rows of 128, 1024 x 2048 133 / 109, 16384 rows 160 / 156); behind the gate, where a tile ends with as many reads as writes and nothing
+// else runs on its unit, 4 rounds of long sums (65536 rows of 64, 1024 outputs, sums of 512 238 / 201, 1024 296 / 273, 2048 411 / 417, 4096 655 / 711).
+constexpr int64_t kNever = INT64_MAX;
+
+int64_t least_tall(int kind, int64_t rows, int64_t d, int64_t experts)
 {
-    if (direct && tall && type != REGOT_F32 && tiles(tile_shape(kTileBig)) >= 2 * kCUs) return kTileBig;
+    if (kind == kWeightGrad) return 2 * kCUs;
+    if (rows < 192 * experts) return kNever;
+    return kind != kGateGrad ? 5 * kCUs / 2 : d >= 2048 ? 4 * kCUs : kNever;
+}
+
+template <typename Tiles>
+int choose_tile(int type, bool direct, int64_t least, Tiles tiles)
+{
+    if (direct && type != REGOT_F32 && tiles(tile_shape(kTileBig)) >= least) return kTileBig;
     const bool small = tiles(tile_shape(kTileDirect)) < 2 * kCUs;
     return direct ? small ? kTileDirectSmall : kTileDirect : small ? kTileStagedSmall : kTileStaged;
 }
 
-// (us, tiles of 128 x 128 / few rows, 1400 x 2048 fp16: 256 rows of 60 experts 74 / 70, 512 rows 99 / 83)
-constexpr int64_t kFewRows = 16;  // rows of an expert, on average
+// (us, tiles of 64 x 128 / few rows, bf16, 60 experts: 1400 x 2048, 480 rows 79 / 68, 960 72 / 86; 1400 x 4096 147 / 129, 148 / 167; 512 x 4096 55 / 45, 53 / 57; 16 of 2048 x 4096, 256
+// rows 58 / 52)
+constexpr int64_t kFewRows = 12;  // rows of an expert, on average
 
 // How many stretches of 32 rows of W a workgroup of the kernel for few rows has, of `all` that each of `runs` experts' weights have: four rounds of workgroups, one to a
 // compute unit, so that the last one does not weigh much, or one where two stretches are enough for that.  us, 1 / 2 / 4 / 8 / 16 stretches: 256 rows of 60 experts, 1400 x
@@ -188,7 +201,10 @@ int64_t few_groups(int64_t runs, int64_t all)
     return std::min(all, std::max(rounds(4), std::min<int64_t>(rounds(1), 2)));
 }
 
-// A weight gradient of few tiles is summed in parts, which a second launch adds up.
+// A weight gradient of few tiles is summed in parts of so many rows at least, which a second launch adds up.  us, parts of 512 / 256 / 128 / 64 rows: fp32, 71904 rows
+// of 120 experts, 64 x 111 91 / 56 / 37 / 37, 2048 of 8, 256 x 256 22 / 22 / 18 / 17; bf16, 71904 rows of 120, 64 x 128 11 / 15 / 18 / 18, 1000 of 4, 512 x 512 8 / 8 / 8 / 15.
+constexpr int64_t kPart = 512, kPartF32 = 128;
+
 struct GradPlan {
     int64_t tiles_m = 0, tiles_d = 0;
     int splits = 1;
@@ -196,14 +212,14 @@ struct GradPlan {
     int64_t tiles(int64_t experts) const { return tiles_m * tiles_d * experts * splits; }
 };
 
-GradPlan plan_weight_grad(int64_t rows, int64_t m, int64_t d, int64_t experts, int tile)
+GradPlan plan_weight_grad(int64_t rows, int64_t m, int64_t d, int64_t experts, int tile, int64_t part)
 {
     GradPlan P;
     const TileShape T = tile_shape(tile);
     P.tiles_m = (m + T.rows - 1) / T.rows;
     P.tiles_d = (d + T.cols - 1) / T.cols;
     const int64_t tiles = P.tiles_m * P.tiles_d * experts;
-    if (tiles > 0 && tiles < kCUs) P.splits = (int)std::max<int64_t>(std::min<int64_t>(2 * kCUs / tiles, rows / experts / 512), 1);
+    if (tiles > 0 && tiles < kCUs) P.splits = (int)std::max<int64_t>(std::min<int64_t>(2 * kCUs / tiles, rows / experts / part), 1);
     P.total = padded(P.splits > 1 ? (size_t)P.splits * experts * m * d * sizeof(float) : 0);
     return P;
 }
@@ -425,12 +441,12 @@ int regot_expert_product(int64_t rows, int64_t m, int64_t d, int64_t experts, co
     // (a half's numbers end with a chunk too)
     A.whole = whole_chunks(Y, m, ldY, b) && (!saved || whole_chunks(saved, m, ldSaved, b));
     P.units = (d * b + 128 * kFewWaves - 1) / (128 * kFewWaves);
-    if (direct && A.whole && m % 8 == 0 && !P.across && P.kind != kGateGrad && rows <= kFewRows * experts && P.units <= kFewUnits) {
+    if (direct && !P.across && P.kind != kGateGrad && rows <= kFewRows * experts && P.units <= kFewUnits) {
         P.tile = kTileFew;
         A.groups = (int)few_groups(std::min(rows, experts), (wide + 31) / 32);
     } else {
         // (tiles of a call, where each expert's last one is half empty)
-        P.tile = choose_tile(type, direct, rows >= 192 * experts, [&](TileShape T) { return (rows / T.rows + experts / 2) * ((wide + T.cols - 1) / T.cols); });
+        P.tile = choose_tile(type, direct, least_tall(P.kind, rows, d, experts), [&](TileShape T) { return (rows / T.rows + experts / 2) * ((wide + T.cols - 1) / T.cols); });
     }
     const TileShape T = tile_shape(P.tile);
     const int64_t cols = P.tile == kTileFew ? T.cols * A.groups : T.cols;
@@ -448,7 +464,7 @@ int regot_expert_weight_grad_workspace_bytes(int64_t rows, int64_t m, int64_t d,
 {
     if (!bytes) return REGOT_ERR_NULL;
     if (bad_dim(rows) || bad_dim(m) || bad_dim(d) || experts < 0 || experts > REGOT_ROW_MAX_EXPERTS) return REGOT_ERR_DIM;
-    *bytes = plan_weight_grad(rows, m, d, experts, kTileDirectSmall).total;  // (larger tiles are many, and not in parts)
+    *bytes = plan_weight_grad(rows, m, d, experts, kTileDirectSmall, kPartF32).total;  // (larger tiles are many, and not in parts)
     return REGOT_OK;
 }
 
@@ -465,7 +481,8 @@ int regot_expert_weight_grad(int64_t rows, int64_t m, int64_t d, int64_t experts
     if (ldY < m || ldW < d || (experts > 1 && m > 0 && strideW < (m - 1) * ldW + d)) return REGOT_ERR_LD;
     const int b = element_bytes(type), ob = element_bytes(out_type);
     if (misaligned(dY, b) || misaligned(dW, ob)) return REGOT_ERR_ALIGN;
-    GradPlan G = plan_weight_grad(rows, m, d, experts, kTileDirectSmall);
+    const int64_t part = type == REGOT_F32 ? kPartF32 : kPart;
+    GradPlan G = plan_weight_grad(rows, m, d, experts, kTileDirectSmall, part);
     if (!workspace) return REGOT_ERR_NULL;
     if (misaligned(workspace, kAlign)) return REGOT_ERR_ALIGN;
     if (workspace_bytes < G.total) return REGOT_ERR_WORKSPACE;
@@ -489,10 +506,10 @@ int regot_expert_weight_grad(int64_t rows, int64_t m, int64_t d, int64_t experts
     const bool direct = whole_chunks(X, d, ldX, b) && whole_chunks(dY, m, ldY, b);
     A.whole = whole_chunks(A.Y, d, A.ldY, pb) && A.strideY % (16 / pb) == 0;
     P.tile = kTileDirectSmall;
-    if (!parts) P.tile = choose_tile(type, direct, true, [&](TileShape T) { return (m + T.rows - 1) / T.rows * ((d + T.cols - 1) / T.cols) * experts; });
+    if (!parts) P.tile = choose_tile(type, direct, least_tall(kWeightGrad, rows, d, experts), [&](TileShape T) { return (m + T.rows - 1) / T.rows * ((d + T.cols - 1) / T.cols) * experts; });
     else if (!direct) P.tile = kTileStagedSmall;
     if (!parts) {
-        G = plan_weight_grad(rows, m, d, experts, P.tile);
+        G = plan_weight_grad(rows, m, d, experts, P.tile, part);
         G.splits = 1;
     }
     const int64_t tiles = G.tiles(experts);

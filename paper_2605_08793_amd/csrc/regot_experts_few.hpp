@@ -12,7 +12,8 @@ constexpr int kFewUnits = 16;                // units of a sum that a wave can h
 // reading of the weights, once each, so everything is for keeping loads under way: each wave has its share of the sum, a unit of 128 bytes of each row at a time (so that
 // a workgroup reads 1 KB of each of 32 rows), which it loads into its own part of LDS, four units ahead and across the ends of sums, without
 // registers and without waiting for another wave.  The rows' numbers stay in registers.  The waves' sums are added up in their order, by each wave in turn.
-// Measured: 64 tokens x 4 of 60 experts, 1400 x 2048 fp16 69 us = 5.0 TB/s; one token, 8 of 256, 2048 by 2 x 1024 bf16 14 us = 4.8 TB/s.  (Loads alone in the same order reach 5.4 TB/s
+// Measured: 64 tokens x 4 of 60 experts, 1400 x 2048 fp16 69 us = 5.0 TB/s; one token, 8 of 256, 2048 by 2 x 1024 bf16 14 us = 4.8 TB/s; sums of 3712, 864 rows of 229, 2 x
+// 64 bf16 46 us = 4.8 TB/s.  (Loads alone in the same order reach 5.4 TB/s
 // on rows of 2800 bytes and 6.0 on rows of whole lines; a workgroup's begin, until its first numbers are there, is what is missing.)
 template <int TYPE, bool GATE, int MOST>
 __global__ void __launch_bounds__(kFewWaves *kLanes) expert_few_kernel(const GroupArgs A)
@@ -87,18 +88,18 @@ __global__ void __launch_bounds__(kFewWaves *kLanes) expert_few_kernel(const Gro
         for (int half = 0; half < 2; ++half) asm volatile("" : "+v"(x[u][half]));  // (there before the loop, in which nothing but W is waited for)
 
     const int64_t r = run.first + i;
-    const auto store = [&](void *to, int64_t ld, int64_t c, const float *v) {
+    const auto store = [&](void *to, int64_t ld, int64_t c, const float *v, int64_t left) {
         Raw part[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) part[e] = Score<TYPE>::put(v[e]);
-        store_run<TYPE, 4>(static_cast<char *>(to) + (r * ld + c) * kElem, part, 1, true);
+        store_run<TYPE, 4>(static_cast<char *>(to) + (r * ld + c) * kElem, part, left, A.whole);
     };
     int slot = 0, s = 0;
     for (int of = 0; of < groups; ++of) {
         f32x4 acc[2] = {};
 #pragma unroll
         for (int u = 0; u < MOST; ++u) {
-            if (u >= mine) break;
+            if (u >= mine) continue;  // (an exit of the loop would leave it as a loop, and x in memory)
             // (this unit's loads are the oldest)
             const int behind = min(all - 1 - s, kFewAhead - 1);
             if (behind == 3) asm volatile("s_waitcnt vmcnt(12)" ::: "memory");
@@ -138,14 +139,14 @@ __global__ void __launch_bounds__(kFewWaves *kLanes) expert_few_kernel(const Gro
             float h[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) h[e] = v[0][e] * sigmoid(v[0][e]) * v[1][e];
-            store(A.Y, A.ldY, c, h);
+            store(A.Y, A.ldY, c, h, A.m - c);
             if (A.saved) {
-                store(A.saved, A.ldSaved, c, v[0]);
-                store(A.saved, A.ldSaved, A.m + c, v[1]);
+                store(A.saved, A.ldSaved, c, v[0], A.m - c);
+                store(A.saved, A.ldSaved, A.m + c, v[1], A.m - c);
             }
         } else {
-            store(A.Y, A.ldY, c, v[0]);
-            store(A.Y, A.ldY, c + 4, v[1]);
+            store(A.Y, A.ldY, c, v[0], A.m - c);
+            store(A.Y, A.ldY, c + 4, v[1], A.m - c - 4);
         }
     }
 }

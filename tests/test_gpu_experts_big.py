@@ -5,6 +5,7 @@ import torch
 
 import experts_reference as ref
 from paper_2605_08793_amd.experts import ExpertProduct
+from rows_reference import U
 from test_gpu_experts_product import Case, matrix, same_beyond
 
 pytestmark = pytest.mark.gpu
@@ -31,7 +32,8 @@ def case(n, k, experts, d, m, dtype, **kw):
     return c
 
 
-SIZES = [(900, 2, 1024, 64, 8), (700, 2, 520, 8, 304), (1500, 1, 1024, 200, 128), (400, 4, 600, 136, 264), (1300, 2, 4, 72, 13000), (1100, 1, 3, 8, 29960), (2100, 1, 1, 200, 15008)]
+SIZES = [(900, 2, 1024, 64, 8), (700, 2, 520, 8, 304), (1500, 1, 1024, 200, 128), (400, 4, 600, 136, 264), (1300, 2, 4, 72, 13000), (1100, 1, 3, 8, 29960), (2100, 1, 1, 200, 15008),
+         (1300, 2, 4, 72, 14344), (1100, 1, 3, 8, 34952)]
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=["bf16", "f16"])
@@ -80,3 +82,24 @@ def test_gradients(n, k, experts, d, m, turned, behind_gate, dtype):
             op = c.op(grad_dtype=out)
             op.weight_grad(dY, X, start, order if gather else None, k if gather else 1)
             ref.close(op.dW, want, ref.rounded(want, tol, out), f"dW {out} {gather}")
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["bf16", "f16"])
+@pytest.mark.parametrize("turned", [False, True], ids=["outputs", "inputs"])
+def test_long_sums_behind_the_gate(turned, dtype):
+    """Few rows, very many columns, so that a long sum's tiles are many.  The plain side on the device, in 64 bits."""
+    rows, experts, d, m = 700, 2, 87304, 2056
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    normal = lambda *shape, scale=1.0: (torch.randn(*shape, generator=gen, device="cuda") * scale).to(dtype)  # noqa: E731
+    runs = [3, 300, 650]
+    dY, saved = normal(rows, m), normal(rows, 2 * d, scale=3.0)
+    W = normal(experts, d, m, scale=m ** -0.5).transpose(1, 2) if turned else normal(experts, m, d, scale=m ** -0.5)
+    op = ExpertProduct(rows, m, d, experts, dtype=dtype)
+    op.dX = torch.full((rows, 2 * d), 7.0, dtype=dtype, device="cuda")
+    op.input_grad(dY, W, torch.tensor(runs, device="cuda"), saved=saved)
+    for e, (a, b) in enumerate(zip(runs, runs[1:])):
+        w, g = W[e].double().contiguous(), dY[a:b].double()
+        D, tol = g @ w, (g.abs() @ w.abs()) * 2 * U * (m + 16) + ref.TINY
+        want, tol = ref.gate_grad(D, tol, saved[a:b].double())
+        ref.close(op.dX[a:b], want.cpu(), ref.rounded(want.cpu(), tol.cpu(), dtype), f"expert {e}")
+    assert bool((op.dX[:3] == 7.0).all()) and bool((op.dX[650:] == 7.0).all())

@@ -9,9 +9,10 @@ from rows_reference import TYPES, TYPE_IDS
 pytestmark = pytest.mark.gpu
 
 # (n, k, experts, d, m): sums of one unit, a unit and a part of one, as many units as waves, one more, four for each wave and more; rows of W that end within
-# a stretch of 32, many stretches; runs of 0, 1, 16, 17 and more rows
+# a stretch of 32, and within a chunk of 16 bytes, many stretches; runs of 0, 1, 16, 17 and more rows
 SIZES = [(1, 1, 1, 8, 8), (1, 8, 256, 2048, 96), (3, 2, 7, 64, 40), (5, 3, 4, 72, 32), (16, 1, 1, 512, 24), (17, 1, 2, 576, 1000), (40, 4, 10, 504, 264), (64, 4, 30, 2056, 72),
-         (2, 1, 8, 8192, 64), (9, 8, 1024, 136, 2048)]
+         (2, 1, 8, 8192, 64), (9, 8, 1024, 136, 2048),
+         (12, 1, 1, 512, 24), (40, 3, 10, 504, 264), (5, 3, 4, 72, 33), (1, 8, 256, 2048, 119), (3, 2, 7, 64, 6), (40, 3, 12, 504, 1), (2, 1, 8, 8192, 59), (100, 1, 9, 4104, 150)]
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=TYPE_IDS)
