@@ -715,6 +715,12 @@ __device__ __forceinline__ void expert_tile(const GroupArgs &A, const Run &run, 
             const int64_t r = row_of(x, i), col = first_col + wn * kFragCols * 16 + c;
             typename Score<OUT>::Raw of[16 / kOutElem];
             __builtin_memcpy(of, &v, 16);
+            if (KIND == kWeightGrad && A.whole) {
+                // nothing reads them soon: they go past the caches, which keep what other tiles read too (256 rows of each of 60 experts, 2048 x 2048 bf16 265 us, and so 200;
+                // 4 of each 142 and 123; 512 of 8, 14336 x 4096 868 and 722.  A product's results are read next: a layer's way forward is 208 us, and would be 228)
+                if (r < row_end && col < col_end) __builtin_nontemporal_store(v, reinterpret_cast<u32x4 *>(Y + (r * A.ldY + col) * kOutElem));
+                return;
+            }
             if (r < row_end) store_run<OUT, 16 / kOutElem>(Y + (r * A.ldY + col) * kOutElem, of, col_end - col, A.whole);
         });
     }
