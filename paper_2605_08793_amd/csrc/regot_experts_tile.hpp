@@ -376,7 +376,8 @@ __device__ __forceinline__ void load_run(float *v, const void *p, int64_t left, 
 // 16 bits, DIRECT: what bounds it is the way of the numbers into LDS and the writing of the results.  8192 x 8192 x 8192 bf16 in a copy that leaves parts out, 256 x 256: 1064
 // TFLOP/s; every load from the same place 1230, no loads 1430, products alone 1573 (a library product on this card 1190 to 1317); 192 x 128 (two workgroups to a
 // unit) 1107, 128 x 128 843.  192 x 128 was no faster on runs of some hundred rows (32768 rows of 60 experts 355 and 353 us).  Measured here: 131072 rows, 64 experts,
-// 1024 x 2048: product 591 us = 930 TFLOP/s (writing the 0.54 GB of results is 100 of them), weight gradient 637 us = 863.
+// 1024 x 2048: product 591 us = 930 TFLOP/s (writing the 0.54 GB of results is 100 of them), weight gradient of gathered rows
+// to fp32 637 us = 863, of rows as they are to bf16 537 = 1024.
 // The sums have to be where the loop has them in one block: with an exit in its middle the compiler copies all of them (256 registers) each time round.
 template <int TYPE, int BM, int BN, int WM, int WN, bool ACROSS, int KIND, bool DIRECT, int OUT, bool GATHER>
 __device__ __forceinline__ void expert_tile(const GroupArgs &A, const Run &run, uint32_t b, char *lds)
