@@ -70,6 +70,22 @@ struct Run {
     int64_t first, end;  // rows of the tile: first .. min(first + BM, end) - 1; none where first >= end
 };
 
+// Whether tile t is behind those of expert i, whose run ends at `end`
+template <int BM>
+__host__ __device__ constexpr bool tile_is_behind(int end, int i, int64_t t, bool single)
+{
+    return single ? end <= t : end / BM + i + 1 <= t;
+}
+
+// Tile t where it is behind those of e experts: s is where the run of expert e begins, end where it ends
+template <int BM>
+__host__ __device__ constexpr Run run_of_tile(int e, int s, int end, int64_t t, bool single)
+{
+    if (single) return {e, t, t < s || (t - s) % BM != 0 ? t : end};
+    const int64_t place = t - s / BM - e;  // among the expert's tiles; below 0: in front of the first run, no tile
+    return {e, s + place * BM, place < 0 ? 0 : end};
+}
+
 template <int BM>
 __device__ __forceinline__ Run find_run(const GroupArgs &A, int64_t t)
 {
@@ -84,7 +100,7 @@ __device__ __forceinline__ Run find_run(const GroupArgs &A, int64_t t)
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j) {
             const int i = i0 + j * kLanes;
-            const bool is = i < A.experts, before = is && (A.single ? ends[j] <= t : ends[j] / BM + i + 1 <= t);
+            const bool is = i < A.experts, before = is && tile_is_behind<BM>(ends[j], i, t, A.single);
             e += __popcll(__ballot(before));
             s = before ? max(s, ends[j]) : s;
             end = is && !before ? min(end, ends[j]) : end;
@@ -99,8 +115,7 @@ __device__ __forceinline__ Run find_run(const GroupArgs &A, int64_t t)
     s = __builtin_amdgcn_readfirstlane(e == 0 ? first_start : s);
     end = __builtin_amdgcn_readfirstlane(end);
     e = __builtin_amdgcn_readfirstlane(e);
-    if (A.single) return {e, t, t < s || (t - s) % BM != 0 ? t : end};
-    return {e, s + (t - s / BM - e) * BM, end};
+    return run_of_tile<BM>(e, s, end, t, A.single);
 }
 
 // Workgroups that follow each other run on different dies: each die gets a run of tiles, so that the tiles under way on one share
