@@ -77,7 +77,8 @@ class ExpertProduct(_Buffers):
     `gated`: the first m outputs are put through silu and multiplied by the others.
 
     After `product`: .Y (rows, m), and with `keep` .saved (rows, 2 m: the outputs before the gate).  After `input_grad`: .dX; after
-    `weight_grad`: .dW, of type `grad_dtype` (that of the rows, or float32).  .dX and .dW can be replaced by tensors of the same shape."""
+    `weight_grad`: .dW, of type `grad_dtype` (that of the rows, or float32).  .dX and .dW can be replaced by tensors of the same shape and type (.dX by one of either width: it is
+    that of the last call, and each width keeps its own)."""
     Y, saved, workspace = map(_output, ("_Y", "_saved", "_work"))
 
     def __init__(self, rows: int, m: int, d: int, experts: int, gated=False, keep=False, dtype=torch.bfloat16, grad_dtype=None, device="cuda"):
@@ -93,7 +94,7 @@ class ExpertProduct(_Buffers):
         self._saved = self._buffer(self.rows, 2 * self.m, dtype=dtype) if keep and gated else None
         self._work = self._workspace(B.regot_expert_weight_grad_workspace_bytes(self.rows, self.wide, self.d, self.experts))
         self.dX = self.dW = None
-        self._other_dX = None  # that of the other width: a captured call may still write it
+        self._aside = {}  # .dX by its columns, of the width that was not asked for last: a captured call may still write it
 
     def _run(self, X, x_rows, d, W, by, start, order, k, act, m, Y, saved, ldS):
         _, _, _, w_by, ldW, stride, w_at = W
@@ -112,14 +113,14 @@ class ExpertProduct(_Buffers):
 
     def _out(self, name, shape, dtype):
         t = getattr(self, name)
-        if name == "dX" and t is not None and t.shape != shape:
-            t, self._other_dX = self._other_dX, t
-            self.dX = t
+        if name == "dX" and t is not None and t.shape != shape and t.shape in ((self.rows, self.d), (self.rows, 2 * self.d)):
+            self._aside[t.shape[1]] = t
+            t = self._aside.get(shape[1])
         if t is None:
             t = self._buffer(*shape, dtype=dtype)
-            setattr(self, name, t)
         if t.shape != shape or t.dtype != dtype or t.device != self.device:
             raise TypeError(f"{name} must be of shape {tuple(shape)}, type {dtype}, on {self.device}")
+        setattr(self, name, t)
         return t
 
     def product(self, X, W, start, order=None, k=1):
