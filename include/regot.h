@@ -769,7 +769,8 @@ int regot_expert_combine_grad(int64_t n, int k, int64_t m, int64_t rows,
 /*
  * The norm over many tensors, and clipping:
  *     norm[0]   = sqrt(sum of the squares of all numbers of all tensors), squares and sums in fp64
- *     factor[0] = max_norm / norm where norm > max_norm, else 1; 1 too where the norm is not finite: a program looks at norm and leaves the step out
+ *     factor[0] = max_norm / norm where norm > max_norm, else 1; 1 too where norm[0] is not finite (a norm beyond fp32 is told as inf): a program looks at
+ *                 norm and leaves the step out
  *     out       = factor * data, rounded once, for each tensor; out may be data, and is then not written where factor is 1
  * `list` is a HOST array, read during the call; each tensor is `count` numbers without gaps.  Types may differ.  regot_grad_norm does not look at
  * `out`.  Tensors whose outputs share memory with each other, or with another's numbers, are refused: they would be scaled twice.

@@ -107,9 +107,10 @@ __device__ __forceinline__ float clip_factor(const ClipArgs &A, bool tell)
 #pragma unroll 8
     for (uint32_t i = threadIdx.x; i < A.parts; i += kThreads) v += A.sums[i];
     const double norm = sqrt(block_total(v));
-    const float factor = norm > A.max_norm && norm < __builtin_inf() ? (float)(A.max_norm / norm) : 1.f;
+    const float told = (float)norm;  // (decided on this one: a norm that a program sees as an infinity has scaled nothing)
+    const float factor = norm > A.max_norm && told < __builtin_inff() ? (float)(A.max_norm / norm) : 1.f;
     if (tell && threadIdx.x == 0) {
-        A.norm[0] = (float)norm;
+        A.norm[0] = told;
         if (A.factor) A.factor[0] = factor;
     }
     return factor;
