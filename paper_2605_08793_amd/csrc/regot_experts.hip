@@ -260,7 +260,8 @@ int check_tensors(int64_t count, const regot_tensor *list, bool clip)
         if (list[t].count < 0 || list[t].count > kMaxNumbers) return REGOT_ERR_DIM;
         if (bad_type(list[t].type)) return REGOT_ERR_ARG;
         if (list[t].count > 0 && (!list[t].data || (clip && !list[t].out))) return REGOT_ERR_NULL;
-        if (misaligned(list[t].data, element_bytes(list[t].type)) || misaligned(list[t].out, element_bytes(list[t].type))) return REGOT_ERR_ALIGN;
+        const size_t b = element_bytes(list[t].type);
+        if (misaligned(list[t].data, b) || (clip && misaligned(list[t].out, b))) return REGOT_ERR_ALIGN;
     }
     return REGOT_OK;
 }
