@@ -127,6 +127,16 @@ __device__ __forceinline__ uint32_t die_order(uint32_t b, uint32_t n)
     return die * each + min(die, more) + b / kDies;
 }
 
-__device__ __forceinline__ float sigmoid(float g) { return 1.0f / (1.0f + __expf(-g)); }
+// s(g) = 1 / (1 + exp(-g)).  The fast exponential is that of a rounded product with log2 e, so it is off by about |g| units of the last place: at most 2^-17 of itself before it
+// is 0, which 16 bits do not see.  For results of 32 bits it is the exact one to a unit, of -|g|, so that it does not overflow where s(g) still has bits.
+template <int TYPE>
+__device__ __forceinline__ float sigmoid(float g)
+{
+    if constexpr (TYPE == REGOT_F32) {
+        const float e = expf(-fabsf(g));
+        return (g < 0.0f ? e : 1.0f) / (1.0f + e);
+    }
+    return 1.0f / (1.0f + __expf(-g));
+}
 
 }  // namespace regot

@@ -138,7 +138,7 @@ __global__ void __launch_bounds__(kFewWaves *kLanes) expert_few_kernel(const Gro
         if constexpr (GATE) {
             float h[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) h[e] = v[0][e] * sigmoid(v[0][e]) * v[1][e];
+            for (int e = 0; e < 4; ++e) h[e] = v[0][e] * sigmoid<TYPE>(v[0][e]) * v[1][e];
             store(A.Y, A.ldY, c, h, A.m - c);
             if (A.saved) {
                 store(A.saved, A.ldSaved, c, v[0], A.m - c);

@@ -664,7 +664,7 @@ __device__ __forceinline__ void expert_tile(const GroupArgs &A, const Run &run, 
         };
         results<TYPE, kFragRows, kHalf, ACROSS, kMine>(mine, [&](int x, int y, int e) {
             const float gate = result(x, y, e);
-            return gate * sigmoid(gate) * result(x, kUp + y, e);
+            return gate * sigmoid<TYPE>(gate) * result(x, kUp + y, e);
         }, store(static_cast<char *>(A.Y), A.ldY));
         if (A.saved) {
             results<TYPE, kFragRows, kHalf, ACROSS, kMine>(mine, result, store(static_cast<char *>(A.saved), A.ldSaved));
@@ -683,7 +683,7 @@ __device__ __forceinline__ void expert_tile(const GroupArgs &A, const Run &run, 
             Raw dg[4], du[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float p = sigmoid(of.g[e]), D = __uint_as_float(v[e]);
+                const float p = sigmoid<TYPE>(of.g[e]), D = __uint_as_float(v[e]);
                 dg[e] = Score<TYPE>::put(D * of.u[e] * (p * (1.0f + of.g[e] * (1.0f - p))));
                 du[e] = Score<TYPE>::put(D * (of.g[e] * p));
             }
