@@ -191,8 +191,11 @@ __device__ __forceinline__ f32x4 multiply(u32x4 a, u32x4 b, f32x4 c)
     }
 }
 
-// 8 numbers of 32 bits as three of 8 significant bits each, which add up to them exactly (numbers that are not finite, or round to infinity, give a NaN)
+// 8 numbers of 32 bits, times 2^24, as three of 8 significant bits each.  The scaled number's last bit is not below 2^-125, so the pieces are normal numbers or 0, and add up to it exactly,
+// whatever number of 32 bits it was.  (Numbers that are not finite, or from 2^104 on, give a NaN or an infinity.)
 struct Pieces {
+    static constexpr float kScale = 0x1p24f, kUnscale = 0x1p-48f;  // of a number; of a product of two
+
     u32x4 high, mid, low;
     static __device__ __forceinline__ uint32_t rounded(float x, float y)
     {
@@ -204,7 +207,7 @@ struct Pieces {
     {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            float x = __uint_as_float(i < 2 ? a[2 * i] : b[2 * i - 4]), y = __uint_as_float(i < 2 ? a[2 * i + 1] : b[2 * i - 3]);
+            float x = kScale * __uint_as_float(i < 2 ? a[2 * i] : b[2 * i - 4]), y = kScale * __uint_as_float(i < 2 ? a[2 * i + 1] : b[2 * i - 3]);
             high[i] = rounded(x, y);
             x -= __uint_as_float(high[i] << 16);
             y -= __uint_as_float(high[i] & 0xffff0000u);
@@ -545,8 +548,9 @@ __device__ __forceinline__ void expert_tile(const GroupArgs &A, const Run &run, 
         for (int x = 0; x < kFragRows; ++x) multiplied(acc[x]);
     } else {
         // Numbers of 32 bits are multiplied in pieces.  A tile whose sums are not all finite is summed once more as the numbers are, and gives its results in the place of
-        // those that are not, so that infinities and NaNs are those of the numbers.  us, pieces / numbers as they are: 8192 rows of 60 experts, 2048 by 2 x 1024 with the gate
-        // 600 / 829, gradients of 2048 x 1024 611 / 833, of 777 x 555 with 2997 rows of 12 107 / 137.  The splitting (361 vector instructions for 96 products) bounds it.
+        // those that are not, so that infinities and NaNs are those of the numbers (and those from 2^80 on, which the scale takes beyond 32 bits, are right too).  us, pieces /
+        // numbers as they are: 8192 rows of 60 experts, 2048 by 2 x 1024 with the gate 591 / 775, gradients of 2048 x 1024 608 / 840, of 777 x 555 with 2997 rows of 12 115 / 134.  The
+        // splitting (430 vector instructions for 96 products) bounds it; 64 of them are the scale's (without it, and with what it keeps lost: 568, 584, 110).
         const auto stretch = [&](const char *at, bool pieces) {
             if constexpr (TYPE == REGOT_F32) {
                 if (pieces) {
@@ -629,7 +633,10 @@ __device__ __forceinline__ void expert_tile(const GroupArgs &A, const Run &run, 
             bool all_finite = true;
 #pragma unroll
             for (int xy = 0; xy < kFragRows * kFragCols; ++xy) all_finite &= finite(acc[xy / kFragCols][xy % kFragCols]);
-            if (__builtin_expect(!__syncthreads_and(all_finite), 0)) {
+            const bool again = !__syncthreads_and(all_finite);
+#pragma unroll
+            for (int xy = 0; xy < kFragRows * kFragCols; ++xy) acc[xy / kFragCols][xy % kFragCols] *= Pieces::kUnscale;
+            if (__builtin_expect(again, 0)) {
                 f32x4 first[kFragRows][kFragCols];
                 __builtin_memcpy(first, acc, sizeof(acc));
                 pass(false);
