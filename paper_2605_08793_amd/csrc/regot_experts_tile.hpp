@@ -14,7 +14,7 @@ __device__ const uint32_t kNoNumbers[8] = {};  // what is loaded in the place of
 // for it but s_waitcnt vmcnt.  (As the compiler's builtin it would make every read of LDS behind it wait, whatever it reads.)
 __device__ __forceinline__ void load_to_lds(const char *p, uint32_t lds)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(p) : "memory");  // (M0 is used by nothing else here)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(p) : "memory", "m0");
 }
 
 __device__ __forceinline__ uint32_t lds_address(const void *p)
