@@ -65,3 +65,28 @@ def test_halves_of_the_experts(rows, starts, d, m, dtype):
         for a, b in parts:
             B.regot_expert_product(X, W[a:b], start[a:b + 1], Y)
         check(Y, z, tol, starts, "Y")
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=TYPE_IDS)
+@pytest.mark.parametrize("rows,starts,d,m", [(90, [40, 60, 61, 61, 70, 75, 77, 79, 80], 64, 40), (1000, [300, 500, 500, 700], 72, 40), (1000, [300, 500, 700], 33, 17), (9000, [4000, 8700], 64, 40)],
+                         ids=["few", "whole", "odd", "in parts"])
+def test_weight_gradients(rows, starts, d, m, dtype):
+    """Rows of no run hold NaN, and slots of no token: a gradient that looked at one would be NaN."""
+    gen = torch.Generator().manual_seed(rows)
+    start, k = torch.tensor(starts, device="cuda"), 2
+    dY, X = matrix(gen, rows, m, dtype), matrix(gen, rows, d, dtype)
+    order = torch.randint(0, rows * k, (rows,), generator=gen, dtype=torch.int32)
+    order[:starts[0]] = -1
+    order[starts[-1]:] = -1
+    for gather in (False, True):
+        there = X.cpu().double()[order.long().clamp(min=0) // k] if gather else X.cpu().double()
+        g, x = dY.clone(), X.clone()
+        for t in (g,) if gather else (g, x):
+            t[:starts[0]] = float("nan")
+            t[starts[-1]:] = float("nan")
+        for out in {dtype, torch.float32}:
+            dW = torch.full((len(starts) - 1, m, d), 7.0, dtype=out, device="cuda")
+            ws = torch.empty(B.regot_expert_weight_grad_workspace_bytes(rows, m, d, len(starts) - 1), dtype=torch.uint8, device="cuda")
+            B.regot_expert_weight_grad(g, x, start, dW, order=order.cuda() if gather else None, k=k if gather else 1, workspace=ws)
+            want, tol = ref.weight_grad(dY.cpu().double(), there, starts)
+            ref.close(dW, want, ref.rounded(want, tol, out), f"dW {out} {gather}")
