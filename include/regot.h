@@ -687,7 +687,8 @@ int regot_row_route_grad(int64_t n, int64_t m,
  *     with leading dimensions in elements, aligned to their elements.  (Products whose matrices begin at multiples of 16 bytes, with
  *     rows of whole multiples of 16 bytes, are faster: they go from memory to LDS without registers between.)
  *   - Rows that belong to one expert are a run: start[e] .. start[e+1] - 1.  Rows in front of start[0] and from start[experts] on belong to none:
- *     they are not read and not written.  start[] has to ascend; what lies outside 0 .. rows is not followed.
+ *     they are not read and not written, so a call may have some of a layer's experts (start + e, W + e * strideW).  start[] has to ascend; what lies outside 0 .. rows is
+ *     not followed.  What a launch is planned for is all `rows`: where most of them belong to none, calls on fewer rows are faster.
  *   - Outputs that share memory with an input or with each other are refused (REGOT_ERR_ARG); the rows of one may lie between those of the other,
  *     at the same distance.  Non-finite numbers follow IEEE arithmetic within their row (weight gradients: within their expert).
  *   - Sums are added up in a fixed order: the same call gives the same bits.  0 <= experts <= REGOT_ROW_MAX_EXPERTS, 1 <= k <= REGOT_ROW_MAX_CHOICES.
@@ -771,7 +772,7 @@ int regot_expert_combine_grad(int64_t n, int k, int64_t m, int64_t rows,
  *     norm[0]   = sqrt(sum of the squares of all numbers of all tensors), squares and sums in fp64
  *     factor[0] = max_norm / norm where norm > max_norm, else 1; 1 too where norm[0] is not finite (a norm beyond fp32 is told as inf): a program looks at
  *                 norm and leaves the step out
- *     out       = factor * data, rounded once, for each tensor; out may be data, and is then not written where factor is 1
+ *     out       = factor * data in fp32, rounded to its type, for each tensor; out may be data, and is then not written where factor is 1
  * `list` is a HOST array, read during the call; each tensor is `count` numbers without gaps.  Types may differ.  regot_grad_norm does not look at
  * `out`.  Tensors whose outputs share memory with each other, or with another's numbers, are refused: they would be scaled twice.
  * max_norm > 0 (inf: nothing is scaled).  count <= 2^40.  The workspace's size depends on the tensors' counts.

@@ -170,7 +170,8 @@ void launch(const GroupArgs &A, const TilePlan &P, int type, hipStream_t s)
 // So they are taken from `least` tiles on:
 // weight gradients 2 rounds; products 2.5 (576 tiles: 16384 rows of 16, 1024 x 2048 90 / 80; 720: 2048 x 2560 188 / 206), but none of fewer than 192 rows an expert, which
 // leave most of a tall tile empty (600 rows of 128, 1024 x 2048 133 / 109, 16384 rows 160 / 156); behind the gate, where a tile ends with as many reads as writes and nothing
-// else runs on its unit, 4 rounds of long sums (65536 rows of 64, 1024 outputs, sums of 512 238 / 201, 1024 296 / 273, 2048 411 / 417, 4096 655 / 711).
+// else runs on its unit, 4 rounds of long sums (65536 rows of 64, 1024 outputs, sums of 512 238 / 201, 1024 296 / 273, 2048 411 / 417, 4096 655 / 711; where each expert has 1024 rows, which
+// fill tall tiles, sums of 1536 306 / 324, 2048 352 / 388, 4096 556 / 650).
 constexpr int64_t kNever = INT64_MAX;
 
 int64_t least_tall(int kind, int64_t rows, int64_t d, int64_t experts)
@@ -189,7 +190,8 @@ int choose_tile(int type, bool direct, int64_t least, Tiles tiles)
 }
 
 // (us, tiles of 64 x 128 / few rows, bf16, 60 experts: 1400 x 2048, 480 rows 79 / 68, 960 72 / 86; 1400 x 4096 147 / 129, 148 / 167; 512 x 4096 55 / 45, 53 / 57; 16 of 2048 x 4096, 256
-// rows 58 / 52)
+// rows 58 / 52; fp32, 4 / 8 / 12 / 16 rows of each: 60 of 1400 x 2048 204 / 138, 187 / 137, 187 / 149, 187 / 174, 16 of 2048 x 2048 117 / 59, 114 / 59, 114 / 59, 114 / 60, 256 of 1024 x
+// 512 151 / 118, 147 / 118, 145 / 119, 145 / 178; bf16, short sums: 60 of 1400 x 1024 33 / 40, 33 / 41, 34 / 46, 34 / 58)
 constexpr int64_t kFewRows = 12;  // rows of an expert, on average
 
 // How many stretches of 32 rows of W a workgroup of the kernel for few rows has, of `all` that each of `runs` experts' weights have: four rounds of workgroups, one to a
